@@ -37,7 +37,7 @@ extern "C" {
 #define XORENC_API
 #endif
 
-#define XORENC_VERSION 0x00020300u
+#define XORENC_VERSION 0x00020400u
 
 enum {
   XORENC_OK = 0,
@@ -332,6 +332,105 @@ XORENC_API int32_t xorenc_spmm(const xorenc_layer *layer, const void *X, int32_t
 #define XORENC_SPMM_WORKSPACE_BYTES (12u << 20)
 XORENC_API int32_t xorenc_spmm_ws(const xorenc_layer *layer, const void *X, int32_t x_dtype, int64_t ldx, int32_t B, float *Y,
                                   int64_t ldy, void *workspace, int64_t workspace_bytes, void *hip_stream);
+
+/*
+ * Dense layers in 8 bits: the layers of a network that are not pruned, or that are decoded once because they multiply many
+ * columns.  A matrix is held as e4m3 values (OCP 8-bit floating point: sign, 4 bits of exponent, 3 of mantissa, largest
+ * 448, no infinities) with one fp32 scale per block: element (r, c) stands for Q[r][c] * S[r / block_rows][c / 128].
+ * Activations (tokens x features) have blocks of 1 x 128, weights (outputs x inputs) blocks of 128 x 128; the last block of
+ * a row or column may be a short one.
+ *
+ * Where the library quantises, a block's scale is max(amax / 448, 2^-126) with amax its largest magnitude, and its values
+ * are y * (1 / scale) in fp32, rounded to nearest even.  The scale of a block that holds a NaN is NaN, with an infinity
+ * (and no NaN) infinity, so that what is multiplied by it is not finite either.
+ *
+ * Rules beside the general ones above:
+ *   - matrices are row-major, leading dimensions are in elements; rows of e4m3 matrices start on 16-byte boundaries (base address
+ *     and leading dimension), other rows may start anywhere (16-byte boundaries are faster).  Bytes between a row's last
+ *     element and the next multiple of 16 may be read, and never reach a result;
+ *   - S has two strides where it belongs to activations: element (r, b) is S[r * s_row + b * s_blk].  s_row = 1 (block column
+ *     by block column) is what the kernels write and read fastest;
+ *   - calls with no rows (tokens) succeed and enqueue nothing;
+ *   - outputs do not overlap inputs, except where an entry point says so.
+ */
+#define XORENC_FP8_BLOCK 128
+
+/*
+ * `matrices` matrices of rows x cols (element (r, c) of matrix i: X[i * x_stride + r * ldx + c], and so on for Q; scale (r, b)
+ * of matrix i: S[i * s_stride + r * s_row + b * s_blk]) to 8 bits, in blocks of block_rows (1 or 128) x 128.
+ * XORENC_ELIMIT from 2^28 - 16 blocks of one row, or 2^24 of 128, on in one matrix.
+ */
+XORENC_API int32_t xorenc_quant_fp8(const void *X, int32_t x_dtype, int64_t ldx, int64_t x_stride, int32_t matrices, int64_t rows,
+                                    int32_t cols, int32_t block_rows, uint8_t *Q, int64_t ldq, int64_t q_stride, float *S,
+                                    int64_t s_row, int64_t s_blk, int64_t s_stride, void *hip_stream);
+
+/*
+ * The residual's addition and the RMS norm, with the result in 8 bits (blocks of 1 x 128):
+ *   t = X + residual;  y = t / sqrt(mean(t^2) + eps) * weight;  Q, S = y
+ * in fp32 (t is not rounded before it is normed).  residual, total and Y may be NULL: nothing is added, t or y is not stored.
+ * total and Y have X's type; weight (cols values, contiguous) has its own.  total may be X or residual itself.  Y[r * y_row +
+ * c * y_col]: with y_col = 1 rows of features, with y_row = 1 the columns that xorenc_spmm multiplies.  XORENC_ELIMIT from 2^22 rows on.
+ */
+XORENC_API int32_t xorenc_add_rmsnorm_fp8(const void *X, int32_t x_dtype, int64_t ldx, const void *residual, int64_t ldr,
+                                          const void *weight, int32_t w_dtype, int64_t rows, int32_t cols, float eps, void *total,
+                                          int64_t ldt, void *Y, int64_t y_row, int64_t y_col, uint8_t *Q, int64_t ldq, float *S,
+                                          int64_t s_row, int64_t s_blk, void *hip_stream);
+
+/*
+ * Q, S = gate / (1 + exp(-gate)) * up, in blocks of 1 x 128.  gate and up share the leading dimension: the halves of one
+ * product's rows, usually.  XORENC_ELIMIT as xorenc_quant_fp8.
+ */
+XORENC_API int32_t xorenc_silu_mul_fp8(const void *gate, const void *up, int32_t x_dtype, int64_t ldx, int64_t rows, int32_t cols,
+                                       uint8_t *Q, int64_t ldq, float *S, int64_t s_row, int64_t s_blk, void *hip_stream);
+
+/*
+ * Y = A W^T: A (M x K, blocks of 1 x 128, scale (m, b) at SA[m * sa_row + b * sa_blk]), W (N x K, blocks of 128 x 128, scale
+ * (i, b) at SW[i * ldsw + b]), Y (M x N, XORENC_X_F32 or XORENC_X_BF16).  Scaled sums of blocks are added in fp32.  bf16 results
+ * come from the 8-bit matrix instruction, whose sums inside a block are 1.5e-5 of the result off (2-norm, Gaussian
+ * values); fp32 results from the bf16 one, which is exact in the products and half as fast.
+ * XORENC_ELIMIT beyond 4194240 rows of A or 2^24 rows or columns of W.
+ */
+XORENC_API int32_t xorenc_matmul_fp8(const uint8_t *A, int64_t lda, const float *SA, int64_t sa_row, int64_t sa_blk, const uint8_t *W,
+                                     int64_t ldw, const float *SW, int64_t ldsw, int32_t M, int32_t N, int32_t K, void *Y,
+                                     int32_t y_dtype, int64_t ldy, void *hip_stream);
+
+/*
+ * A mixture of experts: `experts` pairs of matrices W13 (2 inner x hidden: the gates' rows, then the ups') and W2 (hidden x
+ * inner) in e4m3 with blocks of 128 x 128, counted from each matrix's first row, and the router (experts x hidden, the type of X).
+ * Matrix e starts at W13 + e * w13_stride bytes (a multiple of 16), its scales at S13 + e * s13_stride elements.
+ */
+typedef struct xorenc_moe {
+  uint32_t struct_size; /* = sizeof(xorenc_moe), ABI guard */
+  int32_t experts, hidden, inner;
+  const void *router;
+  int64_t ld_router;
+  const uint8_t *W13;
+  int64_t ld_w13, w13_stride;
+  const float *S13;
+  int64_t ld_s13, s13_stride;
+  const uint8_t *W2;
+  int64_t ld_w2, w2_stride;
+  const float *S2;
+  int64_t ld_s2, s2_stride;
+} xorenc_moe;
+
+#define XORENC_MOE_MAX_TOKENS 64
+#define XORENC_MOE_MAX_EXPERTS 256
+#define XORENC_MOE_MAX_PICKS 16
+
+/*
+ * The whole layer for a few tokens (X tokens x hidden, Y likewise and of the same type; Y may be X):
+ *   logits = router x (fp32);  the `picks` experts with the largest logits, the lowest index of equals;
+ *   share = softmax over all experts, with renormalise != 0 divided by the picked ones' sum;
+ *   y = sum over the picks of share * W2_e (silu(G_e x) * (U_e x)).
+ * Activations are not rounded to 8 bits; the inner ones keep 16 bits of mantissa (24 for fp32 X).  Weights of experts that no
+ * token picks are not read.  The same bits on every call.  workspace: DEV, 16-byte aligned, xorenc_moe_workspace bytes, contents
+ * undefined before and after.  XORENC_ELIMIT beyond the limits above, and for hidden > 2^24 or inner > 2^23.
+ */
+XORENC_API int32_t xorenc_moe_workspace(int32_t tokens, int32_t hidden, int32_t inner, int32_t experts, int32_t picks, int32_t x_dtype,
+                                        int64_t *bytes /*HOST*/);
+XORENC_API int32_t xorenc_moe_fp8(const xorenc_moe *layer, const void *X, int32_t x_dtype, int64_t ldx, int32_t tokens, int32_t picks,
+                                  int32_t renormalise, void *Y, int64_t ldy, void *workspace, int64_t workspace_bytes, void *hip_stream);
 
 #ifdef __cplusplus
 }

@@ -27,8 +27,20 @@ from .binding import (
     unpack,
     version,
 )
+from .fp8 import (
+    FP8_BLOCK,
+    MOE_MAX_EXPERTS,
+    MOE_MAX_PICKS,
+    MOE_MAX_TOKENS,
+    add_rmsnorm_fp8,
+    matmul_fp8,
+    moe_fp8,
+    quant_fp8,
+    silu_mul_fp8,
+)
 
 __all__ = [
+    "FP8_BLOCK", "MOE_MAX_EXPERTS", "MOE_MAX_PICKS", "MOE_MAX_TOKENS", "add_rmsnorm_fp8", "matmul_fp8", "moe_fp8", "quant_fp8", "silu_mul_fp8",
     "OUT_BF16", "OUT_F32", "OUT_PLANES", "PackedLayer", "XorencError", "check_packed", "decode", "encode", "encode_exhaustive", "encode_static", "STATIC_SCRATCH_BYTES", "SPMM_WORKSPACE_BYTES",
     "pack_bits",
     "paper_export", "paper_import", "paper_sizes", "get_sizes", "library_path", "load_library", "pack", "spmm", "strerror", "unpack", "version",

@@ -1,0 +1,188 @@
+// Shared by the kernels for dense layers in 8 bits: e4m3 values (sign, 4 bits of exponent, 3 of mantissa, largest 448, no
+// infinities) with one fp32 scale for each block of 128 columns.
+#ifndef XORENC_FP8_H
+#define XORENC_FP8_H
+
+#include <hip/hip_runtime.h>
+
+#include "xorenc_internal.h"
+
+typedef __attribute__((ext_vector_type(8))) __bf16 bf16x8;
+typedef __attribute__((ext_vector_type(2))) __bf16 bf16x2;
+typedef __attribute__((ext_vector_type(4))) float f32x4;
+typedef __attribute__((ext_vector_type(8))) int i32x8;
+typedef __attribute__((ext_vector_type(4))) uint32_t u32x4;
+typedef __attribute__((ext_vector_type(2))) uint32_t u32x2;
+
+namespace xorenc_fp8_detail {
+
+constexpr int kBlock = XORENC_FP8_BLOCK;
+constexpr float kE4m3Most = 448.f;
+constexpr float kLeastScale = 1.1754943508222875e-38f;  // 2^-126: its reciprocal is finite
+
+// The scale of a block from the bits of its largest magnitude (taken as integers, so that infinities and NaN come through).
+__device__ inline float block_scale(uint32_t amax_bits) {
+  const float s = __uint_as_float(amax_bits) / kE4m3Most;
+  return s < kLeastScale ? kLeastScale : s;
+}
+
+__device__ inline uint32_t magnitude_bits(float v) { return __float_as_uint(v) & 0x7fffffffu; }
+
+// Four fp32 values as e4m3, nearest-even.
+__device__ inline uint32_t pack_e4m3(float a, float b, float c, float d) {
+  int w = __builtin_amdgcn_cvt_pk_fp8_f32(a, b, 0, false);
+  return (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(c, d, w, true);
+}
+
+__device__ inline float bf16_lo(uint32_t w) { return __uint_as_float(w << 16); }
+__device__ inline float bf16_hi(uint32_t w) { return __uint_as_float(w & 0xffff0000u); }
+
+// x / (1 + exp(-x)).  The exponential's argument is rounded once in base 2: 4e-8 |x| of relative error, far below what 8
+// bits keep; exp(-x) = infinity gives -0.
+__device__ inline float silu(float x) { return x * __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(x * -1.44269504f)); }
+
+// fp32 -> bf16, nearest-even (the compiler takes the conversion instruction; NaN stays NaN)
+__device__ inline uint16_t to_bf16(float v) { return __builtin_bit_cast(uint16_t, (__bf16)v); }
+__device__ inline uint32_t to_bf16x2(float a, float b) { return (uint32_t)to_bf16(a) | ((uint32_t)to_bf16(b) << 16); }
+
+struct F32 {
+  typedef float Elem;
+  static __device__ inline float load(const Elem *p) { return *p; }
+  static __device__ inline void store(Elem *p, float v) { *p = v; }
+  static __device__ inline void load8(const Elem *p, float *v) {  // 16-byte aligned
+    const f32x4 a = *reinterpret_cast<const f32x4 *>(p), b = *reinterpret_cast<const f32x4 *>(p + 4);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) v[i] = a[i], v[4 + i] = b[i];
+  }
+  static __device__ inline void store8(Elem *p, const float *v) {
+    *reinterpret_cast<f32x4 *>(p) = f32x4{v[0], v[1], v[2], v[3]};
+    *reinterpret_cast<f32x4 *>(p + 4) = f32x4{v[4], v[5], v[6], v[7]};
+  }
+};
+
+struct BF16 {
+  typedef uint16_t Elem;
+  static __device__ inline float load(const Elem *p) { return __uint_as_float((uint32_t)*p << 16); }
+  static __device__ inline void store(Elem *p, float v) { *p = to_bf16(v); }
+  static __device__ inline void load8(const Elem *p, float *v) {
+    const u32x4 a = *reinterpret_cast<const u32x4 *>(p);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) v[2 * i] = bf16_lo(a[i]), v[2 * i + 1] = bf16_hi(a[i]);
+  }
+  static __device__ inline void store8(Elem *p, const float *v) {
+    *reinterpret_cast<u32x4 *>(p) =
+        u32x4{to_bf16x2(v[0], v[1]), to_bf16x2(v[2], v[3]), to_bf16x2(v[4], v[5]), to_bf16x2(v[6], v[7])};
+  }
+};
+
+// Up to eight values of a row from column c on; columns from `cols` on are zero.  `wide`: the row's pieces of eight are
+// 16-byte aligned.
+template <class T>
+__device__ inline void load_piece(const typename T::Elem *row, int c, int cols, bool wide, float *v) {
+  if (wide && c + 8 <= cols) {
+    T::load8(row + c, v);
+  } else {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) v[i] = c + i < cols ? T::load(row + c + i) : 0.f;
+  }
+}
+
+template <class T>
+__device__ inline void store_piece(typename T::Elem *row, int c, int cols, bool wide, const float *v) {
+  if (wide && c + 8 <= cols) {
+    T::store8(row + c, v);
+  } else {
+#pragma unroll
+    for (int i = 0; i < 8; ++i)
+      if (c + i < cols) T::store(row + c + i, v[i]);
+  }
+}
+
+// Eight values as e4m3 to row[c ..].  Rows of Q start on 16-byte boundaries and c is a multiple of eight.
+__device__ inline void store_e4m3_piece(uint8_t *row, int c, int cols, const float *v, float inv) {
+  const u32x2 w = {pack_e4m3(v[0] * inv, v[1] * inv, v[2] * inv, v[3] * inv),
+                   pack_e4m3(v[4] * inv, v[5] * inv, v[6] * inv, v[7] * inv)};
+  if (c + 8 <= cols) {
+    *reinterpret_cast<u32x2 *>(row + c) = w;
+  } else {
+#pragma unroll
+    for (int i = 0; i < 8; ++i)
+      if (c + i < cols) row[c + i] = (uint8_t)(w[i >> 2] >> (8 * (i & 3)));
+  }
+}
+
+// Largest of 16 neighbouring lanes' values, on all of them: a row of the DPP network.
+__device__ inline uint32_t max_of_16_lanes(uint32_t v) {
+  v = max(v, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0xB1, 0xf, 0xf, true));   // quad: 1 0 3 2
+  v = max(v, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0x4E, 0xf, 0xf, true));   // quad: 2 3 0 1
+  v = max(v, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0x141, 0xf, 0xf, true));  // half row mirrored
+  v = max(v, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0x140, 0xf, 0xf, true));  // row mirrored
+  return v;
+}
+
+// Operands of the matrix instructions for 128 columns of 16 rows.  Lane l holds 32 values of row l % 16: columns
+// 16 (l / 16) + 0..15 of the first 64 columns, then of the second 64, so that each 16-byte load of a wave covers 64 contiguous
+// bytes of every row.  Which of the instruction's k a column becomes does not matter as long as both operands agree.
+__device__ inline int piece_column(int lane, int piece) { return piece * 64 + (lane >> 4) * 16; }
+
+// One of a lane's two 16-byte pieces of row `row`, columns from `c` on; columns from K on are zero, whatever lies there.  A piece
+// that holds a valid column is inside the allocation: rows start on 16-byte boundaries.
+__device__ inline u32x4 load_e4m3_piece(const uint8_t *row, int c, int K) {
+  u32x4 v = {0u, 0u, 0u, 0u};
+  if (c < K) {
+    v = *reinterpret_cast<const u32x4 *>(row + c);
+    if (c + 16 > K) {
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const int left = K - (c + 4 * i);
+        v[i] = left >= 4 ? v[i] : left <= 0 ? 0u : v[i] & ((1u << (8 * left)) - 1u);
+      }
+    }
+  }
+  return v;
+}
+
+struct E4m3Operand {
+  u32x4 piece[2];
+};
+
+__device__ inline i32x8 as_operand(const E4m3Operand &o) {
+  return i32x8{(int)o.piece[0][0], (int)o.piece[0][1], (int)o.piece[0][2], (int)o.piece[0][3],
+               (int)o.piece[1][0], (int)o.piece[1][1], (int)o.piece[1][2], (int)o.piece[1][3]};
+}
+
+// Quarter q of a lane's 32 values (columns 8 (q % 2) .. + 7 of piece q / 2) as bf16, which holds every e4m3 value exactly.
+__device__ inline bf16x8 quarter_as_bf16(const E4m3Operand &o, int q) {
+  const uint32_t w0 = o.piece[q >> 1][2 * (q & 1)], w1 = o.piece[q >> 1][2 * (q & 1) + 1];
+  const bf16x2 a = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w0, 1.f, false), b = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w0, 1.f, true);
+  const bf16x2 c = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w1, 1.f, false), d = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w1, 1.f, true);
+  return bf16x8{a[0], a[1], b[0], b[1], c[0], c[1], d[0], d[1]};
+}
+
+// The product of 16 rows of A and 16 of B over 128 columns.  Lane l gets column l % 16 (a row of B), rows 4 (l / 16) .. + 3
+// (of A).  The 8-bit instruction adds products aligned to the largest of them: 1.5e-5 of the result for Gaussian
+// values (2-norm), which results of 16 bits do not show.  Results of 32 bits come from the bf16 instruction, which
+// multiplies e4m3 values exactly and adds in fp32, at half the rate.
+template <bool EXACT>
+__device__ inline f32x4 product_128(const E4m3Operand &a, const E4m3Operand &b) {
+  f32x4 d = {0.f, 0.f, 0.f, 0.f};
+  if constexpr (EXACT) {
+#pragma unroll
+    for (int q = 0; q < 4; ++q)
+      d = __builtin_amdgcn_mfma_f32_16x16x32_bf16(quarter_as_bf16(a, q), quarter_as_bf16(b, q), d, 0, 0, 0);
+  } else {
+    d = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(as_operand(a), as_operand(b), d, 0, 0, 0, 0, 0, 0);
+  }
+  return d;
+}
+
+// Host checks shared by the entry points.
+inline bool known_dtype(int32_t t) { return t == XORENC_X_F32 || t == XORENC_X_BF16; }
+inline int dtype_bytes(int32_t t) { return t == XORENC_X_F32 ? 4 : 2; }
+inline bool aligned_to(const void *p, size_t n) { return ((uintptr_t)p & (n - 1)) == 0; }
+// pieces of eight values of every row on 16-byte boundaries
+inline bool wide_rows(const void *p, int64_t ld, int32_t t) { return aligned_to(p, 16) && ld % (16 / dtype_bytes(t)) == 0; }
+
+}  // namespace xorenc_fp8_detail
+
+#endif

@@ -14,11 +14,11 @@ const char *xorenc_strerror(int32_t code) {
   switch (code) {
     case XORENC_OK: return "ok";
     case XORENC_EINVAL: return "invalid argument (null pointer, negative or inconsistent size)";
-    case XORENC_EUNSUPPORTED: return "unsupported configuration (n_out in {64,128,192,256}, n_in in 4..32, q in 1..4)";
+    case XORENC_EUNSUPPORTED: return "unsupported configuration (n_out in {64,128,192,256}, n_in in 4..32, q in 1..4; dtype; rows per block)";
     case XORENC_EALIGN: return "misaligned pointer or leading dimension";
     case XORENC_EHIP: return "HIP runtime call failed";
     case XORENC_EFORMAT: return "malformed compressed data";
-    case XORENC_ELIMIT: return "request exceeds a fixed capacity of the library (static scratch area)";
+    case XORENC_ELIMIT: return "request exceeds a fixed capacity of the library (static scratch area, sizes of a launch)";
     default: return "unknown xorenc status";
   }
 }
