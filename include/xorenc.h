@@ -388,7 +388,8 @@ XORENC_API int32_t xorenc_silu_mul_fp8(const void *gate, const void *up, int32_t
  * (i, b) at SW[i * ldsw + b]), Y (M x N, XORENC_X_F32 or XORENC_X_BF16).  Scaled sums of blocks are added in fp32.  bf16 results
  * come from the 8-bit matrix instruction, whose sums inside a block are 1.5e-5 of the result off (2-norm, Gaussian
  * values); fp32 results from the bf16 one, which is exact in the products and half as fast.
- * XORENC_ELIMIT beyond 4194240 rows of A or 2^24 rows or columns of W.
+ * XORENC_ELIMIT beyond 4194240 rows of A, 2^22 tiles of 128 x 128 results, 2^22 columns (or such a leading dimension of A or W), sa_row = 2^20, and
+ * where 256 * sa_row + sa_blk * ceil(K / 128) reaches 2^29.
  */
 XORENC_API int32_t xorenc_matmul_fp8(const uint8_t *A, int64_t lda, const float *SA, int64_t sa_row, int64_t sa_blk, const uint8_t *W,
                                      int64_t ldw, const float *SW, int64_t ldsw, int32_t M, int32_t N, int32_t K, void *Y,

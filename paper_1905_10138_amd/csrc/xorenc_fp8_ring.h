@@ -1,0 +1,161 @@
+// The block-scaled product where tiles of 256 x 256 would be too few: a workgroup owns BN = 16 TN WN rows of W and
+// BM = 16 TM WM rows of A, and keeps a ring of NS stages of both in LDS, so that NS - 1 stages are on their way from memory
+// while one is multiplied.  KG groups of WN x WM waves take the blocks of 128 columns in turn (a stage holds KG blocks)
+// and add up at the end: more bytes on their way, and fewer barriers, for the same tile.
+#ifndef XORENC_FP8_RING_H
+#define XORENC_FP8_RING_H
+
+#include "xorenc_fp8_tile.h"
+
+namespace xorenc_fp8_detail {
+
+template <int TN, int TM, int WN, int WM, int KG, int NS>
+struct RingShape {
+  static constexpr int BN = 16 * TN * WN, BM = 16 * TM * WM, GROUP = WN * WM, WAVES = GROUP * KG;
+  static constexpr int BLOCK = (BN + BM) * 128 + BM * 4;  // one block's rows of W, of A, and the scales of A
+  static constexpr int STAGE = KG * BLOCK;
+  static constexpr int SUMS = KG > 1 ? (KG - 1) * BN * BM * 4 : 0;
+  static constexpr int LDS = NS * STAGE > SUMS ? NS * STAGE : SUMS;
+  static constexpr int PER = (BN + BM) / 8 / GROUP;  // 1 KB loads of a wave per block
+  static_assert((BN + BM) % (8 * GROUP) == 0 && BM % 64 == 0 && 128 % (16 * TN) == 0 && LDS <= 160 * 1024, "shape");
+};
+
+template <int TN, int TM, int WN, int WM, int KG, int NS, bool EXACT>
+__global__ __launch_bounds__(WN *WM *KG * 64) void matmul_ring_kernel(MatmulArgs g, int wide, int n_tiles, int m_tiles, int per_xcd) {
+  typedef RingShape<TN, TM, WN, WM, KG, NS> Shape;
+  constexpr int BN = Shape::BN, BM = Shape::BM, PER = Shape::PER, BLOCK = Shape::BLOCK, STAGE = Shape::STAGE;
+  extern __shared__ __attribute__((aligned(1024))) uint8_t ring_lds[];
+  const int tile = (blockIdx.x & 7) * per_xcd + (blockIdx.x >> 3);  // XCDs take runs of tiles that share rows of W
+  if (tile >= n_tiles * m_tiles) return;
+  const int tile_n = tile / m_tiles, tile_m = tile - tile_n * m_tiles;
+  const int n0 = tile_n * BN, m0 = tile_m * BM;
+  const int tid = threadIdx.x, lane = tid & 63, r = lane & 15;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int kg = wave / Shape::GROUP, in_group = wave % Shape::GROUP, wn = in_group % WN, wm = in_group / WN;
+  const uint32_t lds0 = __builtin_amdgcn_readfirstlane((uint32_t)(size_t)(__attribute__((address_space(3))) uint8_t *)ring_lds);
+
+  // ---- loads: this wave's part of its group's blocks
+  const uint64_t w_base = reinterpret_cast<uint64_t>(g.W + n0 * g.ldw), a_base = reinterpret_cast<uint64_t>(g.A + m0 * g.lda),
+                 s_base = reinterpret_cast<uint64_t>(g.SA + m0 * g.sa_row);
+  const u32x4 w_desc = {(uint32_t)w_base, (uint32_t)(w_base >> 32) & 0xffffu, (uint32_t)kMostTileBytes, kRawBuffer};
+  const u32x4 a_desc = {(uint32_t)a_base, (uint32_t)(a_base >> 32) & 0xffffu, (uint32_t)kMostTileBytes, kRawBuffer};
+  const u32x4 s_desc = {(uint32_t)s_base, (uint32_t)(s_base >> 32) & 0xffffu, (uint32_t)kMostTileBytes, kRawBuffer};
+  const int lane_row = lane >> 3;
+  auto row_of = [&](int i) {  // of W, then of A
+    const int row = (in_group * PER + i) * 8;
+    return row < BN ? row : row - BN;
+  };
+  auto of_w = [&](int i) { return (in_group * PER + i) * 8 < BN; };
+  auto chunk_of = [&](int i) { return ((lane & 7) ^ (((row_of(i) + lane_row) >> 1) & 7)) * 16; };
+  uint32_t at[PER];
+#pragma unroll
+  for (int i = 0; i < PER; ++i)
+    at[i] = (uint32_t)(min(row_of(i) + lane_row, (of_w(i) ? g.N - n0 : g.M - m0) - 1) * (of_w(i) ? g.ldw : g.lda)) + (uint32_t)chunk_of(i);
+  const int s_rows = in_group % (BM / 64) * 64;
+  const uint32_t s_at = (uint32_t)(min(s_rows + lane, g.M - m0 - 1) * g.sa_row) * 4u, s_step = (uint32_t)(g.sa_blk * 4);
+  const int tail = g.K & (kBlock - 1), stages = (g.blocks + KG - 1) / KG;
+  // Stage s of this group's blocks into its slot.  A block past the last one reads as zero, and so do chunks behind column K.
+  auto fetch = [&](int s) {
+    const int b = s * KG + kg;
+    const uint32_t to = lds0 + (uint32_t)(s % NS) * STAGE + kg * BLOCK;
+    const int most = b >= g.blocks ? 0 : tail && b == g.blocks - 1 ? tail : kBlock;  // columns of the block
+    const uint32_t col = (uint32_t)b * kBlock;
+#pragma unroll
+    for (int i = 0; i < PER; ++i) {
+      const uint32_t off = chunk_of(i) >= most ? kBeyond : at[i];
+      asm volatile("s_mov_b32 m0, %0\n\tbuffer_load_dwordx4 %1, %2, %3 offen lds" ::"s"(to + (in_group * PER + i) * 1024), "v"(off),
+                   "s"(of_w(i) ? w_desc : a_desc), "s"(most ? col : 0u)
+                   : "memory");
+    }
+    asm volatile("s_mov_b32 m0, %0\n\tbuffer_load_dword %1, %2, %3 offen lds" ::"s"(to + (BN + BM) * 128 + s_rows * 4),
+                 "v"(most ? s_at : kBeyond), "s"(s_desc), "s"(most ? (uint32_t)b * s_step : 0u)
+                 : "memory");
+  };
+  const int w_row = (n0 + wn * (TN * 16)) / kBlock;
+  const float *const sw_row = g.SW + (int64_t)(w_row * kBlock < g.N ? w_row : 0) * g.ldsw;
+  float sw_run = sw_row[min(lane, g.blocks - 1)];
+
+  f32x4 acc[TN][TM];
+#pragma unroll
+  for (int i = 0; i < TN; ++i)
+#pragma unroll
+    for (int j = 0; j < TM; ++j) acc[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
+  const uint32_t off = (uint32_t)(r * 128 + (((lane >> 4) ^ ((r >> 1) & 7)) * 16));
+  constexpr int LOADS = PER + 1;  // of a wave per stage
+#pragma unroll
+  for (int s = 0; s < NS - 1; ++s) fetch(s);  // (stages past the last read as zero: every wave has as many loads on their way)
+  for (int s = 0; s < stages; ++s) {
+    // this stage has landed, and every wave has read the one before, whose slot is filled next
+    asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"((NS - 2) * LOADS) : "memory");
+    fetch(s + NS - 1);
+    const int b = s * KG + kg;
+    uint8_t *const slot = ring_lds + (uint32_t)(s % NS) * STAGE + kg * BLOCK;
+    if ((tail & 15) && s == stages - 1) {  // what the last chunk of a row holds behind column K
+      if (b == g.blocks - 1) {
+        for (int row = in_group * 64 + lane; row < BN + BM; row += Shape::GROUP * 64) {
+          uint8_t *const p = slot + row * 128 + (((tail >> 4) ^ (((row < BN ? row : row - BN) >> 1) & 7)) * 16);
+          u32x4 v = *reinterpret_cast<u32x4 *>(p);
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            const int left = (tail & 15) - 4 * i;
+            v[i] = left >= 4 ? v[i] : left <= 0 ? 0u : v[i] & ((1u << (8 * left)) - 1u);
+          }
+          *reinterpret_cast<u32x4 *>(p) = v;
+        }
+      }
+      asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
+    }
+    if (b >= g.blocks) continue;  // (uniform; the last stage)
+    E4m3Operand w[TN], a[TM];
+    float sa[TM];
+#pragma unroll
+    for (int j = 0; j < TM; ++j) sa[j] = reinterpret_cast<const float *>(slot + (BN + BM) * 128)[(wm * TM + j) * 16 + r];
+#pragma unroll
+    for (int j = 0; j < TM; ++j)
+#pragma unroll
+      for (int p = 0; p < 2; ++p)
+        a[j].piece[p] = *reinterpret_cast<const u32x4 *>(slot + BN * 128 + (wm * TM + j) * 2048 + (off ^ (64u * p)));
+#pragma unroll
+    for (int i = 0; i < TN; ++i)
+#pragma unroll
+      for (int p = 0; p < 2; ++p) w[i].piece[p] = *reinterpret_cast<const u32x4 *>(slot + (wn * TN + i) * 2048 + (off ^ (64u * p)));
+    if ((b & 63) == kg % 64 && b >= 64) sw_run = sw_row[min((b & ~63) + lane, g.blocks - 1)];
+    const float sw = __int_as_float(__builtin_amdgcn_readlane(__float_as_int(sw_run), b & 63));
+#pragma unroll
+    for (int j = 0; j < TM; ++j) {
+      const float f = sa[j] * sw;
+#pragma unroll
+      for (int i = 0; i < TN; ++i) {
+        const f32x4 d = product_128<EXACT>(w[i], a[j]);
+#pragma unroll
+        for (int k = 0; k < 4; ++k) acc[i][j][k] += f * d[k];
+      }
+    }
+  }
+  asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");  // (no load may land in what follows)
+  if constexpr (KG > 1) {  // the groups' sums meet in LDS, in the order of the groups
+    f32x4 *const sums = reinterpret_cast<f32x4 *>(ring_lds);
+    if (kg > 0) {
+#pragma unroll
+      for (int i = 0; i < TN; ++i)
+#pragma unroll
+        for (int j = 0; j < TM; ++j) sums[(((kg - 1) * Shape::GROUP + in_group) * (TN * TM) + i * TM + j) * 64 + lane] = acc[i][j];
+    }
+    __syncthreads();
+    if (kg == 0) {
+#pragma unroll
+      for (int k = 1; k < KG; ++k)
+#pragma unroll
+        for (int i = 0; i < TN; ++i)
+#pragma unroll
+          for (int j = 0; j < TM; ++j) acc[i][j] += sums[(((k - 1) * Shape::GROUP + in_group) * (TN * TM) + i * TM + j) * 64 + lane];
+    }
+    __syncthreads();
+    if (kg > 0) return;
+  }
+  store_tile<TN, TM, EXACT>(g, acc, ring_lds + in_group * (16 * TM * 16 * TN * 4), m0 + wm * (16 * TM), n0 + wn * (16 * TN), lane, wide);
+}
+
+}  // namespace xorenc_fp8_detail
+
+#endif
