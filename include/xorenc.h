@@ -426,7 +426,7 @@ typedef struct xorenc_moe {
  *   y = sum over the picks of share * W2_e (silu(G_e x) * (U_e x)).
  * Activations are not rounded to 8 bits; the inner ones keep 16 bits of mantissa (24 for fp32 X).  Weights of experts that no
  * token picks are not read.  The same bits on every call.  workspace: DEV, 16-byte aligned, xorenc_moe_workspace bytes, contents
- * undefined before and after.  XORENC_ELIMIT beyond the limits above, and for hidden > 2^24 or inner > 2^23.
+ * undefined before and after.  XORENC_ELIMIT beyond the limits above, and for hidden or inner > 2^17.
  */
 XORENC_API int32_t xorenc_moe_workspace(int32_t tokens, int32_t hidden, int32_t inner, int32_t experts, int32_t picks, int32_t x_dtype,
                                         int64_t *bytes /*HOST*/);

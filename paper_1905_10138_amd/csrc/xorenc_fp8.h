@@ -146,6 +146,16 @@ struct E4m3Operand {
   u32x4 piece[2];
 };
 
+// A lane's part of a whole block of a row, and of the last one, of which `left` columns are left.
+__device__ inline void load_block(const uint8_t *row, int lane, E4m3Operand &o) {
+#pragma unroll
+  for (int k = 0; k < 2; ++k) o.piece[k] = *reinterpret_cast<const u32x4 *>(row + piece_column(lane, k));
+}
+__device__ inline void load_last_block(const uint8_t *row, int lane, int left, E4m3Operand &o) {
+#pragma unroll
+  for (int k = 0; k < 2; ++k) o.piece[k] = load_e4m3_piece(row, piece_column(lane, k), left);
+}
+
 __device__ inline i32x8 as_operand(const E4m3Operand &o) {
   return i32x8{(int)o.piece[0][0], (int)o.piece[0][1], (int)o.piece[0][2], (int)o.piece[0][3],
                (int)o.piece[1][0], (int)o.piece[1][1], (int)o.piece[1][2], (int)o.piece[1][3]};
@@ -174,6 +184,34 @@ __device__ inline f32x4 product_128(const E4m3Operand &a, const E4m3Operand &b) 
     d = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(as_operand(a), as_operand(b), d, 0, 0, 0, 0, 0, 0);
   }
   return d;
+}
+
+// multiply(step, operands) for step = 0 .. steps - 1, with load(step, operands) AHEAD steps before it.  The loads are
+// unconditional (past the end the last step's again): a load that may or may not have been issued would make the compiler
+// wait for all loads on their way, not for the oldest ones.  For the same reason `load` has no branches, and loads
+// no value through the scalar cache.
+template <int AHEAD, class Operands, class Load, class Multiply>
+__device__ inline void pipeline(int steps, Load load, Multiply multiply) {
+  if (steps <= 0) return;
+  Operands o[AHEAD + 1];
+#pragma unroll
+  for (int k = 0; k < AHEAD; ++k) load(min(k, steps - 1), o[k]);
+  for (int s = 0; s < steps; s += AHEAD + 1) {  // (one exit, for the same reason)
+#pragma unroll
+    for (int k = 0; k <= AHEAD; ++k) {
+      load(min(s + k + AHEAD, steps - 1), o[(k + AHEAD) % (AHEAD + 1)]);
+      __builtin_amdgcn_sched_barrier(0);
+      if (s + k < steps) multiply(s + k, o[k]);
+    }
+  }
+}
+
+// Zero, in a vector register as far as the compiler knows: an address that it is added to is loaded from through the vector
+// memory path, although it is the same for all lanes.
+__device__ inline int vector_zero() {
+  int z;
+  asm volatile("v_mov_b32 %0, 0" : "=v"(z));
+  return z;
 }
 
 // Host checks shared by the entry points.

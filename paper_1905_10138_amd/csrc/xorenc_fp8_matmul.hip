@@ -34,7 +34,7 @@ __device__ inline void store_result(const MatmulArgs &g, int m, int n, f32x4 v, 
 // in turn, each with all of the tile, and operands go from memory to the registers of the wave that multiplies them, the next
 // block's while this one's are multiplied; the sums meet in LDS, in the order of the waves.  Every CU so has work of its own
 // where tiles of the other kernel would be too few, and no barrier stands between a load and its use.
-template <int MT, int NT, int WAVES, bool EXACT>
+template <int MT, int NT, int WAVES, int AHEAD, bool EXACT>
 __global__ __launch_bounds__(WAVES * 64) void matmul_rows_kernel(MatmulArgs g, int wide, int n_tiles) {
   constexpr int TILES = MT * NT, PASS = TILES < 8 ? TILES : 8;  // tiles whose sums are in LDS at a time
   __shared__ f32x4 part[WAVES][PASS][64];
@@ -46,11 +46,11 @@ __global__ __launch_bounds__(WAVES * 64) void matmul_rows_kernel(MatmulArgs g, i
   const float *const sa_base = g.SA + m0 * g.sa_row;
   uint32_t w_at[NT], a_at[MT], sa_at[MT];
 #pragma unroll
-  for (int i = 0; i < NT; ++i) w_at[i] = (uint32_t)(min(16 * i + r, g.N - n0 - 1) * g.ldw) + piece_column(lane, 0);
+  for (int i = 0; i < NT; ++i) w_at[i] = (uint32_t)(min(16 * i + r, g.N - n0 - 1) * g.ldw);
 #pragma unroll
   for (int i = 0; i < MT; ++i) {
     const int m = min(16 * i + r, g.M - m0 - 1);
-    a_at[i] = (uint32_t)(m * g.lda) + piece_column(lane, 0);
+    a_at[i] = (uint32_t)(m * g.lda);
     sa_at[i] = (uint32_t)(m * g.sa_row);
   }
   const float *const sw = g.SW + (int64_t)(n0 / kBlock) * g.ldsw;
@@ -58,30 +58,10 @@ __global__ __launch_bounds__(WAVES * 64) void matmul_rows_kernel(MatmulArgs g, i
     E4m3Operand w[NT], a[MT];
     float sa[MT], sw;
   };
-  auto load = [&](int b, Operands &o) {
-    const uint8_t *const wb = w_base + (int64_t)b * kBlock, *const ab = a_base + (int64_t)b * kBlock;
+  const int zero = vector_zero();
+  auto load_scales = [&](int b, Operands &o) {
     const float *const sb = sa_base + b * g.sa_blk;
-    if ((b + 1) * kBlock <= g.K) {  // uniform
-#pragma unroll
-      for (int i = 0; i < NT; ++i)
-#pragma unroll
-        for (int p = 0; p < 2; ++p) o.w[i].piece[p] = *reinterpret_cast<const u32x4 *>(wb + w_at[i] + 64 * p);
-#pragma unroll
-      for (int i = 0; i < MT; ++i)
-#pragma unroll
-        for (int p = 0; p < 2; ++p) o.a[i].piece[p] = *reinterpret_cast<const u32x4 *>(ab + a_at[i] + 64 * p);
-    } else {
-      const int left = g.K - b * kBlock;
-#pragma unroll
-      for (int p = 0; p < 2; ++p) {
-        const int c = piece_column(lane, p);
-#pragma unroll
-        for (int i = 0; i < NT; ++i) o.w[i].piece[p] = load_e4m3_piece(wb + w_at[i] - piece_column(lane, 0), c, left);
-#pragma unroll
-        for (int i = 0; i < MT; ++i) o.a[i].piece[p] = load_e4m3_piece(ab + a_at[i] - piece_column(lane, 0), c, left);
-      }
-    }
-    o.sw = sw[b];
+    o.sw = sw[b + zero];
 #pragma unroll
     for (int i = 0; i < MT; ++i) o.sa[i] = sb[sa_at[i]];
   };
@@ -90,7 +70,7 @@ __global__ __launch_bounds__(WAVES * 64) void matmul_rows_kernel(MatmulArgs g, i
   for (int i = 0; i < MT; ++i)
 #pragma unroll
     for (int j = 0; j < NT; ++j) acc[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
-  auto multiply = [&](const Operands &o) {
+  auto multiply = [&](int, const Operands &o) {
 #pragma unroll
     for (int i = 0; i < MT; ++i) {
       const float f = o.sa[i] * o.sw;
@@ -102,17 +82,24 @@ __global__ __launch_bounds__(WAVES * 64) void matmul_rows_kernel(MatmulArgs g, i
       }
     }
   };
-  Operands o[2];
-  int b = wave;
-  if (b < g.blocks) load(b, o[0]);
-  while (b < g.blocks) {
-    if (b + WAVES < g.blocks) load(b + WAVES, o[1]);
-    multiply(o[0]);
-    b += WAVES;
-    if (b >= g.blocks) break;
-    if (b + WAVES < g.blocks) load(b + WAVES, o[0]);
-    multiply(o[1]);
-    b += WAVES;
+  const int whole = g.K / kBlock;
+  pipeline<AHEAD, Operands>((whole - wave + WAVES - 1) / WAVES, [&](int s, Operands &o) {
+    const int b = wave + s * WAVES;
+#pragma unroll
+    for (int i = 0; i < NT; ++i) load_block(w_base + (int64_t)b * kBlock + w_at[i], lane, o.w[i]);
+#pragma unroll
+    for (int i = 0; i < MT; ++i) load_block(a_base + (int64_t)b * kBlock + a_at[i], lane, o.a[i]);
+    load_scales(b, o);
+  }, multiply);
+  if (whole < g.blocks && whole % WAVES == wave) {  // the last block, a short one
+    const int c = whole * kBlock, left = g.K - c;
+    Operands o;
+#pragma unroll
+    for (int i = 0; i < NT; ++i) load_last_block(w_base + c + w_at[i], lane, left, o.w[i]);
+#pragma unroll
+    for (int i = 0; i < MT; ++i) load_last_block(a_base + c + a_at[i], lane, left, o.a[i]);
+    load_scales(whole, o);
+    multiply(0, o);
   }
 #pragma unroll
   for (int t0 = 0; t0 < TILES; t0 += PASS) {
@@ -138,10 +125,10 @@ void launch_tile(const MatmulArgs &g, bool wide, hipStream_t st) {
                      (int)wide, n_tiles, m_tiles, per_xcd);
 }
 
-template <int MT, int NT, int WAVES, bool EXACT>
+template <int MT, int NT, int WAVES, int AHEAD, bool EXACT>
 void launch_rows_of_a(const MatmulArgs &g, bool wide, hipStream_t st) {
   const int n_tiles = (g.N + 16 * NT - 1) / (16 * NT), m_tiles = (g.M + 16 * MT - 1) / (16 * MT);
-  hipLaunchKernelGGL((matmul_rows_kernel<MT, NT, WAVES, EXACT>), dim3((unsigned)(n_tiles * m_tiles)), dim3(WAVES * 64), 0, st, g, (int)wide, n_tiles);
+  hipLaunchKernelGGL((matmul_rows_kernel<MT, NT, WAVES, AHEAD, EXACT>), dim3((unsigned)(n_tiles * m_tiles)), dim3(WAVES * 64), 0, st, g, (int)wide, n_tiles);
 }
 
 template <int TN, int TM, int WN, int WM, int KG, int NS, bool EXACT>
@@ -205,8 +192,8 @@ int32_t dispatch_matmul(const MatmulArgs &g, bool wide, hipStream_t st) {
     case 2: launch_tile<4, 2, 2, 2, EXACT>(g, wide, st); break;
     case 3: launch_ring<2, 2, 2, 2, 2, 2, EXACT>(g, wide, st); break;
     case 4: launch_ring<2, 2, 2, 2, 1, 2, EXACT>(g, wide, st); break;
-    case 5: launch_rows_of_a<1, 1, 8, EXACT>(g, wide, st); break;
-    case 6: launch_rows_of_a<2, 2, 8, EXACT>(g, wide, st); break;
+    case 5: launch_rows_of_a<1, 1, 8, 2, EXACT>(g, wide, st); break;
+    case 6: launch_rows_of_a<2, 2, 8, 1, EXACT>(g, wide, st); break;
     default: return XORENC_ELIMIT;
   }
   return xorenc_internal_check_launch();

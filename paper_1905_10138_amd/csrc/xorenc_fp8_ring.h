@@ -12,12 +12,13 @@ namespace xorenc_fp8_detail {
 template <int TN, int TM, int WN, int WM, int KG, int NS>
 struct RingShape {
   static constexpr int BN = 16 * TN * WN, BM = 16 * TM * WM, GROUP = WN * WM, WAVES = GROUP * KG;
-  static constexpr int BLOCK = (BN + BM) * 128 + BM * 4;  // one block's rows of W, of A, and the scales of A
+  static constexpr int SCALES = BM < 64 ? 64 : BM;             // scales of A that are fetched (those of the last row again, past it)
+  static constexpr int BLOCK = (BN + BM) * 128 + SCALES * 4;  // one block's rows of W, of A, and the scales of A
   static constexpr int STAGE = KG * BLOCK;
   static constexpr int SUMS = KG > 1 ? (KG - 1) * BN * BM * 4 : 0;
   static constexpr int LDS = NS * STAGE > SUMS ? NS * STAGE : SUMS;
   static constexpr int PER = (BN + BM) / 8 / GROUP;  // 1 KB loads of a wave per block
-  static_assert((BN + BM) % (8 * GROUP) == 0 && BM % 64 == 0 && 128 % (16 * TN) == 0 && LDS <= 160 * 1024, "shape");
+  static_assert((BN + BM) % (8 * GROUP) == 0 && SCALES % 64 == 0 && 128 % (16 * TN) == 0 && LDS <= 160 * 1024, "shape");
 };
 
 template <int TN, int TM, int WN, int WM, int KG, int NS, bool EXACT>
@@ -51,7 +52,7 @@ __global__ __launch_bounds__(WN *WM *KG * 64) void matmul_ring_kernel(MatmulArgs
 #pragma unroll
   for (int i = 0; i < PER; ++i)
     at[i] = (uint32_t)(min(row_of(i) + lane_row, (of_w(i) ? g.N - n0 : g.M - m0) - 1) * (of_w(i) ? g.ldw : g.lda)) + (uint32_t)chunk_of(i);
-  const int s_rows = in_group % (BM / 64) * 64;
+  const int s_rows = in_group % (Shape::SCALES / 64) * 64;
   const uint32_t s_at = (uint32_t)(min(s_rows + lane, g.M - m0 - 1) * g.sa_row) * 4u, s_step = (uint32_t)(g.sa_blk * 4);
   const int tail = g.K & (kBlock - 1), stages = (g.blocks + KG - 1) / KG;
   // Stage s of this group's blocks into its slot.  A block past the last one reads as zero, and so do chunks behind column K.
@@ -86,7 +87,10 @@ __global__ __launch_bounds__(WN *WM *KG * 64) void matmul_ring_kernel(MatmulArgs
   for (int s = 0; s < NS - 1; ++s) fetch(s);  // (stages past the last read as zero: every wave has as many loads on their way)
   for (int s = 0; s < stages; ++s) {
     // this stage has landed, and every wave has read the one before, whose slot is filled next
-    asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"((NS - 2) * LOADS) : "memory");
+    if constexpr (Shape::GROUP > 1)
+      asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"((NS - 2) * LOADS) : "memory");
+    else  // (a wave on its own)
+      asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" ::"n"((NS - 2) * LOADS) : "memory");
     fetch(s + NS - 1);
     const int b = s * KG + kg;
     uint8_t *const slot = ring_lds + (uint32_t)(s % NS) * STAGE + kg * BLOCK;

@@ -1,12 +1,17 @@
 // A mixture-of-experts layer for a few tokens: Y = sum over a token's picks of share * W2_e (silu(G_e x) * (U_e x)), with
 // expert weights in e4m3 (a scale per 128 x 128 block) and everything else in 16 or 32 bits.
 //
-// Three launches: the router's logits; the gated activations h of the picked experts; their second product and the sum
-// over picks.  The bytes of the picked experts' weights bound the last two, so both stream 16 rows of weights per workgroup
-// from memory to registers, its waves taking the blocks of the reduction in turn.  e4m3 values become bf16 exactly and
-// multiply bf16 terms of the activations (one for bf16 activations, three for fp32, which sum to the value exactly), so that
-// nothing is rounded to 8 bits on the way; h is kept as bf16 terms that hold 16 (24) bits.  Tokens are the columns of the
-// matrix instruction: an expert multiplies those that picked it, the others' columns are zero.
+// Four launches: the router's logits; the picks (not for a single token, whose picks every workgroup finds by itself); the gated
+// activations h of the picked experts; their second product and the sum over picks.  The bytes of the picked experts'
+// weights bound the last two, so both stream 16 rows of weights per workgroup from memory to registers, its waves taking
+// parts of the reduction.  e4m3 values become bf16 exactly and multiply bf16 terms of the activations (one for bf16
+// activations, three for fp32, which sum to the value exactly), so that nothing is rounded to 8 bits on the way; h is kept
+// as bf16 terms that hold 16 (24) bits.  The tokens that picked an expert are the columns of its matrix instructions, 16 at a
+// time; lanes of columns without a token load nothing.
+//
+// Terms of x and h lie in the workspace in the order in which lanes load them: a row is a run of blocks of 128 columns (zero
+// behind the last column), a block its terms one after the other, a term four quarters of 32 columns: those that the
+// four lanes of a row take with one load, 64 contiguous bytes.
 #include "xorenc_fp8.h"
 
 namespace xorenc_fp8_detail {
@@ -15,17 +20,28 @@ namespace {
 constexpr int kMostExperts = XORENC_MOE_MAX_EXPERTS, kMostPicks = XORENC_MOE_MAX_PICKS, kMostTokens = XORENC_MOE_MAX_TOKENS;
 static_assert(kMostExperts == 256 && kMostTokens == 64, "four experts per lane, four column tiles");
 
+// An expert that some token picked: its tokens are `count` entries of the list of pairs of a token and an expert that it
+// picked, from `first` on.  Pairs are ordered by expert, then by token; row i of h is pair i's.
+struct Use {
+  int expert, first, count, unused;
+};
+
 struct MoeArgs {
   const uint8_t *W13, *W2;
   const float *S13, *S2;
   int64_t ldw13, w13_stride, lds13, s13_stride, ldw2, w2_stride, lds2, s2_stride;
   int T, H, I, E, top, renormalise;
-  const float *logits;      // [T][E]
-  const uint16_t *x_terms;  // bf16 terms of x: [term][T][x_ld], zero from H to the next multiple of 16
-  int64_t x_ld, x_term;
-  uint16_t *h_terms;        // [term][T * top][h_ld], zero from I to the next multiple of 16
-  int64_t h_ld, h_term;
+  float *logits;            // [T][E]
+  Use *uses;                // experts in use, ascending; min(E, T * top) of them, the last ones with count 0
+  int *n_used;              // how many
+  uint8_t *use_tokens;      // [use][kMostTokens]
+  float *shares;            // of the entries
+  uint16_t *x_terms, *h_terms;  // rows of tokens, and of pairs
+  int x_row, h_row;             // bytes of a row
 };
+
+// Where column c of a block is in each of its terms.
+__device__ inline int term_place(int c) { return (c >> 6) * 64 + ((c >> 3) & 1) * 32 + ((c >> 4) & 3) * 8 + (c & 7); }
 
 // What rounding to bf16 leaves of a value; nothing of what is not finite (infinity less infinity would be NaN).
 __device__ inline float rest_of_bf16(float v) {
@@ -35,72 +51,56 @@ __device__ inline float rest_of_bf16(float v) {
 
 // ---------------------------------------------------------------------------------------------- router
 
-// Logits in fp32: a wave per expert and four tokens.  The waves behind them write the bf16 terms of x where the products
-// cannot read it as it is.
+// Logits in fp32: a workgroup per expert and four tokens, its waves share the columns.  The workgroups behind them write the
+// bf16 terms of x.
 template <class T, int TERMS>
 __global__ __launch_bounds__(256) void router_kernel(const typename T::Elem *__restrict__ X, int64_t ldx, int wide,
                                                      const typename T::Elem *__restrict__ router, int64_t ldr, int r_wide, int tokens,
                                                      int H, int E, float *__restrict__ logits, uint16_t *__restrict__ terms,
-                                                     int64_t x_ld, int64_t x_term, int logit_groups) {
-  const int lane = threadIdx.x & 63;
-  if ((int)blockIdx.x >= logit_groups) {  // x_ld / 8 pieces per token
-    const int pieces = (int)(x_ld / 8);
+                                                     int logit_groups) {
+  __shared__ float part[4][4];
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  if ((int)blockIdx.x >= logit_groups) {  // eight columns a thread
+    const int pieces = (H + kBlock - 1) / kBlock * 16;
     const int64_t i = (int64_t)(blockIdx.x - logit_groups) * 256 + threadIdx.x;
     if (i >= (int64_t)tokens * pieces) return;
     const int t = (int)(i / pieces), c = (int)(i - (int64_t)t * pieces) * 8;
     float v[8];
     load_piece<T>(X + t * ldx, c, H, wide, v);
+    uint16_t *const dst = terms + ((int64_t)t * (pieces / 16) + c / kBlock) * (TERMS * kBlock) + term_place(c % kBlock);
 #pragma unroll
     for (int k = 0; k < TERMS; ++k) {
-      float w[8];
-#pragma unroll
-      for (int j = 0; j < 8; ++j) w[j] = v[j];
-      BF16::store8(terms + k * x_term + t * x_ld + c, w);
+      BF16::store8(dst + k * kBlock, v);
 #pragma unroll
       for (int j = 0; j < 8; ++j) v[j] = rest_of_bf16(v[j]);
     }
     return;
   }
   const int token_groups = (tokens + 3) / 4;
-  const int w = blockIdx.x * 4 + (threadIdx.x >> 6);
-  if (w >= E * token_groups) return;
-  const int e = w / token_groups, t0 = (w - e * token_groups) * 4;
+  const int e = blockIdx.x / token_groups, t0 = (blockIdx.x - e * token_groups) * 4;
   float acc[4] = {0.f, 0.f, 0.f, 0.f};
-  for (int c = lane * 8; c < H; c += 512) {
-    float r[8];
+  for (int c = threadIdx.x * 8; c < H; c += 2048) {
+    float r[8], v[4][8];
     load_piece<T>(router + e * ldr, c, H, r_wide, r);
 #pragma unroll
-    for (int k = 0; k < 4; ++k) {
-      float v[8];
-      load_piece<T>(X + min(t0 + k, tokens - 1) * ldx, c, H, wide, v);
+    for (int k = 0; k < 4; ++k) load_piece<T>(X + min(t0 + k, tokens - 1) * ldx, c, H, wide, v[k]);
 #pragma unroll
-      for (int j = 0; j < 8; ++j) acc[k] += r[j] * v[j];
-    }
+    for (int k = 0; k < 4; ++k)
+#pragma unroll
+      for (int j = 0; j < 8; ++j) acc[k] += r[j] * v[k][j];
   }
 #pragma unroll
   for (int k = 0; k < 4; ++k) {
 #pragma unroll
     for (int o = 32; o > 0; o >>= 1) acc[k] += __shfl_xor(acc[k], o);
-    if (lane == 0 && t0 + k < tokens) logits[(t0 + k) * E + e] = acc[k];
+    if (lane == 0) part[wave][k] = acc[k];
   }
+  __syncthreads();
+  const int k = threadIdx.x;
+  if (k < 4 && t0 + k < tokens) logits[(t0 + k) * E + e] = (part[0][k] + part[1][k]) + (part[2][k] + part[3][k]);
 }
 
 // ---------------------------------------------------------------------------------------------- picks
-
-constexpr uint8_t kNotPicked = 0xff;
-
-// What every workgroup works out for itself from the logits: the experts that some token picked, ascending, and which of
-// a token's picks each of them is.
-template <int MT>
-struct Picks {
-  float share[16 * MT][kMostPicks];
-  uint16_t expert[16 * MT][kMostPicks];
-  uint16_t used[kMostExperts];  // experts in use
-  uint16_t place[kMostExperts]; // of an expert among them
-  uint32_t in_use[kMostExperts / 32];
-  int n_used;
-  uint8_t slot[kMostExperts * 16 * MT];  // [place][token]: which of the token's picks, or kNotPicked
-};
 
 // fp32 -> integers in the same order (NaN above infinity or below its negative, as the sign says)
 __device__ inline uint32_t ordered(float v) {
@@ -109,252 +109,380 @@ __device__ inline uint32_t ordered(float v) {
 }
 __device__ inline float from_ordered(uint32_t k) { return __uint_as_float(k & 0x80000000u ? k & 0x7fffffffu : ~k); }
 
-template <int MT, int WAVES>
-__device__ inline void find_picks(const MoeArgs &g, Picks<MT> &p) {
+// A token's picks, by one wave: lane j gets the j-th (`expert`, `share`).
+__device__ inline void picks_of_token(const MoeArgs &g, int t, int lane, int &expert, float &share) {
+  const float *const row = g.logits + t * g.E;
+  uint32_t key[4];
+  bool left[4];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const int e = lane + 64 * i;
+    left[i] = e < g.E;
+    key[i] = left[i] ? ordered(row[e]) : 0u;
+  }
+  auto largest = [&]() {  // of the keys that are left, the same on all lanes
+    uint32_t m = 0u;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) m = left[i] ? max(m, key[i]) : m;
+    m = max_of_16_lanes(m);
+    return max(max((uint32_t)__builtin_amdgcn_readlane((int)m, 0), (uint32_t)__builtin_amdgcn_readlane((int)m, 16)),
+               max((uint32_t)__builtin_amdgcn_readlane((int)m, 32), (uint32_t)__builtin_amdgcn_readlane((int)m, 48)));
+  };
+  const float most = from_ordered(largest());
+  float sum = 0.f;
+  if (!g.renormalise) {  // shares of a softmax over all experts
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+      if (left[i]) sum += expf(from_ordered(key[i]) - most);
+#pragma unroll
+    for (int o = 32; o > 0; o >>= 1) sum += __shfl_xor(sum, o);
+  }
+  expert = 0, share = 0.f;
+  for (int j = 0; j < g.top; ++j) {  // the largest that is left; the lowest index of equals
+    const uint32_t m = largest();
+    int e = 0;
+#pragma unroll
+    for (int i = 3; i >= 0; --i) {
+      const uint64_t at = __ballot(left[i] && key[i] == m);
+      if (at) e = 64 * i + __builtin_ctzll(at);
+    }
+#pragma unroll
+    for (int i = 0; i < 4; ++i) left[i] = left[i] && e != lane + 64 * i;
+    const float v = expf(from_ordered(m) - most);
+    if (g.renormalise) sum += v;
+    if (lane == j) expert = e, share = v;
+  }
+  share /= sum;
+}
+
+// One workgroup; a wave per token at a time.
+__global__ __launch_bounds__(1024) void picks_kernel(MoeArgs g) {
+  constexpr int WAVES = 16;
+  __shared__ struct {
+    uint64_t tokens[kMostExperts];  // that picked an expert, a bit each
+    float share[kMostTokens][kMostPicks];
+    uint16_t expert[kMostTokens][kMostPicks];
+    uint16_t place[kMostExperts], first[kMostExperts];  // of an expert among those in use; its first pair
+  } p;
   const int tid = threadIdx.x, lane = tid & 63;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-  const int most_used = min(g.E, g.T * g.top);
-  if (tid < kMostExperts / 32) p.in_use[tid] = 0u;
-  for (int i = tid; i < most_used * (16 * MT) / 4; i += WAVES * 64) reinterpret_cast<uint32_t *>(p.slot)[i] = 0xffffffffu;
+  if (tid < kMostExperts) p.tokens[tid] = 0u;
   __syncthreads();
   for (int t = wave; t < g.T; t += WAVES) {
-    const float *const row = g.logits + t * g.E;
-    uint32_t key[4];
-    bool left[4];
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      const int e = lane + 64 * i;
-      left[i] = e < g.E;
-      key[i] = left[i] ? ordered(row[e]) : 0u;
+    int e;
+    float share;
+    picks_of_token(g, t, lane, e, share);
+    if (lane < g.top) {
+      p.expert[t][lane] = (uint16_t)e;
+      p.share[t][lane] = share;
+      atomicOr(reinterpret_cast<unsigned long long *>(&p.tokens[e]), 1ull << t);
     }
-    float first = 0.f, sum = 0.f, mine = 0.f;
-    if (!g.renormalise) {  // shares of a softmax over all experts
-      uint32_t m = max(max(key[0], key[1]), max(key[2], key[3]));
-      m = max_of_16_lanes(m);
-      m = max(max((uint32_t)__builtin_amdgcn_readlane((int)m, 0), (uint32_t)__builtin_amdgcn_readlane((int)m, 16)),
-              max((uint32_t)__builtin_amdgcn_readlane((int)m, 32), (uint32_t)__builtin_amdgcn_readlane((int)m, 48)));
-      const float most = from_ordered(m);
-#pragma unroll
-      for (int i = 0; i < 4; ++i)
-        if (left[i]) sum += expf(from_ordered(key[i]) - most);
-#pragma unroll
-      for (int o = 32; o > 0; o >>= 1) sum += __shfl_xor(sum, o);
-    }
-    for (int j = 0; j < g.top; ++j) {  // the largest that is left; the lowest index of equals
-      uint32_t m = 0u;
-#pragma unroll
-      for (int i = 0; i < 4; ++i) m = left[i] ? max(m, key[i]) : m;
-      m = max_of_16_lanes(m);
-      m = max(max((uint32_t)__builtin_amdgcn_readlane((int)m, 0), (uint32_t)__builtin_amdgcn_readlane((int)m, 16)),
-              max((uint32_t)__builtin_amdgcn_readlane((int)m, 32), (uint32_t)__builtin_amdgcn_readlane((int)m, 48)));
-      int e = -1;
-#pragma unroll
-      for (int i = 3; i >= 0; --i) {
-        const uint64_t at = __ballot(left[i] && key[i] == m);
-        if (at) e = 64 * i + __builtin_ctzll(at);
-      }
-      e = __builtin_amdgcn_readfirstlane(e);
-#pragma unroll
-      for (int i = 0; i < 4; ++i) left[i] = left[i] && e != lane + 64 * i;
-      const float l = from_ordered(m);
-      if (j == 0) first = l;
-      const float v = expf(l - first);
-      if (g.renormalise) sum += v;
-      if (lane == j) mine = v;
-      if (lane == 0) {
-        p.expert[t][j] = (uint16_t)e;
-        atomicOr(&p.in_use[e >> 5], 1u << (e & 31));
-      }
-    }
-    if (lane < g.top) p.share[t][lane] = mine / sum;
   }
   __syncthreads();
-  if (wave == 0) {
-    int n = 0;
+  if (wave == 0) {  // four experts a lane
+    int n[4], sum = 0;  // experts in use << 16 | pairs
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-      const int e = lane + 64 * i;
-      const bool in = (p.in_use[e >> 5] >> (e & 31)) & 1u;
-      const uint64_t all = __ballot(in);
-      if (in) {
-        const int at = n + __popcll(all & ((1ull << lane) - 1ull));
-        p.used[at] = (uint16_t)e;
-        p.place[e] = (uint16_t)at;
-      }
-      n += __popcll(all);
+      const int k = __popcll(p.tokens[4 * lane + i]);
+      n[i] = k ? k | 0x10000 : 0;
+      sum += n[i];
     }
-    if (lane == 0) p.n_used = n;
+    int before = sum;
+#pragma unroll
+    for (int o = 1; o < 64; o <<= 1) {
+      const int v = __shfl_up(before, o);
+      if (lane >= o) before += v;
+    }
+    const int used = __shfl(before, 63) >> 16;
+    before -= sum;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      if (n[i]) {
+        const int e = 4 * lane + i, at = before >> 16, first = before & 0xffff;
+        p.place[e] = (uint16_t)at;
+        p.first[e] = (uint16_t)first;
+        g.uses[at] = Use{e, first, n[i] & 0xffff, 0};
+      }
+      before += n[i];
+    }
+    if (lane == 0) *g.n_used = used;
+    for (int u = used + lane; u < min(g.E, g.T * g.top); u += 64) g.uses[u] = Use{0, 0, 0, 0};
   }
   __syncthreads();
   for (int i = tid; i < g.T * g.top; i += WAVES * 64) {
-    const int t = i / g.top, j = i - t * g.top;
-    p.slot[p.place[p.expert[t][j]] * (16 * MT) + t] = (uint8_t)j;
+    const int t = i / g.top, j = i - t * g.top, e = p.expert[t][j];
+    const int rank = __popcll(p.tokens[e] & ((1ull << t) - 1ull));
+    g.use_tokens[p.place[e] * kMostTokens + rank] = (uint8_t)t;
+    g.shares[p.first[e] + rank] = p.share[t][j];
   }
-  __syncthreads();
 }
 
 // ---------------------------------------------------------------------------------------------- products
 
-// Quarter q of the columns that a lane holds of a row of bf16 values: the columns that quarter_as_bf16 gives of weights.
-__device__ inline bf16x8 term_quarter(const uint16_t *row, int c, int q, int cols) {
-  const int at = c + (q >> 1) * 64 + (q & 1) * 8;
-  u32x4 v = {0u, 0u, 0u, 0u};
-  if (at < cols) v = *reinterpret_cast<const u32x4 *>(row + at);  // (rows are zero up to a multiple of 16)
-  return __builtin_bit_cast(bf16x8, v);
+typedef __amdgpu_buffer_rsrc_t Buffer;
+constexpr int kNoColumn = (int)0x80000000u;  // an offset behind every buffer: reads as zero, from nowhere
+
+// Terms of a lane's columns of a block, in quarters: the columns that quarter_as_bf16 gives of weights.
+template <int TERMS>
+struct TermOperand {
+  u32x4 q[TERMS][4];
+};
+template <int TERMS>
+__device__ inline void load_terms(Buffer rows, int at, int block, TermOperand<TERMS> &o) {
+#pragma unroll
+  for (int k = 0; k < TERMS; ++k)
+#pragma unroll
+    for (int q = 0; q < 4; ++q)
+      o.q[k][q] = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(rows, at + k * 256 + q * 64, block * (TERMS * 256), 0));
+}
+
+// What a wave of the first product needs to know.
+struct UpRows {
+  const uint8_t *gate, *up;                // this lane's row of weights
+  const float *s_gate, *s_up0, *s_up1;     // scales of the gates' rows, of the ups' rows before `edge` and from it on
+  int edge;
+};
+
+template <int N, int TERMS>
+struct UpOperands {
+  E4m3Operand gate, up;
+  TermOperand<TERMS> x[N];
+  float sg, su0, su1;
+};
+
+// Blocks b0 .. b1 - 1 of the reduction for N tiles of 16 tokens.
+template <int N, int MT, int TERMS>
+__device__ inline void up_blocks(const UpRows &w, Buffer x, const int (&x_at)[MT], int H, int lane, int b0, int b1, f32x4 (&gate)[MT],
+                                 f32x4 (&up)[MT]) {
+  typedef UpOperands<N, TERMS> Operands;
+  const int zero = vector_zero();
+  auto multiply = [&](int, Operands &o) {
+    bf16x8 vg[4], vu[4];
+#pragma unroll
+    for (int q = 0; q < 4; ++q) vg[q] = quarter_as_bf16(o.gate, q), vu[q] = quarter_as_bf16(o.up, q);
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+      f32x4 dg = {0.f, 0.f, 0.f, 0.f}, du = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+      for (int k = 0; k < TERMS; ++k)
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+          const bf16x8 v = __builtin_bit_cast(bf16x8, o.x[i].q[k][q]);
+          dg = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vg[q], v, dg, 0, 0, 0);
+          du = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vu[q], v, du, 0, 0, 0);
+        }
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        gate[i][j] += o.sg * dg[j];
+        up[i][j] += (4 * (lane >> 4) + j < w.edge ? o.su0 : o.su1) * du[j];
+      }
+    }
+  };
+  auto load_others = [&](int b, Operands &o) {
+#pragma unroll
+    for (int i = 0; i < N; ++i) load_terms<TERMS>(x, x_at[i], b, o.x[i]);
+    o.sg = w.s_gate[b + zero], o.su0 = w.s_up0[b + zero], o.su1 = w.s_up1[b + zero];
+  };
+  const int whole = H / kBlock;
+  pipeline<0, Operands>(min(b1, whole) - b0, [&](int s, Operands &o) {
+    load_block(w.gate + (b0 + s) * kBlock, lane, o.gate);
+    load_block(w.up + (b0 + s) * kBlock, lane, o.up);
+    load_others(b0 + s, o);
+  }, multiply);
+  if (b0 < b1 && b1 > whole) {  // the last block, a short one
+    const int c = whole * kBlock;
+    Operands o;
+    load_last_block(w.gate + c, lane, H - c, o.gate);
+    load_last_block(w.up + c, lane, H - c, o.up);
+    load_others(whole, o);
+    multiply(0, o);
+  }
 }
 
 // h of 16 rows of an expert for all tokens that picked it.
 template <int MT, int TERMS, int H_TERMS, int WAVES>
-__global__ __launch_bounds__(WAVES * 64) void moe_up_kernel(MoeArgs g) {
-  __shared__ Picks<MT> picks;
+__global__ __launch_bounds__(WAVES * 64, 2) void moe_up_kernel(MoeArgs g) {
   __shared__ f32x4 part[WAVES][2][MT][64];
-  find_picks<MT, WAVES>(g, picks);
-  const int u = blockIdx.y;
-  if (u >= picks.n_used) return;
-  const int e = __builtin_amdgcn_readfirstlane(picks.used[u]);
   const int tid = threadIdx.x, lane = tid & 63, r = lane & 15;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int i0 = blockIdx.x * 16;
+  int e, first, count, token;
+  float one_share = 0.f;
+  if (MT == 1 && g.T == 1) {  // its picks are the experts in use, in their order
+    int expert;
+    picks_of_token(g, 0, lane, expert, one_share);
+    first = blockIdx.y, count = 1, token = 0;
+    e = __builtin_amdgcn_readlane(expert, first);
+    one_share = __shfl(one_share, first);
+    if (blockIdx.x == 0 && tid == 0) {
+      g.uses[first] = Use{e, first, 1, 0};
+      g.use_tokens[first * kMostTokens] = 0;
+      if (first == 0) *g.n_used = g.top;
+    }
+  } else {
+    const Use use = g.uses[blockIdx.y];
+    token = g.use_tokens[blockIdx.y * kMostTokens + lane];
+    e = use.expert, first = use.first, count = use.count;
+    if (count == 0) return;
+  }
+  const int tiles = (count + 15) / 16;
+  const int h_block = i0 / kBlock * (H_TERMS * kBlock) + term_place(i0 % kBlock + 4 * (lane >> 4));  // where this lane's four results go
+  uint16_t *const h = g.h_terms + (int64_t)first * (g.h_row / 2) + h_block;
+  if (i0 >= g.I) {  // columns that fill up the last block
+    for (int col = 16 * wave + r; col < count; col += 16 * WAVES)
+#pragma unroll
+      for (int k = 0; k < H_TERMS; ++k) *reinterpret_cast<u32x2 *>(h + (int64_t)col * (g.h_row / 2) + k * kBlock) = u32x2{0u, 0u};
+    return;
+  }
   const uint8_t *const base = g.W13 + e * g.w13_stride;
+  const float *const s_base = g.S13 + e * g.s13_stride;
   const int row = min(i0 + r, g.I - 1);
-  const uint8_t *const gate_row = base + row * g.ldw13, *const up_row = base + ((int64_t)g.I + row) * g.ldw13;
   // the up rows of a tile lie in two blocks of scales where I is not a multiple of 16
-  const int first = g.I + i0, last = g.I + min(i0 + 15, g.I - 1), edge = (last / kBlock) * kBlock - first;
-  const float *const s_gate = g.S13 + e * g.s13_stride + (int64_t)(i0 / kBlock) * g.lds13;
-  const float *const s_up0 = g.S13 + e * g.s13_stride + (int64_t)(first / kBlock) * g.lds13;
-  const float *const s_up1 = g.S13 + e * g.s13_stride + (int64_t)(last / kBlock) * g.lds13;
-  const uint16_t *x_row[MT];
-  bool picked[MT], any[MT];
+  const int up_first = g.I + i0, up_last = g.I + min(i0 + 15, g.I - 1);
+  const UpRows w = {base + row * g.ldw13, base + ((int64_t)g.I + row) * g.ldw13, s_base + (int64_t)(i0 / kBlock) * g.lds13,
+                    s_base + (int64_t)(up_first / kBlock) * g.lds13, s_base + (int64_t)(up_last / kBlock) * g.lds13,
+                    (up_last / kBlock) * kBlock - up_first};
+  const Buffer x = __builtin_amdgcn_make_buffer_rsrc(g.x_terms, 0, g.T * g.x_row, 0x00020000);
+  int x_at[MT];
 #pragma unroll
   for (int i = 0; i < MT; ++i) {
-    const int t = 16 * i + r;
-    picked[i] = picks.slot[u * (16 * MT) + t] != kNotPicked;
-    any[i] = __ballot(picked[i]) != 0;
-    x_row[i] = g.x_terms + (picked[i] ? t : 0) * g.x_ld;
+    const int t = __shfl(token, (16 * i + r) & 63);
+    x_at[i] = 16 * i + r < count ? t * g.x_row + (lane >> 4) * 16 : kNoColumn;
   }
   f32x4 gate[MT], up[MT];
 #pragma unroll
   for (int i = 0; i < MT; ++i) gate[i] = up[i] = f32x4{0.f, 0.f, 0.f, 0.f};
-  const int blocks = (g.H + kBlock - 1) / kBlock;
-  for (int b = wave; b < blocks; b += WAVES) {
-    const int c = b * kBlock + piece_column(lane, 0);
-    E4m3Operand wg, wu;
-#pragma unroll
-    for (int k = 0; k < 2; ++k) {
-      wg.piece[k] = load_e4m3_piece(gate_row, c + 64 * k, g.H);
-      wu.piece[k] = load_e4m3_piece(up_row, c + 64 * k, g.H);
-    }
-    const float sg = s_gate[b], su0 = s_up0[b], su1 = s_up1[b];
-    f32x4 dg[MT], du[MT];
-#pragma unroll
-    for (int i = 0; i < MT; ++i) dg[i] = du[i] = f32x4{0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-    for (int q = 0; q < 4; ++q) {
-      const bf16x8 vg = quarter_as_bf16(wg, q), vu = quarter_as_bf16(wu, q);
-#pragma unroll
-      for (int i = 0; i < MT; ++i) {
-        if (!any[i]) continue;
-#pragma unroll
-        for (int k = 0; k < TERMS; ++k) {
-          const bf16x8 x = term_quarter(x_row[i] + k * g.x_term, c, q, picked[i] ? g.H : 0);
-          dg[i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vg, x, dg[i], 0, 0, 0);
-          du[i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vu, x, du[i], 0, 0, 0);
-        }
-      }
-    }
-#pragma unroll
-    for (int i = 0; i < MT; ++i)
-#pragma unroll
-      for (int j = 0; j < 4; ++j) {
-        gate[i][j] += sg * dg[i][j];
-        up[i][j] += (4 * (lane >> 4) + j < edge ? su0 : su1) * du[i][j];
-      }
-  }
+  const int blocks = (g.H + kBlock - 1) / kBlock, b0 = blocks * wave / WAVES, b1 = blocks * (wave + 1) / WAVES;
+  if (tiles == 1)
+    up_blocks<1, MT, TERMS>(w, x, x_at, g.H, lane, b0, b1, gate, up);
+  else if (MT == 2 || tiles == 2)
+    up_blocks<(MT < 2 ? 1 : 2), MT, TERMS>(w, x, x_at, g.H, lane, b0, b1, gate, up);
+  else
+    up_blocks<MT, MT, TERMS>(w, x, x_at, g.H, lane, b0, b1, gate, up);
 #pragma unroll
   for (int i = 0; i < MT; ++i) {
     part[wave][0][i][lane] = gate[i];
     part[wave][1][i][lane] = up[i];
   }
   __syncthreads();
-  for (int i = wave; i < MT; i += WAVES) {
-    f32x4 a = part[0][0][i][lane], b = part[0][1][i][lane];
+  for (int i = wave; i < tiles; i += WAVES) {
+    f32x4 a = part[0][0][i][lane], c = part[0][1][i][lane];
 #pragma unroll
-    for (int w = 1; w < WAVES; ++w) {
-      a += part[w][0][i][lane];
-      b += part[w][1][i][lane];
+    for (int k = 1; k < WAVES; ++k) {
+      a += part[k][0][i][lane];
+      c += part[k][1][i][lane];
     }
-    const int t = 16 * i + r;
-    const uint8_t j = picks.slot[u * (16 * MT) + t];
-    if (j == kNotPicked) continue;
-    const float share = picks.share[t][j];
+    const int col = 16 * i + r;
+    if (col >= count) continue;
+    const float share = MT == 1 && g.T == 1 ? one_share : g.shares[first + col];
     const int at = i0 + 4 * (lane >> 4);
-    float h[4];
+    float v[4];
 #pragma unroll
-    for (int k = 0; k < 4; ++k) h[k] = at + k < g.I ? silu(a[k]) * b[k] * share : 0.f;
-    uint16_t *const dst = g.h_terms + ((int64_t)t * g.top + j) * g.h_ld + at;
+    for (int k = 0; k < 4; ++k) v[k] = at + k < g.I ? silu(a[k]) * c[k] * share : 0.f;
 #pragma unroll
     for (int k = 0; k < H_TERMS; ++k) {
-      *reinterpret_cast<u32x2 *>(dst + k * g.h_term) = u32x2{to_bf16x2(h[0], h[1]), to_bf16x2(h[2], h[3])};
+      *reinterpret_cast<u32x2 *>(h + (int64_t)col * (g.h_row / 2) + k * kBlock) = u32x2{to_bf16x2(v[0], v[1]), to_bf16x2(v[2], v[3])};
 #pragma unroll
-      for (int n = 0; n < 4; ++n) h[n] = rest_of_bf16(h[n]);
+      for (int n = 0; n < 4; ++n) v[n] = rest_of_bf16(v[n]);
     }
   }
 }
 
-// 16 columns of Y (rows of W2) for all tokens: the reduction runs over the blocks of all experts in use, ascending.
-template <class T, int MT, int H_TERMS, int WAVES>
-__global__ __launch_bounds__(WAVES * 64) void moe_down_kernel(MoeArgs g, typename T::Elem *__restrict__ Y, int64_t ldy) {
-  __shared__ Picks<MT> picks;
-  __shared__ f32x4 part[WAVES][MT][64];
-  find_picks<MT, WAVES>(g, picks);
-  const int tid = threadIdx.x, lane = tid & 63, r = lane & 15;
-  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-  const int n0 = blockIdx.x * 16;
-  const int64_t row_off = min(n0 + r, g.H - 1) * g.ldw2, s_off = (int64_t)(n0 / kBlock) * g.lds2;
-  f32x4 acc[MT];
+template <int N, int H_TERMS>
+struct DownOperands {
+  E4m3Operand w;
+  TermOperand<H_TERMS> h[N];
+  float scale;
+};
+
+// Blocks b0 .. b1 - 1 of an expert's reduction for N tiles of 16 tokens, from the lane's rows of weights and of h.
+template <int N, int MT, int H_TERMS>
+__device__ inline void down_blocks(const uint8_t *w_row, const float *s_row, Buffer h, const int (&h_at)[MT], int I, int lane, int b0, int b1,
+                                   f32x4 (&acc)[MT]) {
+  typedef DownOperands<N, H_TERMS> Operands;
+  const int zero = vector_zero();
+  auto multiply = [&](int, Operands &o) {
+    bf16x8 v[4];
 #pragma unroll
-  for (int i = 0; i < MT; ++i) acc[i] = f32x4{0.f, 0.f, 0.f, 0.f};
-  const int blocks = (g.I + kBlock - 1) / kBlock, steps = picks.n_used * blocks;
-  for (int s = wave; s < steps; s += WAVES) {
-    const int u = s / blocks, b = s - u * blocks;
-    const int e = __builtin_amdgcn_readfirstlane(picks.used[u]);
-    const int c = b * kBlock + piece_column(lane, 0);
-    const uint8_t *const w_row = g.W2 + e * g.w2_stride + row_off;
-    E4m3Operand w;
-    w.piece[0] = load_e4m3_piece(w_row, c, g.I);
-    w.piece[1] = load_e4m3_piece(w_row, c + 64, g.I);
-    const float sc = g.S2[e * g.s2_stride + s_off + b];
+    for (int q = 0; q < 4; ++q) v[q] = quarter_as_bf16(o.w, q);
 #pragma unroll
-    for (int i = 0; i < MT; ++i) {
-      const int t = 16 * i + r;
-      const uint8_t j = picks.slot[u * (16 * MT) + t];
-      if (!__ballot(j != kNotPicked)) continue;
-      const uint16_t *const h_row = g.h_terms + ((int64_t)t * g.top + (j == kNotPicked ? 0 : j)) * g.h_ld;
+    for (int i = 0; i < N; ++i) {
       f32x4 d = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-      for (int q = 0; q < 4; ++q) {
-        const bf16x8 v = quarter_as_bf16(w, q);
+      for (int k = 0; k < H_TERMS; ++k)
 #pragma unroll
-        for (int k = 0; k < H_TERMS; ++k)
-          d = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v, term_quarter(h_row + k * g.h_term, c, q, j == kNotPicked ? 0 : g.I), d, 0, 0, 0);
-      }
-      // (a weight or scale of this expert that is not finite concerns the tokens that picked it alone)
+        for (int q = 0; q < 4; ++q) d = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v[q], __builtin_bit_cast(bf16x8, o.h[i].q[k][q]), d, 0, 0, 0);
 #pragma unroll
-      for (int n = 0; n < 4; ++n) acc[i][n] += j != kNotPicked ? sc * d[n] : 0.f;
+      for (int n = 0; n < 4; ++n) acc[i][n] += o.scale * d[n];
     }
+  };
+  auto load_others = [&](int b, Operands &o) {
+#pragma unroll
+    for (int i = 0; i < N; ++i) load_terms<H_TERMS>(h, h_at[i], b, o.h[i]);
+    o.scale = s_row[b + zero];
+  };
+  const int whole = I / kBlock;
+  pipeline<0, Operands>(min(b1, whole) - b0, [&](int s, Operands &o) {
+    load_block(w_row + (b0 + s) * kBlock, lane, o.w);
+    load_others(b0 + s, o);
+  }, multiply);
+  if (b0 < b1 && b1 > whole) {
+    const int c = whole * kBlock;
+    Operands o;
+    load_last_block(w_row + c, lane, I - c, o.w);
+    load_others(whole, o);
+    multiply(0, o);
   }
+}
+
+// 16 columns of Y (rows of W2) for all tokens.  The reduction runs over the blocks of all experts in use, ascending; a wave
+// takes a run of it, and adds an expert's sums to those of the tokens that picked it, in LDS of its own.
+template <class T, int MT, int H_TERMS, int WAVES>
+__global__ __launch_bounds__(WAVES * 64, 2) void moe_down_kernel(MoeArgs g, typename T::Elem *__restrict__ Y, int64_t ldy) {
+  __shared__ f32x4 part[WAVES][16 * MT][4];  // [token][four rows of W2]
+  const int tid = threadIdx.x, lane = tid & 63, r = lane & 15;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
 #pragma unroll
-  for (int i = 0; i < MT; ++i) part[wave][i][lane] = acc[i];
+  for (int i = 0; i < MT; ++i) part[wave][16 * i + r][lane >> 4] = f32x4{0.f, 0.f, 0.f, 0.f};
+  const int n0 = blockIdx.x * 16;
+  const uint8_t *const w_row = g.W2 + min(n0 + r, g.H - 1) * g.ldw2;
+  const float *const s_row = g.S2 + (int64_t)(n0 / kBlock) * g.lds2;
+  const Buffer h = __builtin_amdgcn_make_buffer_rsrc(g.h_terms, 0, g.T * g.top * g.h_row, 0x00020000);
+  const int blocks = (g.I + kBlock - 1) / kBlock, steps = *g.n_used * blocks;
+  const int s0 = (int)((int64_t)steps * wave / WAVES), s1 = (int)((int64_t)steps * (wave + 1) / WAVES);
+  for (int s = s0; s < s1;) {
+    const int u = s / blocks, b0 = s - u * blocks, b1 = min(blocks, b0 + s1 - s);
+    const Use use = g.uses[u];
+    const int token = g.use_tokens[u * kMostTokens + lane];
+    int h_at[MT];
+    f32x4 acc[MT];
+#pragma unroll
+    for (int i = 0; i < MT; ++i) {
+      h_at[i] = 16 * i + r < use.count ? (use.first + 16 * i + r) * g.h_row + (lane >> 4) * 16 : kNoColumn;
+      acc[i] = f32x4{0.f, 0.f, 0.f, 0.f};
+    }
+    const uint8_t *const w = w_row + use.expert * g.w2_stride;
+    const float *const sc = s_row + use.expert * g.s2_stride;
+    if (use.count <= 16)
+      down_blocks<1, MT, H_TERMS>(w, sc, h, h_at, g.I, lane, b0, b1, acc);
+    else if (MT == 2 || use.count <= 32)
+      down_blocks<(MT < 2 ? 1 : 2), MT, H_TERMS>(w, sc, h, h_at, g.I, lane, b0, b1, acc);
+    else
+      down_blocks<MT, MT, H_TERMS>(w, sc, h, h_at, g.I, lane, b0, b1, acc);
+#pragma unroll
+    for (int i = 0; i < MT; ++i) {
+      const int to = __shfl(token, (16 * i + r) & 63);
+      if (16 * i + r < use.count) part[wave][to][lane >> 4] += acc[i];
+    }
+    s += b1 - b0;
+  }
   __syncthreads();
-  for (int i = wave; i < MT; i += WAVES) {
-    f32x4 v = part[0][i][lane];
+  for (int i = tid; i < 16 * g.T; i += WAVES * 64) {
+    const int t = i / 16, n = i % 16;
+    float v = 0.f;
 #pragma unroll
-    for (int w = 1; w < WAVES; ++w) v += part[w][i][lane];
-    const int t = 16 * i + r, n = n0 + 4 * (lane >> 4);
-    if (t >= g.T) continue;
-#pragma unroll
-    for (int k = 0; k < 4; ++k)
-      if (n + k < g.H) T::store(Y + t * ldy + n + k, v[k]);
+    for (int w = 0; w < WAVES; ++w) v += reinterpret_cast<const float *>(part[w][t])[n];
+    if (n0 + n < g.H) T::store(Y + t * ldy + n0 + n, v);
   }
 }
 
@@ -363,39 +491,54 @@ __global__ __launch_bounds__(WAVES * 64) void moe_down_kernel(MoeArgs g, typenam
 constexpr int64_t round_up(int64_t n, int64_t d) { return (n + d - 1) / d * d; }
 
 struct MoePlan {
-  int64_t logits, x, h, total;  // bytes: where they start, and in all
-  int64_t x_ld, h_ld;
+  int64_t logits, n_used, uses, tokens, shares, x, h, total;  // bytes: where they start, and in all
+  int x_row, h_row;  // bytes
 };
 
 MoePlan plan_of(int T, int H, int I, int E, int top, int32_t dtype) {
   MoePlan p;
   const int terms = dtype == XORENC_X_F32 ? 3 : 1, h_terms = dtype == XORENC_X_F32 ? 3 : 2;
-  p.x_ld = round_up(H, 16);
-  p.h_ld = round_up(I, 16);
+  const int64_t most_used = E < T * top ? E : T * top;
+  p.x_row = (H + kBlock - 1) / kBlock * terms * (2 * kBlock);
+  p.h_row = (I + kBlock - 1) / kBlock * h_terms * (2 * kBlock);
   p.logits = 0;
-  p.x = round_up((int64_t)T * E * 4, 256);
-  p.h = p.x + round_up(terms * T * p.x_ld * 2, 256);
-  p.total = p.h + h_terms * T * top * p.h_ld * 2;
+  p.n_used = round_up((int64_t)T * E * 4, 16);
+  p.uses = p.n_used + 16;
+  p.tokens = p.uses + most_used * (int64_t)sizeof(Use);
+  p.shares = p.tokens + most_used * kMostTokens;
+  p.x = round_up(p.shares + (int64_t)T * top * 4, 256);
+  p.h = p.x + (int64_t)T * p.x_row;
+  p.total = p.h + (int64_t)T * top * p.h_row;
   return p;
+}
+
+template <int MT, int TERMS, int H_TERMS, int WAVES>
+void launch_up(const MoeArgs &g, dim3 grid, hipStream_t st) {
+  hipLaunchKernelGGL((moe_up_kernel<MT, TERMS, H_TERMS, WAVES>), grid, dim3(WAVES * 64), 0, st, g);
 }
 
 template <class T, int TERMS, int H_TERMS, int MT>
 void launch_products(const MoeArgs &g, void *Y, int64_t ldy, hipStream_t st) {
-  hipLaunchKernelGGL((moe_up_kernel<MT, TERMS, H_TERMS, 4>), dim3((unsigned)((g.I + 15) / 16), (unsigned)min(g.E, g.T * g.top)), dim3(256),
-                     0, st, g);
-  hipLaunchKernelGGL((moe_down_kernel<T, MT, H_TERMS, 8>), dim3((unsigned)((g.H + 15) / 16)), dim3(512), 0, st, g,
+  constexpr int DOWN_WAVES = 8;
+  const dim3 grid((unsigned)((g.I + kBlock - 1) / kBlock * (kBlock / 16)), (unsigned)min(g.E, g.T * g.top));
+  const int64_t tasks = (int64_t)grid.x * grid.y;
+  if (tasks >= 2048)
+    launch_up<MT, TERMS, H_TERMS, 4>(g, grid, st);
+  else
+    launch_up<MT, TERMS, H_TERMS, 8>(g, grid, st);
+  hipLaunchKernelGGL((moe_down_kernel<T, MT, H_TERMS, DOWN_WAVES>), dim3((unsigned)((g.H + 15) / 16)), dim3(DOWN_WAVES * 64), 0, st, g,
                      static_cast<typename T::Elem *>(Y), ldy);
 }
 
 template <class T, int TERMS, int H_TERMS>
-int32_t launch_moe(const MoeArgs &g, const void *X, int64_t ldx, bool wide, const void *router, int64_t ldr, bool r_wide, bool staged,
-                   float *logits, uint16_t *terms, void *Y, int64_t ldy, hipStream_t st) {
+int32_t launch_moe(const MoeArgs &g, const void *X, int64_t ldx, bool wide, const void *router, int64_t ldr, bool r_wide, void *Y, int64_t ldy, hipStream_t st) {
   typedef typename T::Elem E;
-  const int groups = (g.E * ((g.T + 3) / 4) + 3) / 4;
-  const int64_t pieces = staged ? g.T * (g.x_ld / 8) : 0;
+  const int groups = g.E * ((g.T + 3) / 4);
+  const int64_t pieces = (int64_t)g.T * ((g.H + kBlock - 1) / kBlock) * 16;
   hipLaunchKernelGGL((router_kernel<T, TERMS>), dim3((unsigned)(groups + (pieces + 255) / 256)), dim3(256), 0, st,
-                     static_cast<const E *>(X), ldx, (int)wide, static_cast<const E *>(router), ldr, (int)r_wide, g.T, g.H, g.E, logits,
-                     terms, g.x_ld, g.x_term, groups);
+                     static_cast<const E *>(X), ldx, (int)wide, static_cast<const E *>(router), ldr, (int)r_wide, g.T, g.H, g.E, g.logits,
+                     g.x_terms, groups);
+  if (g.T > 1) hipLaunchKernelGGL(picks_kernel, dim3(1), dim3(1024), 0, st, g);
   int32_t rc = xorenc_internal_check_launch();
   if (rc != XORENC_OK) return rc;
   if (g.T <= 16)
@@ -410,7 +553,7 @@ int32_t launch_moe(const MoeArgs &g, const void *X, int64_t ldx, bool wide, cons
 int32_t check_sizes(int32_t T, int32_t H, int32_t I, int32_t E, int32_t top, int32_t dtype) {
   if (T < 0 || H <= 0 || I <= 0 || E <= 0 || top <= 0 || top > E) return XORENC_EINVAL;
   if (!known_dtype(dtype)) return XORENC_EUNSUPPORTED;
-  if (T > kMostTokens || E > kMostExperts || top > kMostPicks || H > (1 << 24) || I > (1 << 23)) return XORENC_ELIMIT;
+  if (T > kMostTokens || E > kMostExperts || top > kMostPicks || H > (1 << 17) || I > (1 << 17)) return XORENC_ELIMIT;
   return XORENC_OK;
 }
 
@@ -449,25 +592,23 @@ extern "C" int32_t xorenc_moe_fp8(const xorenc_moe *L, const void *X, int32_t x_
     return XORENC_EALIGN;
   unsigned char *const ws = static_cast<unsigned char *>(workspace);
   const bool wide = wide_rows(X, ldx, x_dtype);
-  const bool staged = x_dtype == XORENC_X_F32 || !wide || H % 16;  // the products read x as bf16 in whole pieces
   MoeArgs g;
   g.W13 = L->W13, g.W2 = L->W2, g.S13 = L->S13, g.S2 = L->S2;
   g.ldw13 = L->ld_w13, g.w13_stride = L->w13_stride, g.lds13 = L->ld_s13, g.s13_stride = L->s13_stride;
   g.ldw2 = L->ld_w2, g.w2_stride = L->w2_stride, g.lds2 = L->ld_s2, g.s2_stride = L->s2_stride;
   g.T = tokens, g.H = H, g.I = I, g.E = E, g.top = picks, g.renormalise = renormalise != 0;
-  float *const logits = reinterpret_cast<float *>(ws + p.logits);
-  uint16_t *const terms = reinterpret_cast<uint16_t *>(ws + p.x);
-  g.logits = logits;
-  g.x_terms = staged ? terms : static_cast<const uint16_t *>(X);
-  g.x_ld = staged ? p.x_ld : ldx;
-  g.x_term = tokens * p.x_ld;
+  g.logits = reinterpret_cast<float *>(ws + p.logits);
+  g.uses = reinterpret_cast<Use *>(ws + p.uses);
+  g.n_used = reinterpret_cast<int *>(ws + p.n_used);
+  g.use_tokens = ws + p.tokens;
+  g.shares = reinterpret_cast<float *>(ws + p.shares);
+  g.x_terms = reinterpret_cast<uint16_t *>(ws + p.x);
   g.h_terms = reinterpret_cast<uint16_t *>(ws + p.h);
-  g.h_ld = p.h_ld;
-  g.h_term = (int64_t)tokens * picks * p.h_ld;
+  g.x_row = p.x_row, g.h_row = p.h_row;
   const bool r_wide = wide_rows(L->router, L->ld_router, x_dtype);
   hipStream_t st = static_cast<hipStream_t>(hip_stream);
   xorenc_internal_begin_call();
   return x_dtype == XORENC_X_F32
-             ? launch_moe<F32, 3, 3>(g, X, ldx, wide, L->router, L->ld_router, r_wide, staged, logits, terms, Y, ldy, st)
-             : launch_moe<BF16, 1, 2>(g, X, ldx, wide, L->router, L->ld_router, r_wide, staged, logits, terms, Y, ldy, st);
+             ? launch_moe<F32, 3, 3>(g, X, ldx, wide, L->router, L->ld_router, r_wide, Y, ldy, st)
+             : launch_moe<BF16, 1, 2>(g, X, ldx, wide, L->router, L->ld_router, r_wide, Y, ldy, st);
 }
