@@ -57,8 +57,9 @@ __device__ inline void store_tile(const MatmulArgs &g, const f32x4 (&acc)[TN][TM
   if (wide) {
     const int c = lane % CHUNKS, n = n_first + c * PER_CHUNK;
 #pragma unroll
-    for (int k = 0; k < 16 * TM * CHUNKS / 64; ++k) {
+    for (int k = 0; k < (16 * TM * CHUNKS + 63) / 64; ++k) {
       const int m = k * (64 / CHUNKS) + lane / CHUNKS;
+      if (m >= 16 * TM) break;
       const u32x4 v = *reinterpret_cast<const u32x4 *>(out + m * ROW + (c ^ (m & (CHUNKS - 1))) * 16);
       if (m_first + m >= g.M) continue;
       Out *const y = Y + (int64_t)(m_first + m) * g.ldy + n;
