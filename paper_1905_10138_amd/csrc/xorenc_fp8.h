@@ -121,39 +121,59 @@ __device__ inline uint32_t max_of_16_lanes(uint32_t v) {
 }
 
 // Operands of the matrix instructions for 128 columns of 16 rows.  Lane l holds 32 values of row l % 16: columns
-// 16 (l / 16) + 0..15 of the first 64 columns, then of the second 64, so that each 16-byte load of a wave covers 64 contiguous
-// bytes of every row.  Which of the instruction's k a column becomes does not matter as long as both operands agree.
-__device__ inline int piece_column(int lane, int piece) { return piece * 64 + (lane >> 4) * 16; }
+// 16 (l / 16) + 0..15 of the first 64 columns (piece 0), then of the second 64 (piece 1).  Which of the instruction's k a column
+// becomes does not matter as long as both operands agree.
 
-// One of a lane's two 16-byte pieces of row `row`, columns from `c` on; columns from K on are zero, whatever lies there.  A piece
-// that holds a valid column is inside the allocation: rows start on 16-byte boundaries.
-__device__ inline u32x4 load_e4m3_piece(const uint8_t *row, int c, int K) {
-  u32x4 v = {0u, 0u, 0u, 0u};
-  if (c < K) {
-    v = *reinterpret_cast<const u32x4 *>(row + c);
-    if (c + 16 > K) {
+// What a row's last 16-byte piece holds behind its last column, `left` bytes from its start (1 .. 15): zero.
+__device__ inline u32x4 first_bytes(u32x4 v, int left) {
 #pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        const int left = K - (c + 4 * i);
-        v[i] = left >= 4 ? v[i] : left <= 0 ? 0u : v[i] & ((1u << (8 * left)) - 1u);
-      }
-    }
+  for (int i = 0; i < 4; ++i) {
+    const int n = left - 4 * i;
+    v[i] = n >= 4 ? v[i] : n <= 0 ? 0u : v[i] & ((1u << (8 * n)) - 1u);
   }
   return v;
+}
+
+// Loads from memory to LDS: lane l's 16 (4) bytes at descriptor + off + more go to to + 16 l (4 l).  The compiler does not know
+// of them: who reads the LDS waits for them with s_waitcnt vmcnt, as many later ones left out as it knows of.
+constexpr uint32_t kRawBuffer = 0x00020000u;    // descriptor word 3: untyped data
+constexpr uint32_t kBeyond = 0x80000000u;       // an offset past every descriptor's extent: reads as zero, from nowhere
+constexpr int64_t kMostTileBytes = 0x7fffff00;  // extent of the descriptors
+__device__ inline u32x4 descriptor(const void *p) {
+  const uint64_t a = reinterpret_cast<uint64_t>(p);
+  return u32x4{(uint32_t)__builtin_amdgcn_readfirstlane((int)(uint32_t)a),
+               (uint32_t)__builtin_amdgcn_readfirstlane((int)((uint32_t)(a >> 32) & 0xffffu)), (uint32_t)kMostTileBytes, kRawBuffer};
+}
+__device__ inline void fetch_16(uint32_t to, uint32_t off, const u32x4 &desc, uint32_t more) {
+  asm volatile("s_mov_b32 m0, %0\n\tbuffer_load_dwordx4 %1, %2, %3 offen lds" ::"s"(__builtin_amdgcn_readfirstlane(to)), "v"(off),
+               "s"(desc), "s"(__builtin_amdgcn_readfirstlane(more))
+               : "memory");
+}
+__device__ inline void fetch_4(uint32_t to, uint32_t off, const u32x4 &desc, uint32_t more) {
+  asm volatile("s_mov_b32 m0, %0\n\tbuffer_load_dword %1, %2, %3 offen lds" ::"s"(__builtin_amdgcn_readfirstlane(to)), "v"(off),
+               "s"(desc), "s"(__builtin_amdgcn_readfirstlane(more))
+               : "memory");
+}
+__device__ inline uint32_t lds_address(const void *p) {
+  return __builtin_amdgcn_readfirstlane((uint32_t)(size_t)(__attribute__((address_space(3))) const uint8_t *)p);
+}
+
+// Rows of e4m3 in LDS: 128 bytes each, a row's 16-byte chunks at chunk ^ (row / 2 % 8), so that the 16 rows of an operand read
+// spread over all banks.  A load of eight rows: lane l takes row l / 8 of them, and this chunk of it.
+__device__ inline int e4m3_chunk(int lane, int row) { return (lane & 7) ^ ((row >> 1) & 7); }
+__device__ inline uint32_t e4m3_operand_offset(int lane) {  // of the first piece, in 16 rows; the second's is this ^ 64
+  return (uint32_t)((lane & 15) * 128 + (((lane >> 4) ^ (((lane & 15) >> 1) & 7)) * 16));
 }
 
 struct E4m3Operand {
   u32x4 piece[2];
 };
 
-// A lane's part of a whole block of a row, and of the last one, of which `left` columns are left.
-__device__ inline void load_block(const uint8_t *row, int lane, E4m3Operand &o) {
-#pragma unroll
-  for (int k = 0; k < 2; ++k) o.piece[k] = *reinterpret_cast<const u32x4 *>(row + piece_column(lane, k));
-}
-__device__ inline void load_last_block(const uint8_t *row, int lane, int left, E4m3Operand &o) {
-#pragma unroll
-  for (int k = 0; k < 2; ++k) o.piece[k] = load_e4m3_piece(row, piece_column(lane, k), left);
+__device__ inline E4m3Operand read_operand(const uint8_t *rows, uint32_t offset) {
+  E4m3Operand o;
+  o.piece[0] = *reinterpret_cast<const u32x4 *>(rows + offset);
+  o.piece[1] = *reinterpret_cast<const u32x4 *>(rows + (offset ^ 64u));
+  return o;
 }
 
 __device__ inline i32x8 as_operand(const E4m3Operand &o) {
@@ -184,34 +204,6 @@ __device__ inline f32x4 product_128(const E4m3Operand &a, const E4m3Operand &b) 
     d = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(as_operand(a), as_operand(b), d, 0, 0, 0, 0, 0, 0);
   }
   return d;
-}
-
-// multiply(step, operands) for step = 0 .. steps - 1, with load(step, operands) AHEAD steps before it.  The loads are
-// unconditional (past the end the last step's again): a load that may or may not have been issued would make the compiler
-// wait for all loads on their way, not for the oldest ones.  For the same reason `load` has no branches, and loads
-// no value through the scalar cache.
-template <int AHEAD, class Operands, class Load, class Multiply>
-__device__ inline void pipeline(int steps, Load load, Multiply multiply) {
-  if (steps <= 0) return;
-  Operands o[AHEAD + 1];
-#pragma unroll
-  for (int k = 0; k < AHEAD; ++k) load(min(k, steps - 1), o[k]);
-  for (int s = 0; s < steps; s += AHEAD + 1) {  // (one exit, for the same reason)
-#pragma unroll
-    for (int k = 0; k <= AHEAD; ++k) {
-      load(min(s + k + AHEAD, steps - 1), o[(k + AHEAD) % (AHEAD + 1)]);
-      __builtin_amdgcn_sched_barrier(0);
-      if (s + k < steps) multiply(s + k, o[k]);
-    }
-  }
-}
-
-// Zero, in a vector register as far as the compiler knows: an address that it is added to is loaded from through the vector
-// memory path, although it is the same for all lanes.
-__device__ inline int vector_zero() {
-  int z;
-  asm volatile("v_mov_b32 %0, 0" : "=v"(z));
-  return z;
 }
 
 // Host checks shared by the entry points.

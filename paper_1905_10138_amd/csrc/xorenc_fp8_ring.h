@@ -38,21 +38,17 @@ __global__ __launch_bounds__(WN *WM *KG * 64) void matmul_ring_kernel(MatmulArgs
   const int tid = threadIdx.x, lane = tid & 63, r = lane & 15;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int kg = wave / Shape::GROUP, in_group = wave % Shape::GROUP, wn = in_group % WN, wm = in_group / WN;
-  const uint32_t lds0 = __builtin_amdgcn_readfirstlane((uint32_t)(size_t)(__attribute__((address_space(3))) uint8_t *)ring_lds);
+  const uint32_t lds0 = lds_address(ring_lds);
 
   // ---- loads: this wave's part of its group's blocks
-  const uint64_t w_base = reinterpret_cast<uint64_t>(g.W + n0 * g.ldw), a_base = reinterpret_cast<uint64_t>(g.A + m0 * g.lda),
-                 s_base = reinterpret_cast<uint64_t>(g.SA + m0 * g.sa_row);
-  const u32x4 w_desc = {(uint32_t)w_base, (uint32_t)(w_base >> 32) & 0xffffu, (uint32_t)kMostTileBytes, kRawBuffer};
-  const u32x4 a_desc = {(uint32_t)a_base, (uint32_t)(a_base >> 32) & 0xffffu, (uint32_t)kMostTileBytes, kRawBuffer};
-  const u32x4 s_desc = {(uint32_t)s_base, (uint32_t)(s_base >> 32) & 0xffffu, (uint32_t)kMostTileBytes, kRawBuffer};
+  const u32x4 w_desc = descriptor(g.W + n0 * g.ldw), a_desc = descriptor(g.A + m0 * g.lda), s_desc = descriptor(g.SA + m0 * g.sa_row);
   const int lane_row = lane >> 3;
   auto row_of = [&](int i) {  // of W, then of A
     const int row = (in_group * PER + i) * 8;
     return row < BN ? row : row - BN;
   };
   auto of_w = [&](int i) { return (in_group * PER + i) * 8 < BN; };
-  auto chunk_of = [&](int i) { return ((lane & 7) ^ (((row_of(i) + lane_row) >> 1) & 7)) * 16; };
+  auto chunk_of = [&](int i) { return e4m3_chunk(lane, row_of(i) + lane_row) * 16; };
   uint32_t at[PER];
 #pragma unroll
   for (int i = 0; i < PER; ++i)
@@ -67,15 +63,9 @@ __global__ __launch_bounds__(WN *WM *KG * 64) void matmul_ring_kernel(MatmulArgs
     const int most = b >= g.blocks ? 0 : tail && b == g.blocks - 1 ? tail : kBlock;  // columns of the block
     const uint32_t col = (uint32_t)b * kBlock;
 #pragma unroll
-    for (int i = 0; i < PER; ++i) {
-      const uint32_t off = chunk_of(i) >= most ? kBeyond : at[i];
-      asm volatile("s_mov_b32 m0, %0\n\tbuffer_load_dwordx4 %1, %2, %3 offen lds" ::"s"(to + (in_group * PER + i) * 1024), "v"(off),
-                   "s"(of_w(i) ? w_desc : a_desc), "s"(most ? col : 0u)
-                   : "memory");
-    }
-    asm volatile("s_mov_b32 m0, %0\n\tbuffer_load_dword %1, %2, %3 offen lds" ::"s"(to + (BN + BM) * 128 + s_rows * 4),
-                 "v"(most ? s_at : kBeyond), "s"(s_desc), "s"(most ? (uint32_t)b * s_step : 0u)
-                 : "memory");
+    for (int i = 0; i < PER; ++i)
+      fetch_16(to + (in_group * PER + i) * 1024, chunk_of(i) >= most ? kBeyond : at[i], of_w(i) ? w_desc : a_desc, most ? col : 0u);
+    fetch_4(to + (BN + BM) * 128 + s_rows * 4, most ? s_at : kBeyond, s_desc, most ? (uint32_t)b * s_step : 0u);
   };
   const int w_row = (n0 + wn * (TN * 16)) / kBlock;
   const float *const sw_row = g.SW + (int64_t)(w_row * kBlock < g.N ? w_row : 0) * g.ldsw;
@@ -86,7 +76,7 @@ __global__ __launch_bounds__(WN *WM *KG * 64) void matmul_ring_kernel(MatmulArgs
   for (int i = 0; i < TN; ++i)
 #pragma unroll
     for (int j = 0; j < TM; ++j) acc[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
-  const uint32_t off = (uint32_t)(r * 128 + (((lane >> 4) ^ ((r >> 1) & 7)) * 16));
+  const uint32_t off = e4m3_operand_offset(lane);
   constexpr int LOADS = PER + 1;  // of a wave per stage
 #pragma unroll
   for (int s = 0; s < NS - 1; ++s) fetch(s);  // (stages past the last read as zero: every wave has as many loads on their way)
@@ -103,13 +93,7 @@ __global__ __launch_bounds__(WN *WM *KG * 64) void matmul_ring_kernel(MatmulArgs
       if (b == g.blocks - 1) {
         for (int row = in_group * 64 + lane; row < BN + BM; row += Shape::GROUP * 64) {
           uint8_t *const p = slot + row * 128 + (((tail >> 4) ^ (((row < BN ? row : row - BN) >> 1) & 7)) * 16);
-          u32x4 v = *reinterpret_cast<u32x4 *>(p);
-#pragma unroll
-          for (int i = 0; i < 4; ++i) {
-            const int left = (tail & 15) - 4 * i;
-            v[i] = left >= 4 ? v[i] : left <= 0 ? 0u : v[i] & ((1u << (8 * left)) - 1u);
-          }
-          *reinterpret_cast<u32x4 *>(p) = v;
+          *reinterpret_cast<u32x4 *>(p) = first_bytes(*reinterpret_cast<u32x4 *>(p), tail & 15);
         }
       }
       asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
@@ -120,14 +104,9 @@ __global__ __launch_bounds__(WN *WM *KG * 64) void matmul_ring_kernel(MatmulArgs
 #pragma unroll
     for (int j = 0; j < TM; ++j) sa[j] = reinterpret_cast<const float *>(slot + (BN + BM) * 128)[(wm * TM + j) * 16 + r];
 #pragma unroll
-    for (int j = 0; j < TM; ++j)
+    for (int j = 0; j < TM; ++j) a[j] = read_operand(slot + (BN + (wm * TM + j) * 16) * 128, off);
 #pragma unroll
-      for (int p = 0; p < 2; ++p)
-        a[j].piece[p] = *reinterpret_cast<const u32x4 *>(slot + BN * 128 + (wm * TM + j) * 2048 + (off ^ (64u * p)));
-#pragma unroll
-    for (int i = 0; i < TN; ++i)
-#pragma unroll
-      for (int p = 0; p < 2; ++p) w[i].piece[p] = *reinterpret_cast<const u32x4 *>(slot + (wn * TN + i) * 2048 + (off ^ (64u * p)));
+    for (int i = 0; i < TN; ++i) w[i] = read_operand(slot + (wn * TN + i) * 2048, off);
     if ((b & 63) == kg % 64 && b >= 64) sw_run = sw_row[min((b & ~63) + lane, g.blocks - 1)];
     const float sw = __int_as_float(__builtin_amdgcn_readlane(__float_as_int(sw_run), b & 63));
 #pragma unroll

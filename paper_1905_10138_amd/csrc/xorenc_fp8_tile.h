@@ -29,10 +29,6 @@ struct MatmulArgs {
   int M, N, K, blocks;
 };
 
-constexpr uint32_t kRawBuffer = 0x00020000u;   // descriptor word 3: untyped data
-constexpr uint32_t kBeyond = 0x80000000u;      // an offset past every descriptor's extent: reads as zero
-constexpr int64_t kMostTileBytes = 0x7fffff00; // extent of the rows of a tile
-
 // A wave's 16 TN x 16 TM results, from row n_first of W and m_first of A on.  A lane holds four neighbours of a row of Y in
 // each 16 x 16 tile.  They change places in LDS (`out`, the wave's own; 16-byte chunks of row m at chunk ^ m), so that a store
 // writes 16 bytes a lane and whole runs of 16 TN results (8192 x 16384 x 4096 bf16: 569 -> 539 us).
@@ -109,12 +105,10 @@ __global__ __launch_bounds__(WN *WM * 64, 2) void matmul_tile_kernel(MatmulArgs 
   const int tid = threadIdx.x, lane = tid & 63;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int wn = wave % WN, wm = wave / WN;
-  const uint32_t lds0 = __builtin_amdgcn_readfirstlane((uint32_t)(size_t)(__attribute__((address_space(3))) uint8_t *)tile_lds);
+  const uint32_t lds0 = lds_address(tile_lds);
 
   // ---- this wave's loads
-  const uint64_t w_base = reinterpret_cast<uint64_t>(g.W + n0 * g.ldw), a_base = reinterpret_cast<uint64_t>(g.A + m0 * g.lda);
-  const u32x4 w_desc = {(uint32_t)w_base, (uint32_t)(w_base >> 32) & 0xffffu, (uint32_t)kMostTileBytes, kRawBuffer};
-  const u32x4 a_desc = {(uint32_t)a_base, (uint32_t)(a_base >> 32) & 0xffffu, (uint32_t)kMostTileBytes, kRawBuffer};
+  const u32x4 w_desc = descriptor(g.W + n0 * g.ldw), a_desc = descriptor(g.A + m0 * g.lda), s_desc = descriptor(g.SA + m0 * g.sa_row);
   constexpr int HALF = TN * 8;  // rows of half of a wave's row tiles
   // first row of load i of group 1 (rows of A, then lower halves) and of group 2
   auto row1 = [&](int i) {
@@ -127,7 +121,7 @@ __global__ __launch_bounds__(WN *WM * 64, 2) void matmul_tile_kernel(MatmulArgs 
     return l / TN * (2 * HALF) + HALF + l % TN * 8;
   };
   const int lane_row = lane >> 3;
-  auto chunk_of = [&](int row) { return ((lane & 7) ^ (((row + lane_row) >> 1) & 7)) * 16; };  // this lane's column
+  auto chunk_of = [&](int row) { return e4m3_chunk(lane, row + lane_row) * 16; };  // this lane's column
   uint32_t at1[N1], at2[N2];
 #pragma unroll
   for (int i = 0; i < N1; ++i)
@@ -136,23 +130,14 @@ __global__ __launch_bounds__(WN *WM * 64, 2) void matmul_tile_kernel(MatmulArgs 
   for (int i = 0; i < N2; ++i) at2[i] = (uint32_t)(min(row2(i) + lane_row, g.N - n0 - 1) * g.ldw) + (uint32_t)chunk_of(row2(i));
   // ---- and of 64 rows' scales of A (the waves beyond BM / 64 fetch what others fetch: all wait for as many loads)
   const int s_rows = wave % (BM / 64) * 64;
-  const uint64_t s_base = reinterpret_cast<uint64_t>(g.SA + m0 * g.sa_row);
-  const u32x4 s_desc = {(uint32_t)s_base, (uint32_t)(s_base >> 32) & 0xffffu, (uint32_t)kMostTileBytes, kRawBuffer};
   const uint32_t s_at = (uint32_t)(min(s_rows + lane, g.M - m0 - 1) * g.sa_row) * 4u;
   const uint32_t s_step = (uint32_t)(g.sa_blk * 4);
   const int tail = g.K & (kBlock - 1);
-  auto fetch = [&](uint32_t to, uint32_t off, const u32x4 &desc, uint32_t col) {
-    asm volatile("s_mov_b32 m0, %0\n\tbuffer_load_dwordx4 %1, %2, %3 offen lds" ::"s"(lds0 + to), "v"(off), "s"(desc), "s"(col) : "memory");
-  };
   auto fetch1 = [&](int b, int i) {
-    fetch((b & 1) * STAGE + (of_a(i) ? BN * 128 : 0) + row1(i) * 128, at1[i], of_a(i) ? a_desc : w_desc, (uint32_t)b * kBlock);
+    fetch_16(lds0 + (b & 1) * STAGE + (of_a(i) ? BN * 128 : 0) + row1(i) * 128, at1[i], of_a(i) ? a_desc : w_desc, (uint32_t)b * kBlock);
   };
-  auto fetch2 = [&](int b, int i) { fetch((b & 1) * STAGE + row2(i) * 128, at2[i], w_desc, (uint32_t)b * kBlock); };
-  auto fetch_scales = [&](int b) {
-    asm volatile("s_mov_b32 m0, %0\n\tbuffer_load_dword %1, %2, %3 offen lds" ::"s"(lds0 + 2 * STAGE + (b & 1) * (BM * 4) + s_rows * 4),
-                 "v"(s_at), "s"(s_desc), "s"((uint32_t)b * s_step)
-                 : "memory");
-  };
+  auto fetch2 = [&](int b, int i) { fetch_16(lds0 + (b & 1) * STAGE + row2(i) * 128, at2[i], w_desc, (uint32_t)b * kBlock); };
+  auto fetch_scales = [&](int b) { fetch_4(lds0 + 2 * STAGE + (b & 1) * (BM * 4) + s_rows * 4, s_at, s_desc, (uint32_t)b * s_step); };
   // before the last block is fetched: chunks behind column K read as zero
   auto end1 = [&](int b) {
     if (tail == 0 || b != g.blocks - 1) return;
@@ -170,28 +155,16 @@ __global__ __launch_bounds__(WN *WM * 64, 2) void matmul_tile_kernel(MatmulArgs 
     for (int r = tid; r < BN + BM; r += WN * WM * 64) {
       const int in = r < BN ? r : r - BN;
       uint8_t *const p = tile_lds + (b & 1) * STAGE + r * 128 + (((tail >> 4) ^ ((in >> 1) & 7)) * 16);
-      u32x4 v = *reinterpret_cast<u32x4 *>(p);
-#pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        const int left = (tail & 15) - 4 * i;
-        v[i] = left >= 4 ? v[i] : left <= 0 ? 0u : v[i] & ((1u << (8 * left)) - 1u);
-      }
-      *reinterpret_cast<u32x4 *>(p) = v;
+      *reinterpret_cast<u32x4 *>(p) = first_bytes(*reinterpret_cast<u32x4 *>(p), tail & 15);
     }
     asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
   };
 
   // ---- operand reads
   const int r = lane & 15;
-  const uint32_t off = (uint32_t)(r * 128 + (((lane >> 4) ^ ((r >> 1) & 7)) * 16));
+  const uint32_t off = e4m3_operand_offset(lane);
   const uint8_t *const w_lds = tile_lds + wn * (TN * 2048), *const a_lds = tile_lds + BN * 128 + wm * (TM * 2048);
   const float *const s_lds = reinterpret_cast<const float *>(tile_lds + 2 * STAGE) + wm * (TM * 16) + r;
-  auto read_operand = [&](const uint8_t *tile_base, int t) {
-    E4m3Operand o;
-    o.piece[0] = *reinterpret_cast<const u32x4 *>(tile_base + t * 2048 + off);
-    o.piece[1] = *reinterpret_cast<const u32x4 *>(tile_base + t * 2048 + (off ^ 64u));
-    return o;
-  };
   // ---- scales of W: lane i holds those of block i of a run of 64
   const float *const sw_row = g.SW + (int64_t)((n0 + wn * (TN * 16)) / kBlock < (g.N + kBlock - 1) / kBlock ? (n0 + wn * (TN * 16)) / kBlock : 0) * g.ldsw;
   float sw_run = sw_row[min(lane, g.blocks - 1)];
@@ -231,11 +204,11 @@ __global__ __launch_bounds__(WN *WM * 64, 2) void matmul_tile_kernel(MatmulArgs 
   };
 #pragma unroll
   for (int j = 0; j < TM; ++j) {
-    a[j] = read_operand(a_lds, j);
+    a[j] = read_operand(a_lds + j * 2048, off);
     f[j] = 0.f;
     d[(TN - 1) & 1][j] = f32x4{0.f, 0.f, 0.f, 0.f};
   }
-  w[0] = read_operand(w_lds, 0);
+  w[0] = read_operand(w_lds, off);
   read_scales(0);
   // A row tile's sums are added while the matrix instructions of the next one run: four of them go with each.
   for (int b = 0; b < g.blocks; ++b) {
@@ -249,12 +222,12 @@ __global__ __launch_bounds__(WN *WM * 64, 2) void matmul_tile_kernel(MatmulArgs 
         if (fetches) end1(b + 2);
       }
       if (i < LAST) {
-        w[(i + 1) & 1] = read_operand(w_lds + here, i + 1);
+        w[(i + 1) & 1] = read_operand(w_lds + here + (i + 1) * 2048, off);
       } else if (more) {
         wait_for_loads(fetches);
         clear_tail(b + 1);
         if (fetches) end2(b + 2);
-        w[0] = read_operand(w_lds + there, 0);
+        w[0] = read_operand(w_lds + there, off);
         read_scales(b + 1);
       }
       __builtin_amdgcn_sched_barrier(0);
@@ -262,7 +235,7 @@ __global__ __launch_bounds__(WN *WM * 64, 2) void matmul_tile_kernel(MatmulArgs 
 #pragma unroll
       for (int j = 0; j < TM; ++j) {
         d[i & 1][j] = product_128<EXACT>(w[i & 1], a[j]);
-        if (i == LAST && more) a[j] = read_operand(a_lds + there, j);
+        if (i == LAST && more) a[j] = read_operand(a_lds + there + j * 2048, off);
         if (i == MIDDLE && fetches) {
           if (j == 0) fetch_scales(b + 2);
 #pragma unroll

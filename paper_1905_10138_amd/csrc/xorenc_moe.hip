@@ -3,27 +3,29 @@
 //
 // Four launches: the router's logits; the picks (not for a single token, whose picks every workgroup finds by itself); the gated
 // activations h of the picked experts; their second product and the sum over picks.  The bytes of the picked experts'
-// weights bound the last two, so both stream 16 rows of weights per workgroup from memory to registers, its waves taking
-// parts of the reduction.  e4m3 values become bf16 exactly and multiply bf16 terms of the activations (one for bf16
-// activations, three for fp32, which sum to the value exactly), so that nothing is rounded to 8 bits on the way; h is kept
-// as bf16 terms that hold 16 (24) bits.  The tokens that picked an expert are the columns of its matrix instructions, 16 at a
-// time; lanes of columns without a token load nothing.
+// weights bound the last two.  Weights go from memory to a ring of stages in LDS (eight lanes fetch 128 bytes of a row; loads to
+// registers, where a lane needs 32 bytes of one row of 16, take the address units twice as long: 250 us for 32 tokens and
+// eight experts of 4096 x 9216, %%% this way), and so do the activations that multiply them.  e4m3 values become bf16 exactly
+// and multiply bf16 terms of the activations (one for bf16 activations, three for fp32, which sum to the value exactly), so
+// that nothing is rounded to 8 bits on the way; h is kept as bf16 terms that hold 16 (24) bits.  The tokens that picked an
+// expert are the columns of its matrix instructions; rows of tokens that are not there are not loaded.
 //
-// Terms of x and h lie in the workspace in the order in which lanes load them: a row is a run of blocks of 128 columns (zero
-// behind the last column), a block its terms one after the other, a term four quarters of 32 columns: those that the
-// four lanes of a row take with one load, 64 contiguous bytes.
+// Terms of x and h lie in the workspace in the order in which they are used: a row is a run of blocks of 128 columns (zero
+// behind the last column), a block its terms one after the other, a term the columns 16 g + 64 p + 8 h + 0..7 at 64 p + 32 h + 8 g:
+// a quarter (p, h) of them is what the four lanes g of a row give to one matrix instruction.
 #include "xorenc_fp8.h"
 
 namespace xorenc_fp8_detail {
 namespace {
 
 constexpr int kMostExperts = XORENC_MOE_MAX_EXPERTS, kMostPicks = XORENC_MOE_MAX_PICKS, kMostTokens = XORENC_MOE_MAX_TOKENS;
-static_assert(kMostExperts == 256 && kMostTokens == 64, "four experts per lane, four column tiles");
+static_assert(kMostExperts == 256 && kMostTokens == 64, "four experts per lane, tokens as bits of 64");
 
-// An expert that some token picked: its tokens are `count` entries of the list of pairs of a token and an expert that it
-// picked, from `first` on.  Pairs are ordered by expert, then by token; row i of h is pair i's.
+// Tokens that picked an expert, `count` of them (at most as many as one pass multiplies: an expert that more tokens picked has
+// several uses): pairs of a token and an expert that it picked are ordered by expert, then by token, and these are
+// the pairs from `first` on.  Row i of h is pair i's.
 struct Use {
-  int expert, first, count, unused;
+  uint16_t expert, first, count, unused;
 };
 
 struct MoeArgs {
@@ -31,11 +33,15 @@ struct MoeArgs {
   const float *S13, *S2;
   int64_t ldw13, w13_stride, lds13, s13_stride, ldw2, w2_stride, lds2, s2_stride;
   int T, H, I, E, top, renormalise;
+  int most_uses, pass;      // most_uses of them, the last ones with count 0; tokens that a pass takes at most
   float *logits;            // [T][E]
-  Use *uses;                // experts in use, ascending; min(E, T * top) of them, the last ones with count 0
-  int *n_used;              // how many
-  uint8_t *use_tokens;      // [use][kMostTokens]
-  float *shares;            // of the entries
+  int *n_uses;              // how many
+  Use *uses;
+  uint8_t *pair_tokens;
+  float *shares;            // of the pairs
+  uint32_t *tickets;        // of the second product: workgroups that are done with 128 columns of Y, zero before it
+  float *parts;             // [splits][T][H rounded up to 128]: their sums
+  int splits, row_groups;
   uint16_t *x_terms, *h_terms;  // rows of tokens, and of pairs
   int x_row, h_row;             // bytes of a row
 };
@@ -52,14 +58,16 @@ __device__ inline float rest_of_bf16(float v) {
 // ---------------------------------------------------------------------------------------------- router
 
 // Logits in fp32: a workgroup per expert and four tokens, its waves share the columns.  The workgroups behind them write the
-// bf16 terms of x.
+// bf16 terms of x; the first one clears the tickets.
 template <class T, int TERMS>
 __global__ __launch_bounds__(256) void router_kernel(const typename T::Elem *__restrict__ X, int64_t ldx, int wide,
                                                      const typename T::Elem *__restrict__ router, int64_t ldr, int r_wide, int tokens,
                                                      int H, int E, float *__restrict__ logits, uint16_t *__restrict__ terms,
-                                                     int logit_groups) {
+                                                     int logit_groups, uint32_t *__restrict__ tickets, int n_tickets) {
   __shared__ float part[4][4];
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  if (blockIdx.x == 0)
+    for (int i = threadIdx.x; i < n_tickets; i += 256) tickets[i] = 0u;
   if ((int)blockIdx.x >= logit_groups) {  // eight columns a thread
     const int pieces = (H + kBlock - 1) / kBlock * 16;
     const int64_t i = (int64_t)(blockIdx.x - logit_groups) * 256 + threadIdx.x;
@@ -162,7 +170,7 @@ __global__ __launch_bounds__(1024) void picks_kernel(MoeArgs g) {
     uint64_t tokens[kMostExperts];  // that picked an expert, a bit each
     float share[kMostTokens][kMostPicks];
     uint16_t expert[kMostTokens][kMostPicks];
-    uint16_t place[kMostExperts], first[kMostExperts];  // of an expert among those in use; its first pair
+    uint16_t first[kMostExperts];  // pair of an expert
   } p;
   const int tid = threadIdx.x, lane = tid & 63;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -180,11 +188,11 @@ __global__ __launch_bounds__(1024) void picks_kernel(MoeArgs g) {
   }
   __syncthreads();
   if (wave == 0) {  // four experts a lane
-    int n[4], sum = 0;  // experts in use << 16 | pairs
+    int n[4], sum = 0;  // uses << 16 | pairs
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
       const int k = __popcll(p.tokens[4 * lane + i]);
-      n[i] = k ? k | 0x10000 : 0;
+      n[i] = (k + g.pass - 1) / g.pass << 16 | k;
       sum += n[i];
     }
     int before = sum;
@@ -193,296 +201,371 @@ __global__ __launch_bounds__(1024) void picks_kernel(MoeArgs g) {
       const int v = __shfl_up(before, o);
       if (lane >= o) before += v;
     }
-    const int used = __shfl(before, 63) >> 16;
+    const int uses = __shfl(before, 63) >> 16;
     before -= sum;
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-      if (n[i]) {
-        const int e = 4 * lane + i, at = before >> 16, first = before & 0xffff;
-        p.place[e] = (uint16_t)at;
-        p.first[e] = (uint16_t)first;
-        g.uses[at] = Use{e, first, n[i] & 0xffff, 0};
-      }
+      const int e = 4 * lane + i, first = before & 0xffff, count = n[i] & 0xffff;
+      p.first[e] = (uint16_t)first;
+      for (int k = 0; k * g.pass < count; ++k)
+        g.uses[(before >> 16) + k] = Use{(uint16_t)e, (uint16_t)(first + k * g.pass), (uint16_t)min(g.pass, count - k * g.pass), 0};
       before += n[i];
     }
-    if (lane == 0) *g.n_used = used;
-    for (int u = used + lane; u < min(g.E, g.T * g.top); u += 64) g.uses[u] = Use{0, 0, 0, 0};
+    if (lane == 0) *g.n_uses = uses;
+    for (int u = uses + lane; u < g.most_uses; u += 64) g.uses[u] = Use{0, 0, 0, 0};
   }
   __syncthreads();
   for (int i = tid; i < g.T * g.top; i += WAVES * 64) {
     const int t = i / g.top, j = i - t * g.top, e = p.expert[t][j];
-    const int rank = __popcll(p.tokens[e] & ((1ull << t) - 1ull));
-    g.use_tokens[p.place[e] * kMostTokens + rank] = (uint8_t)t;
-    g.shares[p.first[e] + rank] = p.share[t][j];
+    const int pair = p.first[e] + __popcll(p.tokens[e] & ((1ull << t) - 1ull));
+    g.pair_tokens[pair] = (uint8_t)t;
+    g.shares[pair] = p.share[t][j];
   }
 }
 
 // ---------------------------------------------------------------------------------------------- products
 
-typedef __amdgpu_buffer_rsrc_t Buffer;
-constexpr int kNoColumn = (int)0x80000000u;  // an offset behind every buffer: reads as zero, from nowhere
-
-// Terms of a lane's columns of a block, in quarters: the columns that quarter_as_bf16 gives of weights.
-template <int TERMS>
-struct TermOperand {
-  u32x4 q[TERMS][4];
-};
-template <int TERMS>
-__device__ inline void load_terms(Buffer rows, int at, int block, TermOperand<TERMS> &o) {
-#pragma unroll
-  for (int k = 0; k < TERMS; ++k)
-#pragma unroll
-    for (int q = 0; q < 4; ++q)
-      o.q[k][q] = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(rows, at + k * 256 + q * 64, block * (TERMS * 256), 0));
+// Rows of terms in LDS: 256 bytes each, a row's 16-byte chunks at chunk ^ row % 16.  A load of four rows: lane l takes row l / 16 of
+// them and this chunk of it.  Quarter q of a lane's columns is chunk 4 q + l / 16.
+__device__ inline int term_chunk(int lane, int row) { return (lane ^ row) & 15; }
+__device__ inline bf16x8 read_terms(const uint8_t *rows, int row, int lane, int q) {
+  return *reinterpret_cast<const bf16x8 *>(rows + row * 256 + (((4 * q + (lane >> 4)) ^ row) & 15) * 16);
 }
 
-// What a wave of the first product needs to know.
-struct UpRows {
-  const uint8_t *gate, *up;                // this lane's row of weights
-  const float *s_gate, *s_up0, *s_up1;     // scales of the gates' rows, of the ups' rows before `edge` and from it on
-  int edge;
-};
-
-template <int N, int TERMS>
-struct UpOperands {
-  E4m3Operand gate, up;
-  TermOperand<TERMS> x[N];
-  float sg, su0, su1;
-};
-
-// Blocks b0 .. b1 - 1 of the reduction for N tiles of 16 tokens.
-template <int N, int MT, int TERMS>
-__device__ inline void up_blocks(const UpRows &w, Buffer x, const int (&x_at)[MT], int H, int lane, int b0, int b1, f32x4 (&gate)[MT],
-                                 f32x4 (&up)[MT]) {
-  typedef UpOperands<N, TERMS> Operands;
-  const int zero = vector_zero();
-  auto multiply = [&](int, Operands &o) {
-    bf16x8 vg[4], vu[4];
+// Sums of the products of 16 rows of weights and 16 N rows of TERMS terms over a block; lane l has row l % 16 of the latter and rows 4 (l
+// / 16) .. + 3 of the former.  XR rows are there (four: lanes take them in turn, and only the first of a row's counts).
+template <int N, int XR, int TERMS>
+__device__ inline void block_products(const E4m3Operand &w, const uint8_t *x, int lane, f32x4 (&d)[N]) {
+  bf16x8 v[4];
 #pragma unroll
-    for (int q = 0; q < 4; ++q) vg[q] = quarter_as_bf16(o.gate, q), vu[q] = quarter_as_bf16(o.up, q);
+  for (int q = 0; q < 4; ++q) v[q] = quarter_as_bf16(w, q);
 #pragma unroll
-    for (int i = 0; i < N; ++i) {
-      f32x4 dg = {0.f, 0.f, 0.f, 0.f}, du = {0.f, 0.f, 0.f, 0.f};
+  for (int i = 0; i < N; ++i) {
+    const int row = XR < 16 ? lane & (XR - 1) : 16 * i + (lane & 15);
+    d[i] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-      for (int k = 0; k < TERMS; ++k)
+    for (int k = 0; k < TERMS; ++k)
 #pragma unroll
-        for (int q = 0; q < 4; ++q) {
-          const bf16x8 v = __builtin_bit_cast(bf16x8, o.x[i].q[k][q]);
-          dg = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vg[q], v, dg, 0, 0, 0);
-          du = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vu[q], v, du, 0, 0, 0);
-        }
-#pragma unroll
-      for (int j = 0; j < 4; ++j) {
-        gate[i][j] += o.sg * dg[j];
-        up[i][j] += (4 * (lane >> 4) + j < w.edge ? o.su0 : o.su1) * du[j];
-      }
-    }
-  };
-  auto load_others = [&](int b, Operands &o) {
-#pragma unroll
-    for (int i = 0; i < N; ++i) load_terms<TERMS>(x, x_at[i], b, o.x[i]);
-    o.sg = w.s_gate[b + zero], o.su0 = w.s_up0[b + zero], o.su1 = w.s_up1[b + zero];
-  };
-  const int whole = H / kBlock;
-  pipeline<0, Operands>(min(b1, whole) - b0, [&](int s, Operands &o) {
-    load_block(w.gate + (b0 + s) * kBlock, lane, o.gate);
-    load_block(w.up + (b0 + s) * kBlock, lane, o.up);
-    load_others(b0 + s, o);
-  }, multiply);
-  if (b0 < b1 && b1 > whole) {  // the last block, a short one
-    const int c = whole * kBlock;
-    Operands o;
-    load_last_block(w.gate + c, lane, H - c, o.gate);
-    load_last_block(w.up + c, lane, H - c, o.up);
-    load_others(whole, o);
-    multiply(0, o);
+      for (int q = 0; q < 4; ++q) d[i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v[q], read_terms(x + k * (XR * 256), row, lane, q), d[i], 0, 0, 0);
   }
 }
 
-// h of 16 rows of an expert for all tokens that picked it.
-template <int MT, int TERMS, int H_TERMS, int WAVES>
-__global__ __launch_bounds__(WAVES * 64, 2) void moe_up_kernel(MoeArgs g) {
-  __shared__ f32x4 part[WAVES][2][MT][64];
+// A workgroup takes 16 R rows of h of a use: R waves side by side, and S such groups that take the blocks of the reduction in turn.
+// XR: rows of x that a pass has room for.
+template <int XR, int TERMS, int R, int S, int NS>
+struct UpShape {
+  static constexpr int X_LOADS = XR * TERMS / 4, PER = (X_LOADS + R - 1) / R;  // 1 KB loads of x per block: of a group, of a wave
+  static constexpr int BLOCK = R * 4096 + X_LOADS * 1024 + R * 256;            // gates' and ups' rows, x, scales
+  static constexpr int STAGE = S * BLOCK, RING = NS * STAGE;
+  static constexpr int N = XR <= 16 ? 1 : XR / 16, SUMS = R * S * 2 * N * 1024;
+  static constexpr int LDS = RING > SUMS ? RING : SUMS, LOADS = 4 + PER + 1;
+};
+
+template <int XR, int TERMS, int H_TERMS, int R, int S, int NS>
+__global__ __launch_bounds__(R *S * 64) void moe_up_kernel(MoeArgs g) {
+  typedef UpShape<XR, TERMS, R, S, NS> Shape;
+  constexpr int N = Shape::N, PER = Shape::PER;
+  extern __shared__ __attribute__((aligned(1024))) uint8_t up_lds[];
   const int tid = threadIdx.x, lane = tid & 63, r = lane & 15;
-  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-  const int i0 = blockIdx.x * 16;
-  int e, first, count, token;
-  float one_share = 0.f;
-  if (MT == 1 && g.T == 1) {  // its picks are the experts in use, in their order
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6), kg = wave / R, rt = wave % R;
+  const uint32_t lds0 = lds_address(up_lds);
+  const int i0 = (blockIdx.x * R + rt) * 16;
+  int e, first, count, token = 0;  // token: lane l's is the l-th of the use
+  float share;                     // lane l: of the l-th token
+  if (XR == 4 && g.T == 1) {       // the picks are the uses, in their order
     int expert;
-    picks_of_token(g, 0, lane, expert, one_share);
-    first = blockIdx.y, count = 1, token = 0;
+    picks_of_token(g, 0, lane, expert, share);
+    first = blockIdx.y, count = 1;
     e = __builtin_amdgcn_readlane(expert, first);
-    one_share = __shfl(one_share, first);
+    share = __shfl(share, first);
     if (blockIdx.x == 0 && tid == 0) {
-      g.uses[first] = Use{e, first, 1, 0};
-      g.use_tokens[first * kMostTokens] = 0;
-      if (first == 0) *g.n_used = g.top;
+      g.uses[first] = Use{(uint16_t)e, (uint16_t)first, 1, 0};
+      g.pair_tokens[first] = 0;
+      if (first == 0) *g.n_uses = g.top;
     }
   } else {
     const Use use = g.uses[blockIdx.y];
-    token = g.use_tokens[blockIdx.y * kMostTokens + lane];
     e = use.expert, first = use.first, count = use.count;
     if (count == 0) return;
+    const int pair = first + min(lane, count - 1);
+    token = g.pair_tokens[pair];
+    share = g.shares[pair];
   }
-  const int tiles = (count + 15) / 16;
-  const int h_block = i0 / kBlock * (H_TERMS * kBlock) + term_place(i0 % kBlock + 4 * (lane >> 4));  // where this lane's four results go
-  uint16_t *const h = g.h_terms + (int64_t)first * (g.h_row / 2) + h_block;
-  if (i0 >= g.I) {  // columns that fill up the last block
-    for (int col = 16 * wave + r; col < count; col += 16 * WAVES)
+  // ---- this wave's loads: 16 gates, 16 ups, its part of x, scales
+  const int blocks = (g.H + kBlock - 1) / kBlock, steps = (blocks + S - 1) / S, tail = g.H & (kBlock - 1);
+  const int i_row = min(i0, g.I - 1), last_row = g.I - 1 - i_row;
+  const uint8_t *const gates = g.W13 + e * g.w13_stride + i_row * g.ldw13;
+  const u32x4 gate_desc = descriptor(gates), up_desc = descriptor(gates + g.I * g.ldw13), x_desc = descriptor(g.x_terms),
+              s_desc = descriptor(g.S13 + e * g.s13_stride);
+  uint32_t w_at[2], x_at[PER];
+  int chunk[2];
 #pragma unroll
-      for (int k = 0; k < H_TERMS; ++k) *reinterpret_cast<u32x2 *>(h + (int64_t)col * (g.h_row / 2) + k * kBlock) = u32x2{0u, 0u};
-    return;
+  for (int p = 0; p < 2; ++p) {
+    const int row = 8 * p + (lane >> 3);
+    chunk[p] = e4m3_chunk(lane, row) * 16;
+    w_at[p] = (uint32_t)(min(row, last_row) * g.ldw13) + chunk[p];
   }
-  const uint8_t *const base = g.W13 + e * g.w13_stride;
-  const float *const s_base = g.S13 + e * g.s13_stride;
-  const int row = min(i0 + r, g.I - 1);
+  auto x_load = [&](int j) { return min(rt * PER + j, Shape::X_LOADS - 1); };  // (the last one again, where there are none left)
+#pragma unroll
+  for (int j = 0; j < PER; ++j) {
+    const int row = x_load(j) / TERMS * 4 + (lane >> 4), t = __shfl(token, row & 63);
+    x_at[j] = row < count ? (uint32_t)(t * g.x_row + x_load(j) % TERMS * 256 + term_chunk(lane, row) * 16) : kBeyond;
+  }
   // the up rows of a tile lie in two blocks of scales where I is not a multiple of 16
-  const int up_first = g.I + i0, up_last = g.I + min(i0 + 15, g.I - 1);
-  const UpRows w = {base + row * g.ldw13, base + ((int64_t)g.I + row) * g.ldw13, s_base + (int64_t)(i0 / kBlock) * g.lds13,
-                    s_base + (int64_t)(up_first / kBlock) * g.lds13, s_base + (int64_t)(up_last / kBlock) * g.lds13,
-                    (up_last / kBlock) * kBlock - up_first};
-  const Buffer x = __builtin_amdgcn_make_buffer_rsrc(g.x_terms, 0, g.T * g.x_row, 0x00020000);
-  int x_at[MT];
+  const int up_first = g.I + i_row, up_last = g.I + min(i_row + 15, g.I - 1), edge = up_last / kBlock * kBlock - up_first;
+  const int s_line = (lane & 3) == 0 ? i_row / kBlock : (lane & 3) == 1 ? up_first / kBlock : up_last / kBlock;
+  const uint32_t s_at = (uint32_t)(s_line * g.lds13) * 4u;
+  auto fetch = [&](int s) {
+    const int b = s * S + kg;
+    const uint32_t to = lds0 + (uint32_t)(s % NS) * Shape::STAGE + kg * Shape::BLOCK;
+    const int most = b >= blocks ? 0 : tail && b == blocks - 1 ? tail : kBlock;  // columns of the block
+    const uint32_t at = most ? (uint32_t)b : 0u;
 #pragma unroll
-  for (int i = 0; i < MT; ++i) {
-    const int t = __shfl(token, (16 * i + r) & 63);
-    x_at[i] = 16 * i + r < count ? t * g.x_row + (lane >> 4) * 16 : kNoColumn;
-  }
-  f32x4 gate[MT], up[MT];
-#pragma unroll
-  for (int i = 0; i < MT; ++i) gate[i] = up[i] = f32x4{0.f, 0.f, 0.f, 0.f};
-  const int blocks = (g.H + kBlock - 1) / kBlock, b0 = blocks * wave / WAVES, b1 = blocks * (wave + 1) / WAVES;
-  if (tiles == 1)
-    up_blocks<1, MT, TERMS>(w, x, x_at, g.H, lane, b0, b1, gate, up);
-  else if (MT == 2 || tiles == 2)
-    up_blocks<(MT < 2 ? 1 : 2), MT, TERMS>(w, x, x_at, g.H, lane, b0, b1, gate, up);
-  else
-    up_blocks<MT, MT, TERMS>(w, x, x_at, g.H, lane, b0, b1, gate, up);
-#pragma unroll
-  for (int i = 0; i < MT; ++i) {
-    part[wave][0][i][lane] = gate[i];
-    part[wave][1][i][lane] = up[i];
-  }
-  __syncthreads();
-  for (int i = wave; i < tiles; i += WAVES) {
-    f32x4 a = part[0][0][i][lane], c = part[0][1][i][lane];
-#pragma unroll
-    for (int k = 1; k < WAVES; ++k) {
-      a += part[k][0][i][lane];
-      c += part[k][1][i][lane];
+    for (int p = 0; p < 2; ++p) {
+      const uint32_t off = chunk[p] >= most ? kBeyond : w_at[p];
+      fetch_16(to + rt * 4096 + p * 1024, off, gate_desc, at * kBlock);
+      fetch_16(to + rt * 4096 + 2048 + p * 1024, off, up_desc, at * kBlock);
     }
+#pragma unroll
+    for (int j = 0; j < PER; ++j)
+      fetch_16(to + R * 4096 + (x_load(j) % TERMS * XR + x_load(j) / TERMS * 4) * 256, most ? x_at[j] : kBeyond, x_desc, at * (TERMS * 256));
+    fetch_4(to + R * 4096 + Shape::X_LOADS * 1024 + rt * 256, most ? s_at : kBeyond, s_desc, at * 4);
+  };
+  f32x4 gate[N], up[N];
+#pragma unroll
+  for (int i = 0; i < N; ++i) gate[i] = up[i] = f32x4{0.f, 0.f, 0.f, 0.f};
+  const uint32_t off = e4m3_operand_offset(lane);
+#pragma unroll
+  for (int s = 0; s < NS - 1; ++s) fetch(s);
+  for (int s = 0; s < steps; ++s) {
+    // this stage has landed, and every wave that shares x has read the one before, whose slot is filled next
+    if constexpr (R > 1)
+      asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"((NS - 2) * Shape::LOADS) : "memory");
+    else
+      asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" ::"n"((NS - 2) * Shape::LOADS) : "memory");
+    fetch(s + NS - 1);
+    const int b = s * S + kg;
+    if (b >= blocks) continue;  // (uniform in a group; the last step)
+    uint8_t *const slot = up_lds + (uint32_t)(s % NS) * Shape::STAGE + kg * Shape::BLOCK;
+    uint8_t *const w = slot + rt * 4096;
+    if ((tail & 15) && b == blocks - 1) {  // what the last chunk of a row holds behind column H
+      if (lane < 32) {
+        u32x4 *const p = reinterpret_cast<u32x4 *>(w + lane * 128 + ((tail >> 4) ^ ((r >> 1) & 7)) * 16);
+        *p = first_bytes(*p, tail & 15);
+      }
+      asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+    }
+    const float *const sc = reinterpret_cast<const float *>(slot + R * 4096 + Shape::X_LOADS * 1024 + rt * 256);
+    const float sg = sc[0], su0 = sc[1], su1 = sc[2];
+    const uint8_t *const x = slot + R * 4096;
+    const E4m3Operand wg = read_operand(w, off), wu = read_operand(w + 2048, off);
+    f32x4 dg[N], du[N];
+    if (N == 1 || count > 16) {
+      block_products<N, XR, TERMS>(wg, x, lane, dg);
+      block_products<N, XR, TERMS>(wu, x, lane, du);
+    } else {
+      f32x4 one[1];
+      block_products<1, XR, TERMS>(wg, x, lane, one), dg[0] = one[0];
+      block_products<1, XR, TERMS>(wu, x, lane, one), du[0] = one[0];
+#pragma unroll
+      for (int i = 1; i < N; ++i) dg[i] = du[i] = f32x4{0.f, 0.f, 0.f, 0.f};
+    }
+#pragma unroll
+    for (int i = 0; i < N; ++i)
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        gate[i][j] += sg * dg[i][j];
+        up[i][j] += (4 * (lane >> 4) + j < edge ? su0 : su1) * du[i][j];
+      }
+  }
+  // ---- the groups' sums meet in LDS, in the order of the groups
+  if constexpr (S > 1) {
+    asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");  // (no load may land in what follows)
+    f32x4 *const sums = reinterpret_cast<f32x4 *>(up_lds);
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+      sums[(wave * 2 * N + 2 * i) * 64 + lane] = gate[i];
+      sums[(wave * 2 * N + 2 * i + 1) * 64 + lane] = up[i];
+    }
+    __syncthreads();
+    if (kg > 0) return;
+#pragma unroll
+    for (int k = 1; k < S; ++k)
+#pragma unroll
+      for (int i = 0; i < N; ++i) {
+        gate[i] += sums[((k * R + rt) * 2 * N + 2 * i) * 64 + lane];
+        up[i] += sums[((k * R + rt) * 2 * N + 2 * i + 1) * 64 + lane];
+      }
+  } else {
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");  // (nor behind the end)
+  }
+  if (i0 >= (g.I + kBlock - 1) / kBlock * kBlock) return;
+  const int at = i0 + 4 * (lane >> 4);  // this lane's four columns of h; columns from I on fill up the last block
+#pragma unroll
+  for (int i = 0; i < N; ++i) {
     const int col = 16 * i + r;
+    const float f = __shfl(share, col & 63);
     if (col >= count) continue;
-    const float share = MT == 1 && g.T == 1 ? one_share : g.shares[first + col];
-    const int at = i0 + 4 * (lane >> 4);
     float v[4];
 #pragma unroll
-    for (int k = 0; k < 4; ++k) v[k] = at + k < g.I ? silu(a[k]) * c[k] * share : 0.f;
+    for (int k = 0; k < 4; ++k) v[k] = at + k < g.I ? silu(gate[i][k]) * up[i][k] * f : 0.f;
+    uint16_t *const h = g.h_terms + (int64_t)(first + col) * (g.h_row / 2) + at / kBlock * (H_TERMS * kBlock) + term_place(at % kBlock);
 #pragma unroll
     for (int k = 0; k < H_TERMS; ++k) {
-      *reinterpret_cast<u32x2 *>(h + (int64_t)col * (g.h_row / 2) + k * kBlock) = u32x2{to_bf16x2(v[0], v[1]), to_bf16x2(v[2], v[3])};
+      *reinterpret_cast<u32x2 *>(h + k * kBlock) = u32x2{to_bf16x2(v[0], v[1]), to_bf16x2(v[2], v[3])};
 #pragma unroll
       for (int n = 0; n < 4; ++n) v[n] = rest_of_bf16(v[n]);
     }
   }
 }
 
-template <int N, int H_TERMS>
-struct DownOperands {
-  E4m3Operand w;
-  TermOperand<H_TERMS> h[N];
-  float scale;
+// A workgroup takes 128 columns of Y (rows of W2) for all tokens, eight waves side by side, and one of `splits` parts of the
+// reduction, which runs over the blocks of all uses.  When it leaves a use, its sums go to those of the use's tokens, in LDS.
+constexpr int kDownWaves = 8;
+template <int XR, int H_TERMS, int NS>
+struct DownShape {
+  static constexpr int X_LOADS = XR * H_TERMS / 4, PER = (X_LOADS + kDownWaves - 1) / kDownWaves;
+  static constexpr int STAGE = kDownWaves * 2048 + X_LOADS * 1024 + kDownWaves * 256, RING = NS * STAGE;
+  static constexpr int N = XR <= 16 ? 1 : XR / 16, LOADS = 2 + PER + 1;
 };
 
-// Blocks b0 .. b1 - 1 of an expert's reduction for N tiles of 16 tokens, from the lane's rows of weights and of h.
-template <int N, int MT, int H_TERMS>
-__device__ inline void down_blocks(const uint8_t *w_row, const float *s_row, Buffer h, const int (&h_at)[MT], int I, int lane, int b0, int b1,
-                                   f32x4 (&acc)[MT]) {
-  typedef DownOperands<N, H_TERMS> Operands;
-  const int zero = vector_zero();
-  auto multiply = [&](int, Operands &o) {
-    bf16x8 v[4];
-#pragma unroll
-    for (int q = 0; q < 4; ++q) v[q] = quarter_as_bf16(o.w, q);
-#pragma unroll
-    for (int i = 0; i < N; ++i) {
-      f32x4 d = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-      for (int k = 0; k < H_TERMS; ++k)
-#pragma unroll
-        for (int q = 0; q < 4; ++q) d = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v[q], __builtin_bit_cast(bf16x8, o.h[i].q[k][q]), d, 0, 0, 0);
-#pragma unroll
-      for (int n = 0; n < 4; ++n) acc[i][n] += o.scale * d[n];
-    }
-  };
-  auto load_others = [&](int b, Operands &o) {
-#pragma unroll
-    for (int i = 0; i < N; ++i) load_terms<H_TERMS>(h, h_at[i], b, o.h[i]);
-    o.scale = s_row[b + zero];
-  };
-  const int whole = I / kBlock;
-  pipeline<0, Operands>(min(b1, whole) - b0, [&](int s, Operands &o) {
-    load_block(w_row + (b0 + s) * kBlock, lane, o.w);
-    load_others(b0 + s, o);
-  }, multiply);
-  if (b0 < b1 && b1 > whole) {
-    const int c = whole * kBlock;
-    Operands o;
-    load_last_block(w_row + c, lane, I - c, o.w);
-    load_others(whole, o);
-    multiply(0, o);
-  }
-}
-
-// 16 columns of Y (rows of W2) for all tokens.  The reduction runs over the blocks of all experts in use, ascending; a wave
-// takes a run of it, and adds an expert's sums to those of the tokens that picked it, in LDS of its own.
-template <class T, int MT, int H_TERMS, int WAVES>
-__global__ __launch_bounds__(WAVES * 64, 2) void moe_down_kernel(MoeArgs g, typename T::Elem *__restrict__ Y, int64_t ldy) {
-  __shared__ f32x4 part[WAVES][16 * MT][4];  // [token][four rows of W2]
+template <class T, int XR, int H_TERMS, int NS>
+__global__ __launch_bounds__(kDownWaves * 64) void moe_down_kernel(MoeArgs g, typename T::Elem *__restrict__ Y, int64_t ldy) {
+  typedef DownShape<XR, H_TERMS, NS> Shape;
+  constexpr int N = Shape::N, PER = Shape::PER;
+  extern __shared__ __attribute__((aligned(1024))) uint8_t down_lds[];
+  __shared__ Use uses[XORENC_MOE_MAX_EXPERTS + kMostTokens * kMostPicks / 16];
+  __shared__ uint8_t pair_tokens[kMostTokens * kMostPicks];
+  __shared__ uint32_t ticket;
+  float *const sums = reinterpret_cast<float *>(down_lds + Shape::RING);  // [token][128 rows]
   const int tid = threadIdx.x, lane = tid & 63, r = lane & 15;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-#pragma unroll
-  for (int i = 0; i < MT; ++i) part[wave][16 * i + r][lane >> 4] = f32x4{0.f, 0.f, 0.f, 0.f};
-  const int n0 = blockIdx.x * 16;
-  const uint8_t *const w_row = g.W2 + min(n0 + r, g.H - 1) * g.ldw2;
-  const float *const s_row = g.S2 + (int64_t)(n0 / kBlock) * g.lds2;
-  const Buffer h = __builtin_amdgcn_make_buffer_rsrc(g.h_terms, 0, g.T * g.top * g.h_row, 0x00020000);
-  const int blocks = (g.I + kBlock - 1) / kBlock, steps = *g.n_used * blocks;
-  const int s0 = (int)((int64_t)steps * wave / WAVES), s1 = (int)((int64_t)steps * (wave + 1) / WAVES);
-  for (int s = s0; s < s1;) {
-    const int u = s / blocks, b0 = s - u * blocks, b1 = min(blocks, b0 + s1 - s);
-    const Use use = g.uses[u];
-    const int token = g.use_tokens[u * kMostTokens + lane];
-    int h_at[MT];
-    f32x4 acc[MT];
-#pragma unroll
-    for (int i = 0; i < MT; ++i) {
-      h_at[i] = 16 * i + r < use.count ? (use.first + 16 * i + r) * g.h_row + (lane >> 4) * 16 : kNoColumn;
-      acc[i] = f32x4{0.f, 0.f, 0.f, 0.f};
-    }
-    const uint8_t *const w = w_row + use.expert * g.w2_stride;
-    const float *const sc = s_row + use.expert * g.s2_stride;
-    if (use.count <= 16)
-      down_blocks<1, MT, H_TERMS>(w, sc, h, h_at, g.I, lane, b0, b1, acc);
-    else if (MT == 2 || use.count <= 32)
-      down_blocks<(MT < 2 ? 1 : 2), MT, H_TERMS>(w, sc, h, h_at, g.I, lane, b0, b1, acc);
-    else
-      down_blocks<MT, MT, H_TERMS>(w, sc, h, h_at, g.I, lane, b0, b1, acc);
-#pragma unroll
-    for (int i = 0; i < MT; ++i) {
-      const int to = __shfl(token, (16 * i + r) & 63);
-      if (16 * i + r < use.count) part[wave][to][lane >> 4] += acc[i];
-    }
-    s += b1 - b0;
-  }
+  const uint32_t lds0 = lds_address(down_lds);
+  const int n_uses = *g.n_uses, n0 = blockIdx.x * 128;
+  for (int i = tid; i < n_uses; i += kDownWaves * 64) uses[i] = g.uses[i];
+  for (int i = tid; i < g.T * g.top; i += kDownWaves * 64) pair_tokens[i] = g.pair_tokens[i];
+  for (int i = tid; i < g.T * 128; i += kDownWaves * 64) sums[i] = 0.f;
+  const int blocks = (g.I + kBlock - 1) / kBlock, steps = n_uses * blocks, tail = g.I & (kBlock - 1);
+  const int s0 = (int)((int64_t)steps * blockIdx.y / g.splits), s1 = (int)((int64_t)steps * (blockIdx.y + 1) / g.splits);
   __syncthreads();
-  for (int i = tid; i < 16 * g.T; i += WAVES * 64) {
-    const int t = i / 16, n = i % 16;
-    float v = 0.f;
+  // ---- this wave's loads: 16 rows of W2, its part of h, scales
+  const int row0 = min(n0 + wave * 16, g.H - 1), last_row = g.H - 1 - row0;
+  const u32x4 h_desc = descriptor(g.h_terms);
+  uint32_t w_at[2];
+  int chunk[2];
 #pragma unroll
-    for (int w = 0; w < WAVES; ++w) v += reinterpret_cast<const float *>(part[w][t])[n];
-    if (n0 + n < g.H) T::store(Y + t * ldy + n0 + n, v);
+  for (int p = 0; p < 2; ++p) {
+    const int row = 8 * p + (lane >> 3);
+    chunk[p] = e4m3_chunk(lane, row) * 16;
+    w_at[p] = (uint32_t)(min(row, last_row) * g.ldw2) + chunk[p];
+  }
+  auto x_load = [&](int j) { return min(wave * PER + j, Shape::X_LOADS - 1); };
+  // the use and block of the step to be fetched next
+  int fu = s0 / blocks, fb = s0 - fu * blocks;
+  u32x4 w_desc = h_desc, s_desc = h_desc;
+  uint32_t x_at[PER];
+  auto enter = [&]() {
+    const int e = __builtin_amdgcn_readfirstlane(uses[fu].expert), first = __builtin_amdgcn_readfirstlane(uses[fu].first),
+              count = __builtin_amdgcn_readfirstlane(uses[fu].count);
+    w_desc = descriptor(g.W2 + e * g.w2_stride + row0 * g.ldw2);
+    s_desc = descriptor(g.S2 + e * g.s2_stride + (int64_t)(row0 / kBlock) * g.lds2);
+#pragma unroll
+    for (int j = 0; j < PER; ++j) {
+      const int row = x_load(j) / H_TERMS * 4 + (lane >> 4);
+      x_at[j] = row < count ? (uint32_t)((first + row) * g.h_row + x_load(j) % H_TERMS * 256 + term_chunk(lane, row) * 16) : kBeyond;
+    }
+  };
+  auto fetch = [&](int s) {  // (steps past the last read as zero: every wave has as many loads on their way)
+    const uint32_t to = lds0 + (uint32_t)((s - s0) % NS) * Shape::STAGE;
+    const int most = s >= s1 ? 0 : tail && fb == blocks - 1 ? tail : kBlock;
+    const uint32_t at = most ? (uint32_t)fb : 0u;
+#pragma unroll
+    for (int p = 0; p < 2; ++p) fetch_16(to + wave * 2048 + p * 1024, chunk[p] >= most ? kBeyond : w_at[p], w_desc, at * kBlock);
+#pragma unroll
+    for (int j = 0; j < PER; ++j)
+      fetch_16(to + kDownWaves * 2048 + (x_load(j) % H_TERMS * XR + x_load(j) / H_TERMS * 4) * 256, most ? x_at[j] : kBeyond, h_desc,
+               at * (H_TERMS * 256));
+    fetch_4(to + kDownWaves * 2048 + Shape::X_LOADS * 1024 + wave * 256, most ? 0u : kBeyond, s_desc, at * 4);
+    if (most && ++fb == blocks) {
+      fb = 0;
+      if (++fu < n_uses) enter();
+    }
+  };
+  f32x4 acc[N];
+#pragma unroll
+  for (int i = 0; i < N; ++i) acc[i] = f32x4{0.f, 0.f, 0.f, 0.f};
+  const uint32_t off = e4m3_operand_offset(lane);
+  int u = fu, b = fb;
+  if (s0 < s1) enter();
+#pragma unroll
+  for (int k = 0; k < NS - 1; ++k) fetch(s0 + k);
+  for (int s = s0; s < s1; ++s) {
+    asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"((NS - 2) * Shape::LOADS) : "memory");
+    fetch(s + NS - 1);
+    uint8_t *const slot = down_lds + (uint32_t)((s - s0) % NS) * Shape::STAGE, *const w = slot + wave * 2048;
+    if ((tail & 15) && b == blocks - 1) {
+      if (lane < 16) {
+        u32x4 *const p = reinterpret_cast<u32x4 *>(w + lane * 128 + ((tail >> 4) ^ ((r >> 1) & 7)) * 16);
+        *p = first_bytes(*p, tail & 15);
+      }
+      asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+    }
+    const int first = __builtin_amdgcn_readfirstlane(uses[u].first), count = __builtin_amdgcn_readfirstlane(uses[u].count);
+    const float sc = *reinterpret_cast<const float *>(slot + kDownWaves * 2048 + Shape::X_LOADS * 1024 + wave * 256);
+    const E4m3Operand v = read_operand(w, off);
+    f32x4 d[N];
+    if (N == 1 || count > 16) {
+      block_products<N, XR, H_TERMS>(v, slot + kDownWaves * 2048, lane, d);
+    } else {
+      f32x4 one[1];
+      block_products<1, XR, H_TERMS>(v, slot + kDownWaves * 2048, lane, one), d[0] = one[0];
+#pragma unroll
+      for (int i = 1; i < N; ++i) d[i] = f32x4{0.f, 0.f, 0.f, 0.f};
+    }
+#pragma unroll
+    for (int i = 0; i < N; ++i)
+#pragma unroll
+      for (int j = 0; j < 4; ++j) acc[i][j] += sc * d[i][j];
+    if (++b == blocks || s + 1 == s1) {  // the use's sums to its tokens (a token is once in a use, a row of Y in one wave)
+#pragma unroll
+      for (int i = 0; i < N; ++i) {
+        const int col = 16 * i + r;
+        if (col < count) *reinterpret_cast<f32x4 *>(sums + pair_tokens[first + col] * 128 + wave * 16 + 4 * (lane >> 4)) += acc[i];
+        acc[i] = f32x4{0.f, 0.f, 0.f, 0.f};
+      }
+      b = 0;
+      ++u;
+    }
+  }
+  asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
+  const int n = n0 + (tid & 127);
+  if (g.splits == 1) {
+    for (int t = tid >> 7; t < g.T; t += kDownWaves / 2)
+      if (n < g.H) T::store(Y + t * ldy + n, sums[t * 128 + (tid & 127)]);
+    return;
+  }
+  // ---- the parts' sums, past the L2 (workgroups of other XCDs read them); who comes last adds them, in the order of the parts
+  const int64_t row = (int64_t)g.row_groups * 128, part = g.T * row;
+  for (int t = tid >> 7; t < g.T; t += kDownWaves / 2)
+    __hip_atomic_store(g.parts + blockIdx.y * part + t * row + n, sums[t * 128 + (tid & 127)], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+  asm volatile("s_waitcnt vmcnt(0)" ::: "memory");  // (once they are acknowledged the ticket may be taken)
+  __syncthreads();
+  if (tid == 0) ticket = __hip_atomic_fetch_add(g.tickets + blockIdx.x, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+  __syncthreads();
+  if (ticket != (uint32_t)g.splits - 1) return;
+  for (int t = tid >> 7; t < g.T; t += kDownWaves / 2) {
+    const float *const p = g.parts + t * row + n;
+    float v = 0.f;
+    int k = 0;
+    for (; k + 8 <= g.splits; k += 8) {
+      float q[8];
+#pragma unroll
+      for (int j = 0; j < 8; ++j) q[j] = __hip_atomic_load(p + (k + j) * part, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+#pragma unroll
+      for (int j = 0; j < 8; ++j) v += q[j];
+    }
+    for (; k < g.splits; ++k) v += __hip_atomic_load(p + k * part, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    if (n < g.H) T::store(Y + t * ldy + n, v);
   }
 }
 
@@ -491,43 +574,61 @@ __global__ __launch_bounds__(WAVES * 64, 2) void moe_down_kernel(MoeArgs g, type
 constexpr int64_t round_up(int64_t n, int64_t d) { return (n + d - 1) / d * d; }
 
 struct MoePlan {
-  int64_t logits, n_used, uses, tokens, shares, x, h, total;  // bytes: where they start, and in all
-  int x_row, h_row;  // bytes
+  int64_t logits, n_uses, uses, pair_tokens, shares, tickets, parts, x, h, total;  // bytes: where they start, and in all
+  int x_row, h_row, most_uses, pass, splits, row_groups;
 };
+
+constexpr int pass_of(bool f32) { return f32 ? 16 : 32; }
 
 MoePlan plan_of(int T, int H, int I, int E, int top, int32_t dtype) {
   MoePlan p;
-  const int terms = dtype == XORENC_X_F32 ? 3 : 1, h_terms = dtype == XORENC_X_F32 ? 3 : 2;
-  const int64_t most_used = E < T * top ? E : T * top;
+  const bool f32 = dtype == XORENC_X_F32;
+  const int terms = f32 ? 3 : 1, h_terms = f32 ? 3 : 2, pairs = T * top, used = E < pairs ? E : pairs;
+  p.pass = pass_of(f32);
+  p.most_uses = used + pairs / p.pass < pairs ? used + pairs / p.pass : pairs;
   p.x_row = (H + kBlock - 1) / kBlock * terms * (2 * kBlock);
   p.h_row = (I + kBlock - 1) / kBlock * h_terms * (2 * kBlock);
+  p.row_groups = (H + 127) / 128;
+  // workgroups of the second product: two for each CU, a block of the reduction each at least, 32 parts at most
+  const int64_t steps = (int64_t)used * ((I + kBlock - 1) / kBlock);
+  p.splits = (512 + p.row_groups - 1) / p.row_groups;
+  if (p.splits > steps) p.splits = (int)steps;
+  if (p.splits > 32) p.splits = 32;
   p.logits = 0;
-  p.n_used = round_up((int64_t)T * E * 4, 16);
-  p.uses = p.n_used + 16;
-  p.tokens = p.uses + most_used * (int64_t)sizeof(Use);
-  p.shares = p.tokens + most_used * kMostTokens;
-  p.x = round_up(p.shares + (int64_t)T * top * 4, 256);
+  p.n_uses = round_up((int64_t)T * E * 4, 16);
+  p.uses = p.n_uses + 16;
+  p.pair_tokens = p.uses + p.most_uses * (int64_t)sizeof(Use);
+  p.shares = round_up(p.pair_tokens + pairs, 16);
+  p.tickets = p.shares + pairs * 4;
+  p.parts = round_up(p.tickets + p.row_groups * 4, 256);
+  p.x = p.parts + (p.splits > 1 ? (int64_t)p.splits * T * p.row_groups * 512 : 0);
   p.h = p.x + (int64_t)T * p.x_row;
-  p.total = p.h + (int64_t)T * top * p.h_row;
+  p.total = p.h + (int64_t)pairs * p.h_row;
   return p;
 }
 
-template <int MT, int TERMS, int H_TERMS, int WAVES>
-void launch_up(const MoeArgs &g, dim3 grid, hipStream_t st) {
-  hipLaunchKernelGGL((moe_up_kernel<MT, TERMS, H_TERMS, WAVES>), grid, dim3(WAVES * 64), 0, st, g);
+template <int XR, int TERMS, int H_TERMS, int R, int S>
+void launch_up(const MoeArgs &g, hipStream_t st) {
+  constexpr int NS = UpShape<XR, TERMS, R, S, 3>::RING <= 80 * 1024 ? 3 : 2;  // (two workgroups a CU)
+  typedef UpShape<XR, TERMS, R, S, NS> Shape;
+  static_assert(Shape::LDS <= 160 * 1024, "a CU's");
+  const int tiles = (g.I + kBlock - 1) / kBlock * (kBlock / 16);
+  hipLaunchKernelGGL((moe_up_kernel<XR, TERMS, H_TERMS, R, S, NS>), dim3((unsigned)((tiles + R - 1) / R), (unsigned)g.most_uses), dim3(R * S * 64),
+                     Shape::LDS, st, g);
 }
 
-template <class T, int TERMS, int H_TERMS, int MT>
+template <class T, int XR, int TERMS, int H_TERMS>
 void launch_products(const MoeArgs &g, void *Y, int64_t ldy, hipStream_t st) {
-  constexpr int DOWN_WAVES = 8;
-  const dim3 grid((unsigned)((g.I + kBlock - 1) / kBlock * (kBlock / 16)), (unsigned)min(g.E, g.T * g.top));
-  const int64_t tasks = (int64_t)grid.x * grid.y;
-  if (tasks >= 2048)
-    launch_up<MT, TERMS, H_TERMS, 4>(g, grid, st);
+  const int64_t tiles = (int64_t)((g.I + 15) / 16) * g.most_uses;
+  if (tiles >= 2048)
+    launch_up<XR, TERMS, H_TERMS, 4, 1>(g, st);
   else
-    launch_up<MT, TERMS, H_TERMS, 8>(g, grid, st);
-  hipLaunchKernelGGL((moe_down_kernel<T, MT, H_TERMS, DOWN_WAVES>), dim3((unsigned)((g.H + 15) / 16)), dim3(DOWN_WAVES * 64), 0, st, g,
-                     static_cast<typename T::Elem *>(Y), ldy);
+    launch_up<XR, TERMS, H_TERMS, 1, 4>(g, st);
+  constexpr int NS = 3;
+  typedef DownShape<XR, H_TERMS, NS> Shape;
+  static_assert(Shape::RING + kMostTokens * 512 <= 150 * 1024, "a CU's, less what is declared in the kernel");
+  hipLaunchKernelGGL((moe_down_kernel<T, XR, H_TERMS, NS>), dim3((unsigned)g.row_groups, (unsigned)g.splits), dim3(kDownWaves * 64),
+                     (unsigned)(Shape::RING + g.T * 512), st, g, static_cast<typename T::Elem *>(Y), ldy);
 }
 
 template <class T, int TERMS, int H_TERMS>
@@ -537,16 +638,17 @@ int32_t launch_moe(const MoeArgs &g, const void *X, int64_t ldx, bool wide, cons
   const int64_t pieces = (int64_t)g.T * ((g.H + kBlock - 1) / kBlock) * 16;
   hipLaunchKernelGGL((router_kernel<T, TERMS>), dim3((unsigned)(groups + (pieces + 255) / 256)), dim3(256), 0, st,
                      static_cast<const E *>(X), ldx, (int)wide, static_cast<const E *>(router), ldr, (int)r_wide, g.T, g.H, g.E, g.logits,
-                     g.x_terms, groups);
+                     g.x_terms, groups, g.tickets, g.row_groups);
   if (g.T > 1) hipLaunchKernelGGL(picks_kernel, dim3(1), dim3(1024), 0, st, g);
   int32_t rc = xorenc_internal_check_launch();
   if (rc != XORENC_OK) return rc;
-  if (g.T <= 16)
-    launch_products<T, TERMS, H_TERMS, 1>(g, Y, ldy, st);
-  else if (g.T <= 32)
-    launch_products<T, TERMS, H_TERMS, 2>(g, Y, ldy, st);
+  constexpr int MOST = pass_of(TERMS > 1);
+  if (g.T <= 4)
+    launch_products<T, 4, TERMS, H_TERMS>(g, Y, ldy, st);
+  else if (g.T <= 16)
+    launch_products<T, 16, TERMS, H_TERMS>(g, Y, ldy, st);
   else
-    launch_products<T, TERMS, H_TERMS, 4>(g, Y, ldy, st);
+    launch_products<T, MOST, TERMS, H_TERMS>(g, Y, ldy, st);
   return xorenc_internal_check_launch();
 }
 
@@ -585,6 +687,7 @@ extern "C" int32_t xorenc_moe_fp8(const xorenc_moe *L, const void *X, int32_t x_
   if (!X || !Y || !L->router || !L->W13 || !L->S13 || !L->W2 || !L->S2 || !workspace) return XORENC_EINVAL;
   const MoePlan p = plan_of(tokens, H, I, E, picks, x_dtype);
   if (workspace_bytes < p.total) return XORENC_EINVAL;
+  if (L->ld_w13 > (1 << 24) || L->ld_w2 > (1 << 24) || L->ld_s13 > (1 << 16) || L->ld_s2 > (1 << 16)) return XORENC_ELIMIT;
   const int esz = dtype_bytes(x_dtype);
   if (!aligned_to(X, esz) || !aligned_to(Y, esz) || !aligned_to(L->router, esz) || !aligned_to(L->W13, 16) || L->ld_w13 % 16 ||
       L->w13_stride % 16 || !aligned_to(L->W2, 16) || L->ld_w2 % 16 || L->w2_stride % 16 || !aligned_to(L->S13, 4) ||
@@ -598,13 +701,15 @@ extern "C" int32_t xorenc_moe_fp8(const xorenc_moe *L, const void *X, int32_t x_
   g.ldw2 = L->ld_w2, g.w2_stride = L->w2_stride, g.lds2 = L->ld_s2, g.s2_stride = L->s2_stride;
   g.T = tokens, g.H = H, g.I = I, g.E = E, g.top = picks, g.renormalise = renormalise != 0;
   g.logits = reinterpret_cast<float *>(ws + p.logits);
+  g.n_uses = reinterpret_cast<int *>(ws + p.n_uses);
   g.uses = reinterpret_cast<Use *>(ws + p.uses);
-  g.n_used = reinterpret_cast<int *>(ws + p.n_used);
-  g.use_tokens = ws + p.tokens;
+  g.pair_tokens = ws + p.pair_tokens;
   g.shares = reinterpret_cast<float *>(ws + p.shares);
+  g.tickets = reinterpret_cast<uint32_t *>(ws + p.tickets);
+  g.parts = reinterpret_cast<float *>(ws + p.parts);
   g.x_terms = reinterpret_cast<uint16_t *>(ws + p.x);
   g.h_terms = reinterpret_cast<uint16_t *>(ws + p.h);
-  g.x_row = p.x_row, g.h_row = p.h_row;
+  g.x_row = p.x_row, g.h_row = p.h_row, g.most_uses = p.most_uses, g.pass = p.pass, g.splits = p.splits, g.row_groups = p.row_groups;
   const bool r_wide = wide_rows(L->router, L->ld_router, x_dtype);
   hipStream_t st = static_cast<hipStream_t>(hip_stream);
   xorenc_internal_begin_call();
