@@ -5,7 +5,7 @@
 // activations h of the picked experts; their second product and the sum over picks.  The bytes of the picked experts'
 // weights bound the last two.  Weights go from memory to a ring of stages in LDS (eight lanes fetch 128 bytes of a row; loads to
 // registers, where a lane needs 32 bytes of one row of 16, take the address units twice as long: 250 us for 32 tokens and
-// eight experts of 4096 x 9216, %%% this way), and so do the activations that multiply them.  e4m3 values become bf16 exactly
+// eight experts of 4096 x 9216, 207 this way), and so do the activations that multiply them.  e4m3 values become bf16 exactly
 // and multiply bf16 terms of the activations (one for bf16 activations, three for fp32, which sum to the value exactly), so
 // that nothing is rounded to 8 bits on the way; h is kept as bf16 terms that hold 16 (24) bits.  The tokens that picked an
 // expert are the columns of its matrix instructions; rows of tokens that are not there are not loaded.
@@ -442,7 +442,7 @@ __global__ __launch_bounds__(kDownWaves * 64) void moe_down_kernel(MoeArgs g, ty
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const uint32_t lds0 = lds_address(down_lds);
   const int n_uses = *g.n_uses, n0 = blockIdx.x * 128;
-  for (int i = tid; i < n_uses; i += kDownWaves * 64) uses[i] = g.uses[i];
+  for (int i = tid; i < g.most_uses; i += kDownWaves * 64) uses[i] = g.uses[i];  // (all of them: not a load behind a load)
   for (int i = tid; i < g.T * g.top; i += kDownWaves * 64) pair_tokens[i] = g.pair_tokens[i];
   for (int i = tid; i < g.T * 128; i += kDownWaves * 64) sums[i] = 0.f;
   const int blocks = (g.I + kBlock - 1) / kBlock, steps = n_uses * blocks, tail = g.I & (kBlock - 1);
@@ -589,9 +589,10 @@ MoePlan plan_of(int T, int H, int I, int E, int top, int32_t dtype) {
   p.x_row = (H + kBlock - 1) / kBlock * terms * (2 * kBlock);
   p.h_row = (I + kBlock - 1) / kBlock * h_terms * (2 * kBlock);
   p.row_groups = (H + 127) / 128;
-  // workgroups of the second product: two for each CU, a block of the reduction each at least, 32 parts at most
+  // workgroups of the second product: one for each CU (two: 213 against 207 us for 32 tokens and eight experts of 4096 x 9216, 24.9
+  // against 23.5 for one token and six of 2048 x 1024), a block of the reduction each at least, 32 parts at most
   const int64_t steps = (int64_t)used * ((I + kBlock - 1) / kBlock);
-  p.splits = (512 + p.row_groups - 1) / p.row_groups;
+  p.splits = (256 + p.row_groups - 1) / p.row_groups;
   if (p.splits > steps) p.splits = (int)steps;
   if (p.splits > 32) p.splits = 32;
   p.logits = 0;
@@ -609,7 +610,7 @@ MoePlan plan_of(int T, int H, int I, int E, int top, int32_t dtype) {
 
 template <int XR, int TERMS, int H_TERMS, int R, int S>
 void launch_up(const MoeArgs &g, hipStream_t st) {
-  constexpr int NS = UpShape<XR, TERMS, R, S, 3>::RING <= 80 * 1024 ? 3 : 2;  // (two workgroups a CU)
+  constexpr int NS = R > 1 && UpShape<XR, TERMS, R, S, 3>::RING <= 80 * 1024 ? 3 : 2;  // (two workgroups a CU, three with R = 1)
   typedef UpShape<XR, TERMS, R, S, NS> Shape;
   static_assert(Shape::LDS <= 160 * 1024, "a CU's");
   const int tiles = (g.I + kBlock - 1) / kBlock * (kBlock / 16);
@@ -619,11 +620,14 @@ void launch_up(const MoeArgs &g, hipStream_t st) {
 
 template <class T, int XR, int TERMS, int H_TERMS>
 void launch_products(const MoeArgs &g, void *Y, int64_t ldy, hipStream_t st) {
+  // Four waves: side by side where x is wide and they share it, in pairs otherwise, and all on the same 16 rows where there
+  // are few of them (us, in this order: 32 tokens, two of eight experts of 4096 x 9216 207, 215, 250; 16 tokens 197, 186,
+  // 191; eight tokens, four of 16 experts of 4096 x 4096 176, 163, 167; one token, six of 2048 x 1024 24, 23, 22.5)
   const int64_t tiles = (int64_t)((g.I + 15) / 16) * g.most_uses;
-  if (tiles >= 2048)
-    launch_up<XR, TERMS, H_TERMS, 4, 1>(g, st);
-  else
+  if (tiles < 2048)
     launch_up<XR, TERMS, H_TERMS, 1, 4>(g, st);
+  else
+    launch_up<XR, TERMS, H_TERMS, (XR == 32 ? 4 : 2), (XR == 32 ? 1 : 2)>(g, st);
   constexpr int NS = 3;
   typedef DownShape<XR, H_TERMS, NS> Shape;
   static_assert(Shape::RING + kMostTokens * 512 <= 150 * 1024, "a CU's, less what is declared in the kernel");
