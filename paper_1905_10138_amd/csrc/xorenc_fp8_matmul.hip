@@ -29,38 +29,40 @@ void launch_ring(const MatmulArgs &g, bool wide, hipStream_t st) {
 // waves take the blocks in turn).  Fitted to 80 shapes of 1 .. 8192 x 128 .. 16384 x 256 .. 9216 for either type of results;
 // taking the one that this says is the fastest costs 1 % over taking the one that was.  Some of the times it goes by (us, bf16,
 // in the order of the list):
-//   8192 x 1000 x 770        23   20   21   31   27  110   53   38
-//   4096 x 4096 x 4096       61   76   93  123  125    -    -    -
-//   1024 x 2048 x 2048       25   17   14   11   14   49   20   14
-//   512 x 4096 x 9216       118   66   56   34   55  193   73   53
-//   250 x 6000 x 3000        45   25   21   16   20   67   31   21
-//   64 x 16384 x 4096        57   32   27   17   25   41   23   19
-//   128 x 4096 x 4096        53   29   24   15   24   20   14   11
-//   16 x 4096 x 4096         51   28   24   15   22  5.4  6.6   11
-//   1 x 4096 x 9216         114   59   51   29   51  7.8   10   19
+//   8192 x 1000 x 770        24   17   20   34   28  145  113   76   49
+//   4096 x 4096 x 4096       61   77   96  163  144  615  391  260  191
+//   1024 x 2048 x 2048       31   19   16   12   13   43   32   23   15
+//   512 x 4096 x 9216       116   66   57   34   48  131   73   60   46
+//   250 x 6000 x 3000        45   26   21   16   19   44   31   24   21
+//   64 x 16384 x 4096        55   33   28   18   23   34   22   19   14
+//   128 x 4096 x 4096        54   32   27   15   22   19   12  9.6   12
+//   16 x 4096 x 4096         53   32   27   15   22  5.4  6.5  9.0   12
+//   1 x 4096 x 9216         114   67   56   29   48  8.1  9.9   15   23
 struct Cost {
   int bn, bm, slots, split;
   float start, tile, step, load;
 };
-constexpr int kKernels = 8;
+constexpr int kKernels = 9;
 constexpr Cost kCosts[2][kKernels] = {
-    {{256, 256, 256, 1, 0.00f, 10.25f, 1.54f, 0.24f},  // 0: tiles of 256 x 256, two stages in halves
-     {128, 128, 512, 1, 0.55f, 5.34f, 0.81f, 0.32f},   // 1: of 128 x 128
-     {128, 64, 768, 1, 0.71f, 3.41f, 0.68f, 0.36f},    // 2: of 128 x 64
-     {64, 64, 512, 2, 1.48f, 2.08f, 0.69f, 0.37f},     // 3: rings of two stages: of 64 x 64, two groups of four waves
-     {64, 64, 1024, 1, 0.87f, 2.20f, 0.61f, 0.40f},    // 4: of 64 x 64, one group
-     {16, 16, 512, 8, 2.03f, 1.17f, 0.34f, 0.47f},     // 5: of 16 x 16, eight waves that split the reduction
-     {32, 32, 256, 8, 1.18f, 2.32f, 0.83f, 0.18f},     // 6: of 32 x 32, the same
-     {64, 32, 256, 4, 1.44f, 1.87f, 0.89f, 0.17f}},    // 7: of 64 x 32, four groups of two waves
+    {{256, 256, 256, 1, 0.00f, 10.16f, 1.53f, 0.19f},  // 0: tiles of 256 x 256, two stages in halves
+     {128, 128, 512, 1, 0.60f, 5.17f, 0.84f, 0.27f},   // 1: of 128 x 128
+     {128, 64, 768, 1, 0.76f, 3.25f, 0.70f, 0.32f},    // 2: of 128 x 64
+     {64, 64, 512, 2, 1.23f, 2.41f, 0.71f, 0.37f},     // 3: rings of two stages: of 64 x 64, two groups of four waves
+     {64, 64, 1024, 1, 1.18f, 2.26f, 0.54f, 0.43f},    // 4: of 64 x 64, one group
+     {16, 16, 512, 8, 2.03f, 1.18f, 0.35f, 0.45f},     // 5: of 16 x 16, eight waves that split the reduction
+     {32, 32, 256, 8, 1.14f, 2.39f, 0.81f, 0.18f},     // 6: of 32 x 32, the same
+     {64, 32, 256, 4, 1.59f, 2.98f, 0.65f, 0.12f},     // 7: of three stages: of 64 x 32, four groups of two waves
+     {64, 64, 256, 2, 1.41f, 2.73f, 0.54f, 0.08f}},    // 8: of 64 x 64, two groups of four waves
     // fp32 results (those of a tile of 256 x 256 do not fit in LDS, nor its operands in registers)
     {{},
-     {128, 128, 512, 1, 1.49f, 6.09f, 1.10f, 0.57f},
-     {128, 64, 768, 1, 1.26f, 3.88f, 0.89f, 0.59f},
+     {128, 128, 512, 1, 1.76f, 6.06f, 1.17f, 0.47f},
+     {128, 64, 768, 1, 1.43f, 3.66f, 0.92f, 0.51f},
      {64, 64, 512, 2, 2.00f, 2.29f, 0.72f, 0.60f},
-     {64, 64, 1024, 1, 0.66f, 2.75f, 0.69f, 0.65f},
-     {16, 16, 512, 8, 2.06f, 1.19f, 0.44f, 0.40f},
-     {32, 32, 256, 8, 1.19f, 2.47f, 0.91f, 0.13f},
-     {64, 32, 256, 4, 1.49f, 2.26f, 0.95f, 0.13f}}};
+     {64, 64, 1024, 1, 0.45f, 3.05f, 0.66f, 0.68f},
+     {16, 16, 512, 8, 2.13f, 1.30f, 0.38f, 0.43f},
+     {32, 32, 256, 8, 1.18f, 2.65f, 0.90f, 0.12f},
+     {64, 32, 256, 4, 1.47f, 3.26f, 0.81f, 0.10f},
+     {64, 64, 256, 2, 1.25f, 3.07f, 0.77f, 0.05f}}};
 
 int cheapest(int64_t M, int64_t N, int64_t blocks, bool exact) {
   int best = -1;
@@ -87,9 +89,10 @@ int32_t dispatch_matmul(const MatmulArgs &g, bool wide, hipStream_t st) {
     case 2: launch_tile<4, 2, 2, 2, EXACT>(g, wide, st); break;
     case 3: launch_ring<2, 2, 2, 2, 2, 2, EXACT>(g, wide, st); break;
     case 4: launch_ring<2, 2, 2, 2, 1, 2, EXACT>(g, wide, st); break;
+    case 8: launch_ring<2, 2, 2, 2, 2, 3, EXACT>(g, wide, st); break;
     case 5: launch_ring<1, 1, 1, 1, 8, 2, EXACT>(g, wide, st); break;
     case 6: launch_ring<2, 2, 1, 1, 8, 2, EXACT>(g, wide, st); break;
-    case 7: launch_ring<2, 2, 2, 1, 4, 2, EXACT>(g, wide, st); break;
+    case 7: launch_ring<2, 2, 2, 1, 4, 3, EXACT>(g, wide, st); break;
     default: return XORENC_ELIMIT;
   }
   return xorenc_internal_check_launch();

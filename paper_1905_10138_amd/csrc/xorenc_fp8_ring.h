@@ -56,16 +56,16 @@ __global__ __launch_bounds__(WN *WM *KG * 64) void matmul_ring_kernel(MatmulArgs
   const int s_rows = in_group % (Shape::SCALES / 64) * 64;
   const uint32_t s_at = (uint32_t)(min(s_rows + lane, g.M - m0 - 1) * g.sa_row) * 4u, s_step = (uint32_t)(g.sa_blk * 4);
   const int tail = g.K & (kBlock - 1), stages = (g.blocks + KG - 1) / KG;
-  // Stage s of this group's blocks into its slot.  A block past the last one reads as zero, and so do chunks behind column K.
-  auto fetch = [&](int s) {
+  // Load i of stage s of this group's blocks into its slot.  A block past the last one reads as zero, and so do chunks behind
+  // column K.
+  auto fetch = [&](int s, int i) {
     const int b = s * KG + kg;
     const uint32_t to = lds0 + (uint32_t)(s % NS) * STAGE + kg * BLOCK;
     const int most = b >= g.blocks ? 0 : tail && b == g.blocks - 1 ? tail : kBlock;  // columns of the block
-    const uint32_t col = (uint32_t)b * kBlock;
-#pragma unroll
-    for (int i = 0; i < PER; ++i)
-      fetch_16(to + (in_group * PER + i) * 1024, chunk_of(i) >= most ? kBeyond : at[i], of_w(i) ? w_desc : a_desc, most ? col : 0u);
-    fetch_4(to + (BN + BM) * 128 + s_rows * 4, most ? s_at : kBeyond, s_desc, most ? (uint32_t)b * s_step : 0u);
+    if (i < PER)
+      fetch_16(to + (in_group * PER + i) * 1024, chunk_of(i) >= most ? kBeyond : at[i], of_w(i) ? w_desc : a_desc, most ? (uint32_t)b * kBlock : 0u);
+    else
+      fetch_4(to + (BN + BM) * 128 + s_rows * 4, most ? s_at : kBeyond, s_desc, most ? (uint32_t)b * s_step : 0u);
   };
   const int w_row = (n0 + wn * (TN * 16)) / kBlock;
   const float *const sw_row = g.SW + (int64_t)(w_row * kBlock < g.N ? w_row : 0) * g.ldsw;
@@ -78,19 +78,15 @@ __global__ __launch_bounds__(WN *WM *KG * 64) void matmul_ring_kernel(MatmulArgs
     for (int j = 0; j < TM; ++j) acc[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
   const uint32_t off = e4m3_operand_offset(lane);
   constexpr int LOADS = PER + 1;  // of a wave per stage
-#pragma unroll
-  for (int s = 0; s < NS - 1; ++s) fetch(s);  // (stages past the last read as zero: every wave has as many loads on their way)
-  for (int s = 0; s < stages; ++s) {
-    // this stage has landed, and every wave has read the one before, whose slot is filled next
-    if constexpr (Shape::GROUP > 1)
-      asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"((NS - 2) * LOADS) : "memory");
-    else  // (a wave on its own)
-      asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" ::"n"((NS - 2) * LOADS) : "memory");
-    fetch(s + NS - 1);
-    const int b = s * KG + kg;
+  struct Operands {
+    E4m3Operand w[TN], a[TM];
+    float sa[TM];
+  };
+  // The operands of stage s, which has landed.
+  auto read = [&](int s, Operands &o) {
     uint8_t *const slot = ring_lds + (uint32_t)(s % NS) * STAGE + kg * BLOCK;
     if ((tail & 15) && s == stages - 1) {  // what the last chunk of a row holds behind column K
-      if (b == g.blocks - 1) {
+      if (s * KG + kg == g.blocks - 1) {
         for (int row = in_group * 64 + lane; row < BN + BM; row += Shape::GROUP * 64) {
           uint8_t *const p = slot + row * 128 + (((tail >> 4) ^ (((row < BN ? row : row - BN) >> 1) & 7)) * 16);
           *reinterpret_cast<u32x4 *>(p) = first_bytes(*reinterpret_cast<u32x4 *>(p), tail & 15);
@@ -98,26 +94,72 @@ __global__ __launch_bounds__(WN *WM *KG * 64) void matmul_ring_kernel(MatmulArgs
       }
       asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
     }
-    if (b >= g.blocks) continue;  // (uniform; the last stage)
-    E4m3Operand w[TN], a[TM];
-    float sa[TM];
 #pragma unroll
-    for (int j = 0; j < TM; ++j) sa[j] = reinterpret_cast<const float *>(slot + (BN + BM) * 128)[(wm * TM + j) * 16 + r];
+    for (int j = 0; j < TM; ++j) o.a[j] = read_operand(slot + (BN + (wm * TM + j) * 16) * 128, off);
 #pragma unroll
-    for (int j = 0; j < TM; ++j) a[j] = read_operand(slot + (BN + (wm * TM + j) * 16) * 128, off);
+    for (int i = 0; i < TN; ++i) o.w[i] = read_operand(slot + (wn * TN + i) * 2048, off);
 #pragma unroll
-    for (int i = 0; i < TN; ++i) w[i] = read_operand(slot + (wn * TN + i) * 2048, off);
-    if ((b & 63) == kg % 64 && b >= 64) sw_run = sw_row[min((b & ~63) + lane, g.blocks - 1)];
+    for (int j = 0; j < TM; ++j) o.sa[j] = reinterpret_cast<const float *>(slot + (BN + BM) * 128)[(wm * TM + j) * 16 + r];
+  };
+  // The products of stage s; between them the loads of stage `next`, where it is not negative.
+  auto multiply = [&](int s, const Operands &o, int next) {
+    const int b = s * KG + kg;
+    if ((b & 63) == kg && b >= 64) sw_run = sw_row[min(b + lane - kg, g.blocks - 1)];
     const float sw = __int_as_float(__builtin_amdgcn_readlane(__float_as_int(sw_run), b & 63));
+    const bool there = b < g.blocks;  // (else the last stage, for some groups: zeros)
 #pragma unroll
     for (int j = 0; j < TM; ++j) {
-      const float f = sa[j] * sw;
+      const float f = there ? o.sa[j] * sw : 0.f;
 #pragma unroll
       for (int i = 0; i < TN; ++i) {
-        const f32x4 d = product_128<EXACT>(w[i], a[j]);
+        const int k = j * TN + i;
+        const f32x4 d = product_128<EXACT>(o.w[i], o.a[j]);
+        if (next >= 0) {
 #pragma unroll
-        for (int k = 0; k < 4; ++k) acc[i][j][k] += f * d[k];
+          for (int l = k * LOADS / (TN * TM); l < (k + 1) * LOADS / (TN * TM); ++l) fetch(next, l);
+        }
+#pragma unroll
+        for (int n = 0; n < 4; ++n) acc[i][j][n] += f * d[n];
       }
+    }
+  };
+  auto fetch_all = [&](int s) {  // (stages past the last read as zero: every wave has as many loads on their way)
+#pragma unroll
+    for (int l = 0; l < LOADS; ++l) fetch(s, l);
+  };
+  if constexpr (Shape::GROUP > 1 && !(EXACT && KG * NS == 4)) {
+    // A stage's operands are in registers before the one before is multiplied, and the loads into its slot go between the
+    // products: a wave that issues its loads in a run waits for the address unit, 35 cycles a load, before it may multiply
+    // (64 x 16384 x 4096 with three stages 17.2 -> 14.4 us).
+    Operands o[2];
+#pragma unroll
+    for (int s = 0; s < NS; ++s) fetch_all(s);
+    asm volatile("s_waitcnt vmcnt(%0)\n\ts_barrier" ::"n"((NS - 1) * LOADS) : "memory");
+    read(0, o[0]);
+    auto landed = [&]() {  // and every wave has read the stage before, whose slot is filled next
+      asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"((NS - 2) * LOADS) : "memory");
+    };
+    for (int s = 0; s < stages; s += 2) {
+      landed();
+      if (s + 1 < stages) read(s + 1, o[1]);
+      multiply(s, o[0], s + NS);
+      if (s + 1 == stages) break;
+      landed();
+      if (s + 2 < stages) read(s + 2, o[0]);
+      multiply(s + 1, o[1], s + 1 + NS);
+    }
+  } else {
+    // A stage's loads, its operands, its products, where that leaves registers for more waves: those on their own, which need no
+    // barrier (1 x 4096 x 9216 8.1 us; as above 10.1), and two workgroups a CU with operands in bf16 (250 x 6000 x 3000 21, 29).
+    Operands o;
+#pragma unroll
+    for (int s = 0; s < NS - 1; ++s) fetch_all(s);
+    for (int s = 0; s < stages; ++s) {
+      asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" ::"n"((NS - 2) * LOADS) : "memory");
+      if constexpr (Shape::GROUP > 1) asm volatile("s_barrier" ::: "memory");
+      fetch_all(s + NS - 1);
+      read(s, o);
+      multiply(s, o, -1);
     }
   }
   asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");  // (no load may land in what follows)
