@@ -10,7 +10,7 @@
 // lower half of its rows of W, so that those of the next block but one can be fetched into their place (group 1), and the
 // upper half of this block's W has landed; at the second, before the last row tile, all of the block has been read (the
 // upper half is fetched, group 2) and the next block's group 1 has landed.  A fetch so has 1.4 blocks' time to land, not one
-// (8192 x 16384 x 4096: 624 -> %%% us), and the matrix instructions of the row tile behind a barrier cover its wait and the
+// (8192 x 16384 x 4096: 624 -> 570 us), and the matrix instructions of the row tile behind a barrier cover its wait and the
 // operand reads behind it.
 #ifndef XORENC_FP8_TILE_H
 #define XORENC_FP8_TILE_H
