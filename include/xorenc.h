@@ -421,7 +421,7 @@ typedef struct xorenc_moe {
 
 /*
  * The whole layer for a few tokens (X tokens x hidden, Y likewise and of the same type; Y may be X):
- *   logits = router x (fp32);  the `picks` experts with the largest logits, the lowest index of equals;
+ *   logits = router x (fp32);  the `picks` experts with the largest logits (a NaN before all), the lowest index of equals;
  *   share = softmax over all experts, with renormalise != 0 divided by the picked ones' sum;
  *   y = sum over the picks of share * W2_e (silu(G_e x) * (U_e x)).
  * Activations are not rounded to 8 bits; the inner ones keep 16 bits of mantissa (24 for fp32 X).  Weights of experts that no

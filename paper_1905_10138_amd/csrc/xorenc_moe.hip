@@ -110,9 +110,10 @@ __global__ __launch_bounds__(256) void router_kernel(const typename T::Elem *__r
 
 // ---------------------------------------------------------------------------------------------- picks
 
-// fp32 -> integers in the same order (NaN above infinity or below its negative, as the sign says)
+// fp32 -> integers in the same order, any NaN above infinity
 __device__ inline uint32_t ordered(float v) {
   const uint32_t b = __float_as_uint(v);
+  if (v != v) return 0xffffffffu;
   return b & 0x80000000u ? ~b : b | 0x80000000u;
 }
 __device__ inline float from_ordered(uint32_t k) { return __uint_as_float(k & 0x80000000u ? k & 0x7fffffffu : ~k); }
