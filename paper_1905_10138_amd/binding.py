@@ -113,6 +113,20 @@ def load_library():
     lib.xorenc_spmm.argtypes = [_LayerArgument, vp, i32, i64, i32, vp, i64, vp]
     lib.xorenc_spmm_ws.restype = i32
     lib.xorenc_spmm_ws.argtypes = [_LayerArgument, vp, i32, i64, i32, vp, i64, vp, i64, vp]
+    f32 = ctypes.c_float
+    lib.xorenc_quant_fp8.restype = i32
+    lib.xorenc_quant_fp8.argtypes = [vp, i32, i64, i64, i32, i64, i32, i32, vp, i64, i64, vp, i64, i64, i64, vp]
+    lib.xorenc_add_rmsnorm_fp8.restype = i32
+    lib.xorenc_add_rmsnorm_fp8.argtypes = [vp, i32, i64, vp, i64, vp, i32, i64, i32, f32, vp, i64, vp, i64, i64, vp, i64,
+                                           vp, i64, i64, vp]
+    lib.xorenc_silu_mul_fp8.restype = i32
+    lib.xorenc_silu_mul_fp8.argtypes = [vp, vp, i32, i64, i64, i32, vp, i64, vp, i64, i64, vp]
+    lib.xorenc_matmul_fp8.restype = i32
+    lib.xorenc_matmul_fp8.argtypes = [vp, i64, vp, i64, i64, vp, i64, vp, i64, i32, i32, i32, vp, i32, i64, vp]
+    lib.xorenc_moe_workspace.restype = i32
+    lib.xorenc_moe_workspace.argtypes = [i32, i32, i32, i32, i32, i32, vp]
+    lib.xorenc_moe_fp8.restype = i32
+    lib.xorenc_moe_fp8.argtypes = [ctypes.c_char_p, vp, i32, i64, i32, i32, i32, vp, i64, vp, i64, vp]
     _LIB = lib
     return lib
 

@@ -1,14 +1,16 @@
-"""Builds libxorenc.so (HIP, gfx950) in-tree with hipcc.  `python -m paper_1905_10138_amd.build`."""
+"""Builds libxorenc.so (HIP, gfx950) and _fp8.so (the calls for torch tensors) in-tree with hipcc.  `python -m paper_1905_10138_amd.build`."""
 import os
 import shutil
 import subprocess
 import sys
+import sysconfig
 from concurrent.futures import ThreadPoolExecutor
 
 PKG_DIR = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(PKG_DIR, "csrc")
 OBJ_DIR = os.path.join(PKG_DIR, "_build")
 LIB_PATH = os.path.join(PKG_DIR, "libxorenc.so")
+EXT_PATH = os.path.join(PKG_DIR, "_fp8.so")
 SOURCES = ["xorenc_host.cpp", "xorenc_paper.cpp", "xorenc_decode.hip", "xorenc_encode.hip", "xorenc_spmm.hip",
            "xorenc_spmm_q1.hip", "xorenc_spmm_q2.hip", "xorenc_spmm_q3.hip", "xorenc_spmm_q4.hip",
            "xorenc_fp8_rows.hip", "xorenc_fp8_matmul.hip", "xorenc_moe.hip"]
@@ -18,6 +20,22 @@ FLAGS = [
     "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops",
     "-Wall", "-Wno-unused-function",
 ]
+
+
+def extension_commands(hipcc):
+    """Compile and link _fp8.so, against torch's libraries and libxorenc.so beside it."""
+    import torch
+    base = os.path.dirname(torch.__file__)
+    obj = os.path.join(OBJ_DIR, "xorenc_torch_fp8.o")
+    compile_it = [hipcc, "-x", "c++", "-O2", "-std=c++17", "-fPIC", "-fvisibility=hidden", "-D__HIP_PLATFORM_AMD__=1", "-DUSE_ROCM=1",
+                  f"-D_GLIBCXX_USE_CXX11_ABI={int(torch._C._GLIBCXX_USE_CXX11_ABI)}", "-isystem", os.path.join(base, "include"),
+                  "-isystem", os.path.join(base, "include", "torch", "csrc", "api", "include"),
+                  "-isystem", sysconfig.get_paths()["include"],
+                  "-isystem", os.path.join(os.path.dirname(os.path.dirname(os.path.realpath(hipcc))), "include"), "-Wall",
+                  "-c", os.path.join(CSRC, "xorenc_torch_fp8.cpp"), "-o", obj]
+    link_it = [hipcc, "-shared", "-fPIC", obj, "-L" + os.path.join(base, "lib"), "-lc10", "-lc10_hip", "-ltorch_cpu", "-ltorch_hip", "-ltorch_python",
+               "-L" + PKG_DIR, "-lxorenc", "-Wl,-rpath,$ORIGIN", "-o", EXT_PATH + ".tmp"]
+    return compile_it, link_it
 
 
 def hipcc_path() -> str:
@@ -36,19 +54,23 @@ def _run(cmd):
 
 
 def build_library(verbose: bool = False, jobs: int = 8) -> str:
-    """Compile every HIP source for gfx950 (objects in parallel) and link one shared library."""
+    """Compile every source (objects in parallel; HIP for gfx950) and link the shared library and the extension."""
     hipcc = hipcc_path()
     os.makedirs(OBJ_DIR, exist_ok=True)
     objs = [os.path.join(OBJ_DIR, os.path.splitext(s)[0] + ".o") for s in SOURCES]
     cmds = [[hipcc] + FLAGS + ["-x", "hip", "-c", os.path.join(CSRC, s), "-o", o] for s, o in zip(SOURCES, objs)]
+    compile_extension, link_extension = extension_commands(hipcc)
+    cmds.insert(0, compile_extension)
     with ThreadPoolExecutor(max_workers=max(1, min(jobs, len(cmds)))) as ex:
         outs = list(ex.map(_run, cmds))
     outs.append(_run([hipcc, "--offload-arch=gfx950", "-shared", "-fPIC"] + objs + ["-o", LIB_PATH + ".tmp"]))
+    os.replace(LIB_PATH + ".tmp", LIB_PATH)
+    outs.append(_run(link_extension))
+    os.replace(EXT_PATH + ".tmp", EXT_PATH)
     if verbose:
         for o in outs:
             if o.strip():
                 print(o)
-    os.replace(LIB_PATH + ".tmp", LIB_PATH)
     return LIB_PATH
 
 

@@ -69,3 +69,17 @@ def test_the_whole(example, layers, tokens):
     t, d = gated(x, r)
     s, e = moe(d, t)
     assert torch.equal(y, s + e) and torch.equal(s, (d.float() + t.float()).to(s.dtype)) and torch.isfinite(y).all()
+
+
+def test_arguments_that_are_no_tensors_of_the_call():
+    x = torch.zeros(4, 256, device="cuda")
+    Q, S = xe.quant_fp8(x)
+    W, SW = xe.quant_fp8(x, block_rows=128)
+    for call in (lambda: xe.quant_fp8(None), lambda: xe.silu_mul_fp8([1.0]), lambda: xe.matmul_fp8(Q, S, W, 1), lambda: xe.quant_fp8(x, "1"),
+                 lambda: xe.add_rmsnorm_fp8(x, x[0], eps="1"), lambda: xe.add_rmsnorm_fp8(x, x[0], normed="yes")):
+        with pytest.raises(TypeError):
+            call()
+    for call in (lambda: xe.quant_fp8(x, 1 << 40), lambda: xe.matmul_fp8(Q, S, W, SW, out_dtype=3), lambda: xe.quant_fp8(x.to_sparse()),
+                 lambda: xe.quant_fp8(x[:, None, None]), lambda: xe.quant_fp8(x.to("meta")), lambda: xe.add_rmsnorm_fp8(x, x[0], normed=x.cpu())):
+        with pytest.raises(ValueError):
+            call()
