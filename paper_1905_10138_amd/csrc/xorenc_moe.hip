@@ -1,7 +1,7 @@
 // A mixture-of-experts layer for a few tokens: Y = sum over a token's picks of share * W2_e (silu(G_e x) * (U_e x)), with
 // expert weights in e4m3 (a scale per 128 x 128 block) and everything else in 16 or 32 bits.
 //
-// Four launches: the router's logits; the picks (not for a single token, whose picks every workgroup finds by itself); the gated
+// Four launches: the router's logits; the picks (not for very few tokens, whose picks every workgroup finds by itself); the gated
 // activations h of the picked experts; their second product and the sum over picks.  The bytes of the picked experts'
 // weights bound the last two.  Weights go from memory to a ring of stages in LDS (eight lanes fetch 128 bytes of a row; loads to
 // registers, where a lane needs 32 bytes of one row of 16, take the address units twice as long: 250 us for 32 tokens and
@@ -34,6 +34,7 @@ struct MoeArgs {
   int64_t ldw13, w13_stride, lds13, s13_stride, ldw2, w2_stride, lds2, s2_stride;
   int T, H, I, E, top, renormalise;
   int most_uses, pass;      // most_uses of them, the last ones with count 0; tokens that a pass takes at most
+  int plans;                // every workgroup of the first product finds the uses by itself
   float *logits;            // [T][E]
   int *n_uses;              // how many
   Use *uses;
@@ -164,15 +165,18 @@ __device__ inline void picks_of_token(const MoeArgs &g, int t, int lane, int &ex
   share /= sum;
 }
 
-// One workgroup; a wave per token at a time.
-__global__ __launch_bounds__(1024) void picks_kernel(MoeArgs g) {
-  constexpr int WAVES = 16;
-  __shared__ struct {
-    uint64_t tokens[kMostExperts];  // that picked an expert, a bit each
-    float share[kMostTokens][kMostPicks];
-    uint16_t expert[kMostTokens][kMostPicks];
-    uint16_t first[kMostExperts];  // pair of an expert
-  } p;
+template <int TOKENS>
+struct Picks {
+  uint64_t tokens[kMostExperts];  // that picked an expert, a bit each
+  float share[TOKENS][kMostPicks];
+  uint16_t expert[TOKENS][kMostPicks];
+  uint16_t first[kMostExperts];  // pair of an expert
+};
+
+// The uses in the order of their experts and the pairs in the order of the uses, by a workgroup of WAVES waves, one per token at a
+// time: put_count(uses), put_use(index, use), up to most_uses of them, and put_pair(index, token, share).
+template <int WAVES, int TOKENS, class PutCount, class PutUse, class PutPair>
+__device__ inline void plan_uses(const MoeArgs &g, Picks<TOKENS> &p, PutCount put_count, PutUse put_use, PutPair put_pair) {
   const int tid = threadIdx.x, lane = tid & 63;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   if (tid < kMostExperts) p.tokens[tid] = 0u;
@@ -209,19 +213,28 @@ __global__ __launch_bounds__(1024) void picks_kernel(MoeArgs g) {
       const int e = 4 * lane + i, first = before & 0xffff, count = n[i] & 0xffff;
       p.first[e] = (uint16_t)first;
       for (int k = 0; k * g.pass < count; ++k)
-        g.uses[(before >> 16) + k] = Use{(uint16_t)e, (uint16_t)(first + k * g.pass), (uint16_t)min(g.pass, count - k * g.pass), 0};
+        put_use((before >> 16) + k, Use{(uint16_t)e, (uint16_t)(first + k * g.pass), (uint16_t)min(g.pass, count - k * g.pass), 0});
       before += n[i];
     }
-    if (lane == 0) *g.n_uses = uses;
-    for (int u = uses + lane; u < g.most_uses; u += 64) g.uses[u] = Use{0, 0, 0, 0};
+    if (lane == 0) put_count(uses);
+    for (int u = uses + lane; u < g.most_uses; u += 64) put_use(u, Use{0, 0, 0, 0});
   }
   __syncthreads();
   for (int i = tid; i < g.T * g.top; i += WAVES * 64) {
     const int t = i / g.top, j = i - t * g.top, e = p.expert[t][j];
-    const int pair = p.first[e] + __popcll(p.tokens[e] & ((1ull << t) - 1ull));
-    g.pair_tokens[pair] = (uint8_t)t;
-    g.shares[pair] = p.share[t][j];
+    put_pair(p.first[e] + __popcll(p.tokens[e] & ((1ull << t) - 1ull)), t, p.share[t][j]);
   }
+}
+
+// One workgroup.
+__global__ __launch_bounds__(1024) void picks_kernel(MoeArgs g) {
+  __shared__ Picks<kMostTokens> p;
+  plan_uses<16>(
+      g, p, [&](int uses) { *g.n_uses = uses; }, [&](int u, Use use) { g.uses[u] = use; },
+      [&](int pair, int t, float share) {
+        g.pair_tokens[pair] = (uint8_t)t;
+        g.shares[pair] = share;
+      });
 }
 
 // ---------------------------------------------------------------------------------------------- products
@@ -284,6 +297,36 @@ __global__ __launch_bounds__(R *S * 64) void moe_up_kernel(MoeArgs g) {
       g.pair_tokens[first] = 0;
       if (first == 0) *g.n_uses = g.top;
     }
+  } else if (XR == 4 && R == 1 && g.plans) {
+    __shared__ struct {
+      Picks<XR> p;
+      Use mine;
+      float share[XR * kMostPicks];
+      uint8_t token[XR * kMostPicks];
+    } own;
+    const bool tells = blockIdx.x == 0 && blockIdx.y == 0;
+    plan_uses<R * S>(
+        g, own.p,
+        [&](int uses) {
+          if (tells) *g.n_uses = uses;
+        },
+        [&](int u, Use use) {
+          if (u != (int)blockIdx.y) return;
+          own.mine = use;
+          if (blockIdx.x == 0) g.uses[u] = use;
+        },
+        [&](int pair, int t, float share) {
+          own.token[pair] = (uint8_t)t;
+          own.share[pair] = share;
+          if (tells) g.pair_tokens[pair] = (uint8_t)t;
+        });
+    __syncthreads();
+    e = __builtin_amdgcn_readfirstlane(own.mine.expert), first = __builtin_amdgcn_readfirstlane(own.mine.first),
+    count = __builtin_amdgcn_readfirstlane(own.mine.count);
+    if (count == 0) return;
+    const int pair = first + min(lane, count - 1);
+    token = own.token[pair];
+    share = own.share[pair];
   } else {
     const Use use = g.uses[blockIdx.y];
     e = use.expert, first = use.first, count = use.count;
@@ -570,6 +613,104 @@ __global__ __launch_bounds__(kDownWaves * 64) void moe_down_kernel(MoeArgs g, ty
   }
 }
 
+// The same for at most XR <= 4 tokens and rows enough: a workgroup takes 16 rows of W2, and its eight waves take the blocks of
+// all uses in turn, each with a ring of its own, so that no sums cross workgroups.
+template <int XR, int H_TERMS, int NS>
+struct FewShape {
+  static constexpr int X_LOADS = (XR * H_TERMS + 3) / 4, STAGE = 2048 + X_LOADS * 1024 + 256, RING = kDownWaves * NS * STAGE;
+  static constexpr int LOADS = 2 + X_LOADS + 1;
+};
+
+template <class T, int XR, int H_TERMS, int NS>
+__global__ __launch_bounds__(kDownWaves * 64) void moe_down_few_kernel(MoeArgs g, typename T::Elem *__restrict__ Y, int64_t ldy) {
+  typedef FewShape<XR, H_TERMS, NS> Shape;
+  constexpr int X_LOADS = Shape::X_LOADS;
+  extern __shared__ __attribute__((aligned(1024))) uint8_t few_lds[];
+  __shared__ Use uses[4 * kMostPicks];
+  __shared__ uint8_t pair_tokens[4 * kMostPicks];
+  __shared__ __attribute__((aligned(16))) float sums[kDownWaves][XR][16];
+  const int tid = threadIdx.x, lane = tid & 63, r = lane & 15;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const uint32_t lds0 = lds_address(few_lds) + (uint32_t)wave * (NS * Shape::STAGE);
+  const int n_uses = *g.n_uses, n0 = blockIdx.x * 16;
+  if (tid < g.most_uses) uses[tid] = g.uses[tid];
+  if (tid < g.T * g.top) pair_tokens[tid] = g.pair_tokens[tid];
+  for (int i = lane; i < XR * 16; i += 64) sums[wave][i / 16][i % 16] = 0.f;
+  const int blocks = (g.I + kBlock - 1) / kBlock, steps = n_uses * blocks, tail = g.I & (kBlock - 1);
+  __syncthreads();
+  const u32x4 h_desc = descriptor(g.h_terms);
+  uint32_t w_at[2];
+  int chunk[2];
+#pragma unroll
+  for (int p = 0; p < 2; ++p) {
+    const int row = 8 * p + (lane >> 3);
+    chunk[p] = e4m3_chunk(lane, row) * 16;
+    w_at[p] = (uint32_t)(min(row, g.H - 1 - n0) * g.ldw2) + chunk[p];
+  }
+  // the use and block of this wave's step to be fetched next
+  int fs = wave, fu = wave / blocks, fb = wave - fu * blocks, slot_of = 0;
+  auto fetch = [&]() {  // (steps past the last read as zero: every wave has as many loads on their way)
+    const uint32_t to = lds0 + (uint32_t)slot_of * Shape::STAGE;
+    if (++slot_of == NS) slot_of = 0;
+    const int u = min(fu, n_uses - 1);
+    const int e = __builtin_amdgcn_readfirstlane(uses[u].expert), first = __builtin_amdgcn_readfirstlane(uses[u].first),
+              count = __builtin_amdgcn_readfirstlane(uses[u].count);
+    const u32x4 w_desc = descriptor(g.W2 + e * g.w2_stride + n0 * g.ldw2),
+                s_desc = descriptor(g.S2 + e * g.s2_stride + (int64_t)(n0 / kBlock) * g.lds2);
+    const int most = fs >= steps ? 0 : tail && fb == blocks - 1 ? tail : kBlock;
+    const uint32_t at = most ? (uint32_t)fb : 0u;
+#pragma unroll
+    for (int p = 0; p < 2; ++p) fetch_16(to + p * 1024, chunk[p] >= most ? kBeyond : w_at[p], w_desc, at * kBlock);
+#pragma unroll
+    for (int j = 0; j < X_LOADS; ++j) {
+      const int line = 4 * j + (lane >> 4), row = line % XR, k = line / XR;
+      fetch_16(to + 2048 + j * 1024,
+               most && row < count && k < H_TERMS ? (uint32_t)((first + row) * g.h_row + k * 256 + term_chunk(lane, row) * 16) : kBeyond, h_desc,
+               at * (H_TERMS * 256));
+    }
+    fetch_4(to + 2048 + X_LOADS * 1024, most ? 0u : kBeyond, s_desc, at * 4);
+    fs += kDownWaves;
+    for (fb += kDownWaves; fb >= blocks; fb -= blocks) ++fu;
+  };
+  f32x4 acc = f32x4{0.f, 0.f, 0.f, 0.f};
+  const uint32_t off = e4m3_operand_offset(lane);
+  int u = fu, b = fb, slot = 0;
+#pragma unroll
+  for (int k = 0; k < NS - 1; ++k) fetch();
+  for (int s = wave; s < steps; s += kDownWaves) {
+    asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" ::"n"((NS - 2) * Shape::LOADS) : "memory");
+    fetch();
+    uint8_t *const w = few_lds + (wave * NS + slot) * Shape::STAGE;
+    if (++slot == NS) slot = 0;
+    if ((tail & 15) && b == blocks - 1) {
+      if (lane < 16) {
+        u32x4 *const p = reinterpret_cast<u32x4 *>(w + lane * 128 + ((tail >> 4) ^ ((r >> 1) & 7)) * 16);
+        *p = first_bytes(*p, tail & 15);
+      }
+      asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+    }
+    const int first = __builtin_amdgcn_readfirstlane(uses[u].first), count = __builtin_amdgcn_readfirstlane(uses[u].count);
+    const float sc = *reinterpret_cast<const float *>(w + 2048 + X_LOADS * 1024);
+    f32x4 d[1];
+    block_products<1, XR, H_TERMS>(read_operand(w, off), w + 2048, lane, d);
+#pragma unroll
+    for (int j = 0; j < 4; ++j) acc[j] += sc * d[0][j];
+    const int before = u;
+    for (b += kDownWaves; b >= blocks; b -= blocks) ++u;
+    if (u != before || s + kDownWaves >= steps) {  // the use's sums to its tokens (a token is once in a use)
+      if (r < count) *reinterpret_cast<f32x4 *>(&sums[wave][pair_tokens[first + r]][4 * (lane >> 4)]) += acc;
+      acc = f32x4{0.f, 0.f, 0.f, 0.f};
+    }
+  }
+  asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
+  if (tid < g.T * 16 && n0 + r < g.H) {
+    float v = 0.f;
+#pragma unroll
+    for (int k = 0; k < kDownWaves; ++k) v += sums[k][tid >> 4][r];
+    T::store(Y + (tid >> 4) * ldy + n0 + r, v);
+  }
+}
+
 // ---------------------------------------------------------------------------------------------- host
 
 constexpr int64_t round_up(int64_t n, int64_t d) { return (n + d - 1) / d * d; }
@@ -619,6 +760,14 @@ void launch_up(const MoeArgs &g, hipStream_t st) {
                      Shape::LDS, st, g);
 }
 
+template <class T, int XR, int H_TERMS>
+void launch_down_few(const MoeArgs &g, void *Y, int64_t ldy, hipStream_t st) {
+  constexpr int NS = FewShape<XR, H_TERMS, 4>::RING <= 150 * 1024 ? 4 : 3;
+  static_assert(FewShape<XR, H_TERMS, NS>::RING <= 150 * 1024, "a CU's, less what is declared in the kernel");
+  hipLaunchKernelGGL((moe_down_few_kernel<T, XR, H_TERMS, NS>), dim3((unsigned)((g.H + 15) / 16)), dim3(kDownWaves * 64),
+                     (FewShape<XR, H_TERMS, NS>::RING), st, g, static_cast<typename T::Elem *>(Y), ldy);
+}
+
 template <class T, int XR, int TERMS, int H_TERMS>
 void launch_products(const MoeArgs &g, void *Y, int64_t ldy, hipStream_t st) {
   // Four waves: side by side where x is wide and they share it, in pairs otherwise, and all on the same 16 rows where there
@@ -629,6 +778,14 @@ void launch_products(const MoeArgs &g, void *Y, int64_t ldy, hipStream_t st) {
     launch_up<XR, TERMS, H_TERMS, 1, 4>(g, st);
   else
     launch_up<XR, TERMS, H_TERMS, (XR == 32 ? 4 : 2), (XR == 32 ? 1 : 2)>(g, st);
+  if constexpr (XR == 4) {
+    // No sums across workgroups where each has few steps (us, against the other kernel: one token, six of 64 experts of 2048 x
+    // 1024 21.5 and 22.4, two of 16 of 512 x 512 12.5 and 13.7, four of 16 of 2048 x 4096 34.9 and 33.8; four tokens, two of
+    // 16 of 512 x 512 17.6 and 19.1, eight of 32 of 1024 x 256 24.8 and 23.5)
+    const int64_t steps = (int64_t)(g.E < g.T * g.top ? g.E : g.T * g.top) * ((g.I + kBlock - 1) / kBlock);
+    if (g.T == 1 && steps <= 96) return launch_down_few<T, 1, H_TERMS>(g, Y, ldy, st);
+    if (g.T > 1 && steps <= 48) return launch_down_few<T, 4, H_TERMS>(g, Y, ldy, st);
+  }
   constexpr int NS = 3;
   typedef DownShape<XR, H_TERMS, NS> Shape;
   static_assert(Shape::RING + kMostTokens * 512 <= 150 * 1024, "a CU's, less what is declared in the kernel");
@@ -644,7 +801,7 @@ int32_t launch_moe(const MoeArgs &g, const void *X, int64_t ldx, bool wide, cons
   hipLaunchKernelGGL((router_kernel<T, TERMS>), dim3((unsigned)(groups + (pieces + 255) / 256)), dim3(256), 0, st,
                      static_cast<const E *>(X), ldx, (int)wide, static_cast<const E *>(router), ldr, (int)r_wide, g.T, g.H, g.E, g.logits,
                      g.x_terms, groups, g.tickets, g.row_groups);
-  if (g.T > 1) hipLaunchKernelGGL(picks_kernel, dim3(1), dim3(1024), 0, st, g);
+  if (!g.plans) hipLaunchKernelGGL(picks_kernel, dim3(1), dim3(1024), 0, st, g);
   int32_t rc = xorenc_internal_check_launch();
   if (rc != XORENC_OK) return rc;
   constexpr int MOST = pass_of(TERMS > 1);
@@ -715,6 +872,9 @@ extern "C" int32_t xorenc_moe_fp8(const xorenc_moe *L, const void *X, int32_t x_
   g.x_terms = reinterpret_cast<uint16_t *>(ws + p.x);
   g.h_terms = reinterpret_cast<uint16_t *>(ws + p.h);
   g.x_row = p.x_row, g.h_row = p.h_row, g.most_uses = p.most_uses, g.pass = p.pass, g.splits = p.splits, g.row_groups = p.row_groups;
+  // Up to four tokens, up to 1024 workgroups: a launch less for a longer start of each (us: two tokens, four of 16 experts of 1024 x
+  // 1024 22.2 and 23.4; four tokens, six of 64 of 2048 x 1024, 1536 workgroups, 45.0 and 43.9)
+  g.plans = tokens == 1 || (tokens <= 4 && (int64_t)((I + 15) / 16) * p.most_uses <= 1024);
   const bool r_wide = wide_rows(L->router, L->ld_router, x_dtype);
   hipStream_t st = static_cast<hipStream_t>(hip_stream);
   xorenc_internal_begin_call();

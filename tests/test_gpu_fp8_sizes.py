@@ -131,3 +131,27 @@ def test_experts_of_what_is_not_finite(T, renormalise):
         bad = router.clone()
         bad.view(torch.int16)[3, 9] = bits
         assert torch.isnan(xe.moe_fp8(x, bad, W13, S13, W2, S2, 2, renormalise=renormalise)).all()
+
+
+# few steps of the second product and many, few workgroups of the first and many, an expert for all tokens
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("T,H,I,E,n", [(1, 520, 2600, 9, 4), (1, 70, 2500, 12, 5), (2, 300, 1000, 6, 3), (2, 64, 1500, 8, 2), (3, 1000, 700, 8, 2),
+                                       (4, 130, 129, 1, 1), (4, 2050, 300, 16, 4), (4, 96, 2000, 40, 10), (3, 200, 16, 256, 16)])
+def test_experts_of_up_to_four_tokens(T, H, I, E, n, dtype):
+    check_moe(T, H, I, E, n, dtype)
+    check_moe(T, H, I, E, n, dtype, renormalise=False)
+
+
+def test_what_is_not_finite_stays_with_its_token():
+    g = gen(3)
+    T, H, I, E = 3, 136, 40, 6
+    x, router = normal(g, T, H, dtype=torch.bfloat16).to(DEV), normal(g, E, H, dtype=torch.bfloat16).to(DEV)
+    W13, S13 = random_8bit(g, 2 * I, H, 128, lead=(E,))
+    W2, S2 = random_8bit(g, H, I, 128, lead=(E,))
+    clean = xe.moe_fp8(x, router, W13, S13, W2, S2, 3)
+    for t in range(T):
+        bad = x.clone()
+        bad[t, 5] = float("nan")
+        Y = xe.moe_fp8(bad, router, W13, S13, W2, S2, 3)
+        keep = torch.arange(T, device=DEV) != t
+        assert torch.equal(Y[keep], clean[keep]) and torch.isnan(Y[~keep]).all()
