@@ -45,51 +45,89 @@ __device__ inline float silu(float x) { return x * __builtin_amdgcn_rcpf(1.f + _
 __device__ inline uint16_t to_bf16(float v) { return __builtin_bit_cast(uint16_t, (__bf16)v); }
 __device__ inline uint32_t to_bf16x2(float a, float b) { return (uint32_t)to_bf16(a) | ((uint32_t)to_bf16(b) << 16); }
 
+// Rows may start on any element: 16 bytes are loaded and stored wherever they start.
+typedef f32x4 f32x4_anywhere __attribute__((aligned(4)));
+typedef u32x4 u32x4_anywhere __attribute__((aligned(2)));
+
 struct F32 {
   typedef float Elem;
-  static __device__ inline float load(const Elem *p) { return *p; }
-  static __device__ inline void store(Elem *p, float v) { *p = v; }
-  static __device__ inline void load8(const Elem *p, float *v) {  // 16-byte aligned
-    const f32x4 a = *reinterpret_cast<const f32x4 *>(p), b = *reinterpret_cast<const f32x4 *>(p + 4);
-#pragma unroll
-    for (int i = 0; i < 4; ++i) v[i] = a[i], v[4 + i] = b[i];
+  struct Raw {  // eight elements
+    f32x4 a, b;
+  };
+  template <bool STREAM>
+  static __device__ inline Raw load8(const Elem *p) {
+    const f32x4_anywhere *const q = reinterpret_cast<const f32x4_anywhere *>(p);
+    if constexpr (STREAM) return {__builtin_nontemporal_load(q), __builtin_nontemporal_load(q + 1)};
+    return {q[0], q[1]};
   }
+  static __device__ inline Raw first_of(const Elem *p, int n) {  // those from the n-th on are zero
+    Raw r;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) r.a[i] = i < n ? p[i] : 0.f, r.b[i] = 4 + i < n ? p[4 + i] : 0.f;
+    return r;
+  }
+  static __device__ inline void widen(const Raw &r, float *v) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) v[i] = r.a[i], v[4 + i] = r.b[i];
+  }
+  static __device__ inline void store(Elem *p, float v) { *p = v; }
   static __device__ inline void store8(Elem *p, const float *v) {
-    *reinterpret_cast<f32x4 *>(p) = f32x4{v[0], v[1], v[2], v[3]};
-    *reinterpret_cast<f32x4 *>(p + 4) = f32x4{v[4], v[5], v[6], v[7]};
+    *reinterpret_cast<f32x4_anywhere *>(p) = f32x4{v[0], v[1], v[2], v[3]};
+    *reinterpret_cast<f32x4_anywhere *>(p + 4) = f32x4{v[4], v[5], v[6], v[7]};
   }
 };
 
 struct BF16 {
   typedef uint16_t Elem;
-  static __device__ inline float load(const Elem *p) { return __uint_as_float((uint32_t)*p << 16); }
-  static __device__ inline void store(Elem *p, float v) { *p = to_bf16(v); }
-  static __device__ inline void load8(const Elem *p, float *v) {
-    const u32x4 a = *reinterpret_cast<const u32x4 *>(p);
-#pragma unroll
-    for (int i = 0; i < 4; ++i) v[2 * i] = bf16_lo(a[i]), v[2 * i + 1] = bf16_hi(a[i]);
+  typedef u32x4 Raw;
+  template <bool STREAM>
+  static __device__ inline Raw load8(const Elem *p) {
+    const u32x4_anywhere *const q = reinterpret_cast<const u32x4_anywhere *>(p);
+    if constexpr (STREAM) return __builtin_nontemporal_load(q);
+    return *q;
   }
+  static __device__ inline Raw first_of(const Elem *p, int n) {
+    Raw r;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) r[i] = (2 * i < n ? (uint32_t)p[2 * i] : 0u) | (2 * i + 1 < n ? (uint32_t)p[2 * i + 1] << 16 : 0u);
+    return r;
+  }
+  static __device__ inline void widen(const Raw &r, float *v) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) v[2 * i] = bf16_lo(r[i]), v[2 * i + 1] = bf16_hi(r[i]);
+  }
+  static __device__ inline void store(Elem *p, float v) { *p = to_bf16(v); }
   static __device__ inline void store8(Elem *p, const float *v) {
-    *reinterpret_cast<u32x4 *>(p) =
+    *reinterpret_cast<u32x4_anywhere *>(p) =
         u32x4{to_bf16x2(v[0], v[1]), to_bf16x2(v[2], v[3]), to_bf16x2(v[4], v[5]), to_bf16x2(v[6], v[7])};
   }
 };
 
-// Up to eight values of a row from column c on; columns from `cols` on are zero.  `wide`: the row's pieces of eight are
-// 16-byte aligned.
+// Eight values of a row from column c on; columns from `cols` on are zero.  The load comes first, without a branch (so that
+// several are on their way together), and takes the row's last eight elements where fewer are left behind c; the values
+// come from it.  STREAM: they are not kept in caches.
+template <class T, bool STREAM = false>
+__device__ inline typename T::Raw load_piece(const typename T::Elem *row, int c, int cols) {
+  return cols >= 8 ? T::template load8<STREAM>(row + min(c, cols - 8)) : T::first_of(row, c ? 0 : cols);
+}
+
 template <class T>
-__device__ inline void load_piece(const typename T::Elem *row, int c, int cols, bool wide, float *v) {
-  if (wide && c + 8 <= cols) {
-    T::load8(row + c, v);
-  } else {
+__device__ inline void piece_of(const typename T::Raw &raw, int c, int cols, float *v) {
+  T::widen(raw, v);
+  const int off = c + 8 - cols;  // elements before column c
+  if (off > 0 && cols >= 8) {
 #pragma unroll
-    for (int i = 0; i < 8; ++i) v[i] = c + i < cols ? T::load(row + c + i) : 0.f;
+    for (int d = 1; d < 8; d *= 2)
+#pragma unroll
+      for (int i = 0; i < 8; ++i) v[i] = off & d ? (i + d < 8 ? v[i + d] : 0.f) : v[i];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) v[i] = off >= 8 ? 0.f : v[i];
   }
 }
 
 template <class T>
-__device__ inline void store_piece(typename T::Elem *row, int c, int cols, bool wide, const float *v) {
-  if (wide && c + 8 <= cols) {
+__device__ inline void store_piece(typename T::Elem *row, int c, int cols, const float *v) {
+  if (c + 8 <= cols) {
     T::store8(row + c, v);
   } else {
 #pragma unroll
@@ -211,7 +249,6 @@ inline bool known_dtype(int32_t t) { return t == XORENC_X_F32 || t == XORENC_X_B
 inline int dtype_bytes(int32_t t) { return t == XORENC_X_F32 ? 4 : 2; }
 inline bool aligned_to(const void *p, size_t n) { return ((uintptr_t)p & (n - 1)) == 0; }
 // pieces of eight values of every row on 16-byte boundaries
-inline bool wide_rows(const void *p, int64_t ld, int32_t t) { return aligned_to(p, 16) && ld % (16 / dtype_bytes(t)) == 0; }
 
 }  // namespace xorenc_fp8_detail
 

@@ -7,21 +7,21 @@ namespace xorenc_fp8_detail {
 namespace {
 
 template <int TN, int TM, int WN, int WM, bool EXACT>
-void launch_tile(const MatmulArgs &g, bool wide, hipStream_t st) {
+void launch_tile(const MatmulArgs &g, hipStream_t st) {
   typedef TileShape<TN, TM, WN, WM, EXACT> Shape;
   const int n_tiles = (g.N + Shape::BN - 1) / Shape::BN, m_tiles = (g.M + Shape::BM - 1) / Shape::BM;
   const int per_xcd = (n_tiles * m_tiles + 7) / 8;
   hipLaunchKernelGGL((matmul_tile_kernel<TN, TM, WN, WM, EXACT>), dim3((unsigned)(per_xcd * 8)), dim3(Shape::WAVES * 64), Shape::LDS, st, g,
-                     (int)wide, n_tiles, m_tiles, per_xcd);
+                     n_tiles, m_tiles, per_xcd);
 }
 
 template <int TN, int TM, int WN, int WM, int KG, int NS, bool EXACT>
-void launch_ring(const MatmulArgs &g, bool wide, hipStream_t st) {
+void launch_ring(const MatmulArgs &g, hipStream_t st) {
   typedef RingShape<TN, TM, WN, WM, KG, NS> Shape;
   const int n_tiles = (g.N + Shape::BN - 1) / Shape::BN, m_tiles = (g.M + Shape::BM - 1) / Shape::BM;
   const int per_xcd = (n_tiles * m_tiles + 7) / 8;
   hipLaunchKernelGGL((matmul_ring_kernel<TN, TM, WN, WM, KG, NS, EXACT>), dim3((unsigned)(per_xcd * 8)), dim3(Shape::WAVES * 64), Shape::LDS, st, g,
-                     (int)wide, n_tiles, m_tiles, per_xcd);
+                     n_tiles, m_tiles, per_xcd);
 }
 
 // The kernels, and what they take: `start` + rounds * (`tile` + steps * (`step` + `load` * share of the chip in use)), in us, with
@@ -80,19 +80,19 @@ int cheapest(int64_t M, int64_t N, int64_t blocks, bool exact) {
 }
 
 template <bool EXACT>
-int32_t dispatch_matmul(const MatmulArgs &g, bool wide, hipStream_t st) {
+int32_t dispatch_matmul(const MatmulArgs &g, hipStream_t st) {
   switch (cheapest(g.M, g.N, g.blocks, EXACT)) {
     case 0:
-      if constexpr (!EXACT) launch_tile<8, 4, 2, 4, EXACT>(g, wide, st);
+      if constexpr (!EXACT) launch_tile<8, 4, 2, 4, EXACT>(g, st);
       break;
-    case 1: launch_tile<4, 4, 2, 2, EXACT>(g, wide, st); break;
-    case 2: launch_tile<4, 2, 2, 2, EXACT>(g, wide, st); break;
-    case 3: launch_ring<2, 2, 2, 2, 2, 2, EXACT>(g, wide, st); break;
-    case 4: launch_ring<2, 2, 2, 2, 1, 2, EXACT>(g, wide, st); break;
-    case 8: launch_ring<2, 2, 2, 2, 2, 3, EXACT>(g, wide, st); break;
-    case 5: launch_ring<1, 1, 1, 1, 8, 2, EXACT>(g, wide, st); break;
-    case 6: launch_ring<2, 2, 1, 1, 8, 2, EXACT>(g, wide, st); break;
-    case 7: launch_ring<2, 2, 2, 1, 4, 3, EXACT>(g, wide, st); break;
+    case 1: launch_tile<4, 4, 2, 2, EXACT>(g, st); break;
+    case 2: launch_tile<4, 2, 2, 2, EXACT>(g, st); break;
+    case 3: launch_ring<2, 2, 2, 2, 2, 2, EXACT>(g, st); break;
+    case 4: launch_ring<2, 2, 2, 2, 1, 2, EXACT>(g, st); break;
+    case 8: launch_ring<2, 2, 2, 2, 2, 3, EXACT>(g, st); break;
+    case 5: launch_ring<1, 1, 1, 1, 8, 2, EXACT>(g, st); break;
+    case 6: launch_ring<2, 2, 1, 1, 8, 2, EXACT>(g, st); break;
+    case 7: launch_ring<2, 2, 2, 1, 4, 3, EXACT>(g, st); break;
     default: return XORENC_ELIMIT;
   }
   return xorenc_internal_check_launch();
@@ -120,8 +120,7 @@ extern "C" int32_t xorenc_matmul_fp8(const uint8_t *A, int64_t lda, const float 
       256 * row_step + sa_blk * blocks >= (1 << 29))
     return XORENC_ELIMIT;
   const MatmulArgs g = {A, W, SA, SW, Y, lda, ldw, row_step, sa_blk, ldsw, ldy, M, N, K, blocks};
-  const bool wide = wide_rows(Y, ldy, y_dtype);
   xorenc_internal_begin_call();
   hipStream_t st = static_cast<hipStream_t>(hip_stream);
-  return y_dtype == XORENC_X_F32 ? dispatch_matmul<true>(g, wide, st) : dispatch_matmul<false>(g, wide, st);
+  return y_dtype == XORENC_X_F32 ? dispatch_matmul<true>(g, st) : dispatch_matmul<false>(g, st);
 }

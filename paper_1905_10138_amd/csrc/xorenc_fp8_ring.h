@@ -27,7 +27,7 @@ struct RingShape {
 };
 
 template <int TN, int TM, int WN, int WM, int KG, int NS, bool EXACT>
-__global__ __launch_bounds__(WN *WM *KG * 64) void matmul_ring_kernel(MatmulArgs g, int wide, int n_tiles, int m_tiles, int per_xcd) {
+__global__ __launch_bounds__(WN *WM *KG * 64) void matmul_ring_kernel(MatmulArgs g, int n_tiles, int m_tiles, int per_xcd) {
   typedef RingShape<TN, TM, WN, WM, KG, NS> Shape;
   constexpr int BN = Shape::BN, BM = Shape::BM, PER = Shape::PER, BLOCK = Shape::BLOCK, STAGE = Shape::STAGE;
   extern __shared__ __attribute__((aligned(1024))) uint8_t ring_lds[];
@@ -183,7 +183,7 @@ __global__ __launch_bounds__(WN *WM *KG * 64) void matmul_ring_kernel(MatmulArgs
     __syncthreads();
     if (kg > 0) return;
   }
-  store_tile<TN, TM, EXACT>(g, acc, ring_lds + in_group * (16 * TM * 16 * TN * 4), m0 + wm * (16 * TM), n0 + wn * (16 * TN), lane, wide);
+  store_tile<TN, TM, EXACT>(g, acc, ring_lds + in_group * (16 * TM * 16 * TN * 4), m0 + wm * (16 * TM), n0 + wn * (16 * TN), lane);
 }
 
 }  // namespace xorenc_fp8_detail

@@ -2,17 +2,24 @@
 //
 // All of them read every value once, keep it in registers, and write it in 8 bits; the bytes moved bound them.  Sixteen
 // lanes hold a block of 128 columns, eight values each (one 16-byte load of bf16, two of fp32, one 8-byte store of
-// e4m3), so that a block's largest magnitude is one maximum over a DPP row and needs no LDS.
+// e4m3), so that a block's largest magnitude is one maximum over a DPP row and needs no LDS.  Loads start on any element
+// (8192 x 1501 with a residual 22 us; value by value, where rows are not on 16-byte boundaries, 52).
+//
+// us and GB/s read and written (a copy of 1 GB: 5160): rows of 33 x 9216 fp32 5 (the call's time on the host), of 8192 x 5001 bf16
+// 26, 4840; squares of 16384 x 4096 bf16 35, 5660; the gates of 8192 x 9216 bf16 65, 5800; the norm of 8192 x 6000 bf16 with a
+// residual 66, 5250.
+#include <type_traits>
+
 #include "xorenc_fp8.h"
 
 namespace xorenc_fp8_detail {
 namespace {
 
 // Y = x (or silu(x) * up) by blocks of one row x 128.  Sixteen lanes per block, blocks numbered row by row.
-template <class T, bool GATED>
+template <class T, bool GATED, bool STREAM>
 __global__ __launch_bounds__(256) void quant_rows_kernel(const typename T::Elem *__restrict__ X,
                                                          const typename T::Elem *__restrict__ up, int64_t ldx, int64_t blocks,
-                                                         int cols, int per_row, int wide, uint8_t *__restrict__ Q, int64_t ldq,
+                                                         int cols, int per_row, uint8_t *__restrict__ Q, int64_t ldq,
                                                          float *__restrict__ S, int64_t s_row, int64_t s_blk) {
   const int64_t b = (int64_t)blockIdx.x * 16 + (threadIdx.x >> 4);
   if (b >= blocks) return;
@@ -20,12 +27,16 @@ __global__ __launch_bounds__(256) void quant_rows_kernel(const typename T::Elem 
   const int kb = (int)(b - r * per_row), l = threadIdx.x & 15;
   const int c = kb * kBlock + l * 8;
   float v[8];
-  load_piece<T>(X + r * ldx, c, cols, wide, v);
+  const typename T::Raw x = load_piece<T, STREAM>(X + r * ldx, c, cols);
   if constexpr (GATED) {
     float u[8];
-    load_piece<T>(up + r * ldx, c, cols, wide, u);
+    const typename T::Raw y = load_piece<T, STREAM>(up + r * ldx, c, cols);
+    piece_of<T>(x, c, cols, v);
+    piece_of<T>(y, c, cols, u);
 #pragma unroll
     for (int i = 0; i < 8; ++i) v[i] = silu(v[i]) * u[i];
+  } else {
+    piece_of<T>(x, c, cols, v);
   }
   uint32_t a = 0;
 #pragma unroll
@@ -35,10 +46,11 @@ __global__ __launch_bounds__(256) void quant_rows_kernel(const typename T::Elem 
   if (l == 0) S[r * s_row + kb * s_blk] = s;
 }
 
-// Blocks of 128 x 128: a workgroup holds one, 16 rows a pass.
-template <class T>
+// Blocks of 128 x 128: a workgroup holds one, 16 rows a pass, as it was read: all eight loads of a lane are on their way together
+// (16384 x 4096 bf16 41.7 -> 35.3 us), and the values are made from them twice.
+template <class T, bool STREAM>
 __global__ __launch_bounds__(256) void quant_square_kernel(const typename T::Elem *__restrict__ X, int64_t ldx, int64_t x_mat,
-                                                           int rows, int cols, int per_row, int wide, uint8_t *__restrict__ Q,
+                                                           int rows, int cols, int per_row, uint8_t *__restrict__ Q,
                                                            int64_t ldq, int64_t q_mat, float *__restrict__ S, int64_t s_row,
                                                            int64_t s_blk, int64_t s_mat) {
   __shared__ uint32_t wave_max[4];
@@ -47,22 +59,17 @@ __global__ __launch_bounds__(256) void quant_square_kernel(const typename T::Ele
   Q += blockIdx.y * q_mat;
   const int l = threadIdx.x & 15, c = kb * kBlock + l * 8;
   const int r0 = rb * kBlock + (threadIdx.x >> 4);
-  float v[8][8];
+  typename T::Raw x[8];  // (rows past the last: the last one again)
+  float v[8];
   uint32_t a = 0;
 #pragma unroll
+  for (int p = 0; p < 8; ++p) x[p] = load_piece<T, STREAM>(X + min(r0 + 16 * p, rows - 1) * ldx, c, cols);
+#pragma unroll
   for (int p = 0; p < 8; ++p) {
-    const int r = r0 + 16 * p;
-    if (r < rows) {
-      load_piece<T>(X + r * ldx, c, cols, wide, v[p]);
-    } else {
+    piece_of<T>(x[p], c, cols, v);
 #pragma unroll
-      for (int i = 0; i < 8; ++i) v[p][i] = 0.f;
-    }
+    for (int i = 0; i < 8; ++i) a = max(a, magnitude_bits(v[i]));
   }
-#pragma unroll
-  for (int p = 0; p < 8; ++p)
-#pragma unroll
-    for (int i = 0; i < 8; ++i) a = max(a, magnitude_bits(v[p][i]));
   a = max_of_16_lanes(a);
   a = max(a, (uint32_t)__shfl_xor((int)a, 16));
   a = max(a, (uint32_t)__shfl_xor((int)a, 32));
@@ -73,33 +80,48 @@ __global__ __launch_bounds__(256) void quant_square_kernel(const typename T::Ele
 #pragma unroll
   for (int p = 0; p < 8; ++p) {
     const int r = r0 + 16 * p;
-    if (r < rows) store_e4m3_piece(Q + r * ldq, c, cols, v[p], inv);
+    piece_of<T>(x[p], c, cols, v);
+    if (r < rows) store_e4m3_piece(Q + r * ldq, c, cols, v, inv);
   }
   if (threadIdx.x == 0) S[blockIdx.y * s_mat + rb * s_row + kb * s_blk] = s;
 }
 
-// One workgroup per row: s = x + residual, y = s / sqrt(mean s^2 + eps) * w.  PASSES > 0: the row's sums stay in registers, eight
-// per thread and pass.  PASSES = 0, rows that do not fit: x and the residual are read once more for the second half
-// (from the caches; a `total` that is stored over one of them is not read back, it may be rounded).
-template <class T, int THREADS, int PASSES>
-__global__ __launch_bounds__(THREADS) void rmsnorm_kernel(const typename T::Elem *X, int64_t ldx,
+// THREADS per row, ROWS rows a workgroup (more than one only where a row is a wave's): s = x + residual, y = s / sqrt(mean s^2 +
+// eps) * w.  PASSES > 0: the row's sums stay in registers, eight per thread and pass.  PASSES = 0, rows that do not fit: x and the
+// residual are read once more for the second half (from the caches; a `total` that is stored over one of them is not read
+// back, it may be rounded).  Up to 1536 columns a wave holds a row: no barrier, and a quarter of the workgroups (8192 x 600
+// 15.4 -> 12.0 us, 8192 x 1200 without a residual 14.9 -> 11.0; 8192 x 2000 a wave a row 32.8, four 29.4).  Beyond, 256 threads: several
+// rows a CU hide each other's loads (8192 x 9216 without a residual 54 us; 1024 threads 76).
+template <class T, int THREADS, int PASSES, int ROWS, bool STREAM>
+__global__ __launch_bounds__(THREADS *ROWS) void rmsnorm_kernel(const typename T::Elem *X, int64_t ldx,
                                                           const typename T::Elem *R, int64_t ldr, const void *__restrict__ w,
-                                                          int w_bf16, int wide, int w_wide, int cols, int per_row, float eps,
+                                                          int w_bf16, int rows, int cols, float eps,
                                                           typename T::Elem *total, int64_t ldt, typename T::Elem *Y, int64_t y_row,
-                                                          int64_t y_col, int y_wide, uint8_t *__restrict__ Q, int64_t ldq,
+                                                          int64_t y_col, uint8_t *__restrict__ Q, int64_t ldq,
                                                           float *__restrict__ S, int64_t s_row, int64_t s_blk) {
+  static_assert(ROWS == 1 || THREADS == 64, "a barrier is for the row's threads");
   constexpr int STEP = THREADS * 8, WAVES = THREADS / 64;
   __shared__ float wave_sum[WAVES];
-  const int64_t r = blockIdx.x;
-  const int t = threadIdx.x;
+  const int64_t r = (int64_t)blockIdx.x * ROWS + threadIdx.x / THREADS;
+  const int t = threadIdx.x % THREADS;
+  if (ROWS > 1 && r >= rows) return;
   X += r * ldx;
   if (R) R += r * ldr;
   if (total) total += r * ldt;
-  auto sums = [&](int c, float *s) {
-    load_piece<T>(X, c, cols, wide, s);
+  struct Pair {
+    typename T::Raw x, r;
+  };
+  auto load = [&](int c) {
+    Pair p;
+    p.x = load_piece<T, STREAM>(X, c, cols);
+    if (R) p.r = load_piece<T, STREAM>(R, c, cols);
+    return p;
+  };
+  auto sums = [&](const Pair &p, int c, float *s) {
+    piece_of<T>(p.x, c, cols, s);
     if (R) {
       float u[8];
-      load_piece<T>(R, c, cols, wide, u);
+      piece_of<T>(p.r, c, cols, u);
 #pragma unroll
       for (int i = 0; i < 8; ++i) s[i] += u[i];
     }
@@ -108,19 +130,25 @@ __global__ __launch_bounds__(THREADS) void rmsnorm_kernel(const typename T::Elem
   float s[HELD][8];
   float sq = 0.f;
   if constexpr (PASSES > 0) {
+    Pair held[PASSES];
 #pragma unroll
-    for (int p = 0; p < PASSES; ++p) sums(p * STEP + t * 8, s[p]);
+    for (int p = 0; p < PASSES; ++p) held[p] = load(p * STEP + t * 8);
 #pragma unroll
     for (int p = 0; p < PASSES; ++p) {
+      sums(held[p], p * STEP + t * 8, s[p]);
+      float of_pass = 0.f;
 #pragma unroll
-      for (int i = 0; i < 8; ++i) sq += s[p][i] * s[p][i];
-      if (total) store_piece<T>(total, p * STEP + t * 8, cols, wide, s[p]);
+      for (int i = 0; i < 8; ++i) of_pass += s[p][i] * s[p][i];
+      sq += of_pass;
+      if (total) store_piece<T>(total, p * STEP + t * 8, cols, s[p]);
     }
   } else {
     for (int c = t * 8; c < cols; c += STEP) {
-      sums(c, s[0]);
+      sums(load(c), c, s[0]);
+      float of_pass = 0.f;
 #pragma unroll
-      for (int i = 0; i < 8; ++i) sq += s[0][i] * s[0][i];
+      for (int i = 0; i < 8; ++i) of_pass += s[0][i] * s[0][i];
+      sq += of_pass;
     }
   }
 #pragma unroll
@@ -136,9 +164,9 @@ __global__ __launch_bounds__(THREADS) void rmsnorm_kernel(const typename T::Elem
   auto finish = [&](int c, float *v) {
     float g[8];
     if (w_bf16)
-      load_piece<BF16>(static_cast<const uint16_t *>(w), c, cols, w_wide, g);
+      piece_of<BF16>(load_piece<BF16>(static_cast<const uint16_t *>(w), c, cols), c, cols, g);
     else
-      load_piece<F32>(static_cast<const float *>(w), c, cols, w_wide, g);
+      piece_of<F32>(load_piece<F32>(static_cast<const float *>(w), c, cols), c, cols, g);
     uint32_t a = 0;
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
@@ -151,7 +179,7 @@ __global__ __launch_bounds__(THREADS) void rmsnorm_kernel(const typename T::Elem
     if ((t & 15) == 0) S[r * s_row + (int64_t)(c / kBlock) * s_blk] = sc;
     if (Y) {
       if (y_col == 1) {
-        store_piece<T>(Y + r * y_row, c, cols, y_wide, v);
+        store_piece<T>(Y + r * y_row, c, cols, v);
       } else {
 #pragma unroll
         for (int i = 0; i < 8; ++i)
@@ -166,23 +194,38 @@ __global__ __launch_bounds__(THREADS) void rmsnorm_kernel(const typename T::Elem
   } else {
     for (int c0 = 0; c0 < cols; c0 += STEP) {  // uniform: whole rows of 16 lanes take part in a block's maximum
       const int c = c0 + t * 8;
-      sums(c, s[0]);
-      if (total) store_piece<T>(total, c, cols, wide, s[0]);
+      sums(load(c), c, s[0]);
+      if (total) store_piece<T>(total, c, cols, s[0]);
       finish(c, s[0]);
     }
   }
 }
 
-template <class T, bool GATED>
-int32_t launch_rows(const void *X, const void *up, int64_t ldx, int64_t rows, int32_t cols, bool wide, uint8_t *Q, int64_t ldq,
+template <class T, bool GATED, bool STREAM>
+int32_t launch_rows(const void *X, const void *up, int64_t ldx, int64_t rows, int32_t cols, uint8_t *Q, int64_t ldq,
                     float *S, int64_t s_row, int64_t s_blk, hipStream_t st) {
   const int per_row = (cols + kBlock - 1) / kBlock;
   const int64_t blocks = rows * per_row;
-  hipLaunchKernelGGL((quant_rows_kernel<T, GATED>), dim3((unsigned)((blocks + 15) / 16)), dim3(256), 0, st,
+  hipLaunchKernelGGL((quant_rows_kernel<T, GATED, STREAM>), dim3((unsigned)((blocks + 15) / 16)), dim3(256), 0, st,
                      static_cast<const typename T::Elem *>(X), static_cast<const typename T::Elem *>(up), ldx, blocks, cols,
-                     per_row, (int)wide, Q, ldq, S, s_row, s_blk);
+                     per_row, Q, ldq, S, s_row, s_blk);
   return xorenc_internal_check_launch();
 }
+
+// Calls that move more than the memory-side cache holds (256 MB) would find nothing there when they run again, and read past it:
+// 8192 x 6000 with a residual 65 us and, with plain loads, 71; the gates of 8192 x 9216 65 and 69; 16384 x 9000 to squares 99
+// and 122.  Below, such loads cost (8192 x 4096 42.7 and 42.0, 2048 x 6000 21.3 and 17.3), and where two of them share a line: rows of
+// fp32, of which a lane takes 32 bytes (8192 x 9216 with a residual 202 and 185; a square's other rows hide it, 162 and 181).
+inline bool streams(int64_t values, int64_t bytes) { return values > ((int64_t)256 << 20) / bytes; }
+
+// f(type, whether to stream)
+template <class F>
+int32_t for_type(int32_t x_dtype, bool stream, F f) {
+  if (x_dtype == XORENC_X_F32) return stream ? f(F32(), std::true_type()) : f(F32(), std::false_type());
+  return stream ? f(BF16(), std::true_type()) : f(BF16(), std::false_type());
+}
+template <class T, bool STREAM>
+constexpr bool kStreamsRows = STREAM && sizeof(typename T::Elem) == 2;
 
 constexpr int64_t kMostBlocks = ((int64_t)1 << 28) - 16;  // a launch has fewer than 2^32 threads
 
@@ -216,32 +259,29 @@ extern "C" int32_t xorenc_quant_fp8(const void *X, int32_t x_dtype, int64_t ldx,
   if (!aligned_to(X, esz) || (matrices > 1 && q_stride % 16)) return XORENC_EALIGN;
   hipStream_t st = static_cast<hipStream_t>(hip_stream);
   const int per_row = (cols + kBlock - 1) / kBlock;
-  const bool wide = wide_rows(X, ldx, x_dtype) && (matrices == 1 || x_stride * esz % 16 == 0);
   xorenc_internal_begin_call();
   if (block_rows == 1) {
     for (int32_t i = 0; i < matrices; ++i) {
       const void *x = static_cast<const char *>(X) + i * x_stride * esz;
       uint8_t *q = Q + i * q_stride;
       float *s = S + i * s_stride;
-      const int32_t rl = x_dtype == XORENC_X_F32 ? launch_rows<F32, false>(x, nullptr, ldx, rows, cols, wide, q, ldq, s, s_row, s_blk, st)
-                                                 : launch_rows<BF16, false>(x, nullptr, ldx, rows, cols, wide, q, ldq, s, s_row, s_blk, st);
+      const int32_t rl = x_dtype == XORENC_X_F32 ? launch_rows<F32, false, false>(x, nullptr, ldx, rows, cols, q, ldq, s, s_row, s_blk, st)
+                                                 : launch_rows<BF16, false, false>(x, nullptr, ldx, rows, cols, q, ldq, s, s_row, s_blk, st);
       if (rl != XORENC_OK) return rl;
     }
     return XORENC_OK;
   }
   const int64_t squares = (rows + kBlock - 1) / kBlock * per_row;
   if (rows > (1 << 30) || squares >= (1 << 24)) return XORENC_ELIMIT;
-  for (int32_t at = 0; at < matrices; at += 65535) {  // the grid's second size is limited
-    const dim3 grid((unsigned)squares, (unsigned)min(matrices - at, 65535));
-    if (x_dtype == XORENC_X_F32)
-      hipLaunchKernelGGL((quant_square_kernel<F32>), grid, dim3(256), 0, st, static_cast<const float *>(X) + at * x_stride, ldx,
-                         x_stride, (int)rows, cols, per_row, (int)wide, Q + at * q_stride, ldq, q_stride, S + at * s_stride, s_row,
-                         s_blk, s_stride);
-    else
-      hipLaunchKernelGGL((quant_square_kernel<BF16>), grid, dim3(256), 0, st, static_cast<const uint16_t *>(X) + at * x_stride, ldx,
-                         x_stride, (int)rows, cols, per_row, (int)wide, Q + at * q_stride, ldq, q_stride, S + at * s_stride, s_row,
-                         s_blk, s_stride);
-    const int32_t rl = xorenc_internal_check_launch();
+  for (int64_t at = 0; at < matrices; at += 65535) {  // the grid's second size is limited
+    const dim3 grid((unsigned)squares, (unsigned)min(matrices - at, (int64_t)65535));
+    const int32_t rl = for_type(x_dtype, streams(rows * cols, (int64_t)(esz + 1) * matrices), [&](auto type, auto stream) {
+      typedef typename decltype(type)::Elem E;
+      hipLaunchKernelGGL((quant_square_kernel<decltype(type), decltype(stream)::value>), grid, dim3(256), 0, st,
+                         static_cast<const E *>(X) + at * x_stride, ldx, x_stride, (int)rows, cols, per_row, Q + at * q_stride, ldq, q_stride,
+                         S + at * s_stride, s_row, s_blk, s_stride);
+      return xorenc_internal_check_launch();
+    });
     if (rl != XORENC_OK) return rl;
   }
   return XORENC_OK;
@@ -258,38 +298,45 @@ extern "C" int32_t xorenc_silu_mul_fp8(const void *gate, const void *up, int32_t
   const int esz = dtype_bytes(x_dtype);
   if (!aligned_to(gate, esz) || !aligned_to(up, esz)) return XORENC_EALIGN;
   hipStream_t st = static_cast<hipStream_t>(hip_stream);
-  const bool wide = wide_rows(gate, ldx, x_dtype) && wide_rows(up, ldx, x_dtype);
   xorenc_internal_begin_call();
-  return x_dtype == XORENC_X_F32 ? launch_rows<F32, true>(gate, up, ldx, rows, cols, wide, Q, ldq, S, s_row, s_blk, st)
-                                 : launch_rows<BF16, true>(gate, up, ldx, rows, cols, wide, Q, ldq, S, s_row, s_blk, st);
+  return for_type(x_dtype, streams(rows * cols, 2 * esz + 1), [&](auto type, auto stream) {
+    return launch_rows<decltype(type), true, kStreamsRows<decltype(type), decltype(stream)::value>>(gate, up, ldx, rows, cols, Q, ldq, S, s_row, s_blk, st);
+  });
 }
 
 namespace xorenc_fp8_detail {
 namespace {
-template <class T>
-int32_t launch_rmsnorm(const void *X, int64_t ldx, const void *R, int64_t ldr, const void *w, int w_bf16, bool wide, bool w_wide,
+template <class T, bool STREAM>
+int32_t launch_rmsnorm(const void *X, int64_t ldx, const void *R, int64_t ldr, const void *w, int w_bf16,
                        int64_t rows, int32_t cols, float eps, void *total, int64_t ldt, void *Y, int64_t y_row, int64_t y_col,
-                       bool y_wide, uint8_t *Q, int64_t ldq, float *S, int64_t s_row, int64_t s_blk, hipStream_t st) {
+                       uint8_t *Q, int64_t ldq, float *S, int64_t s_row, int64_t s_blk, hipStream_t st) {
   typedef typename T::Elem E;
-  const int per_row = (cols + kBlock - 1) / kBlock;
-#define XORENC_RMSNORM(THREADS, PASSES)                                                                                     \
-  hipLaunchKernelGGL((rmsnorm_kernel<T, THREADS, PASSES>), dim3((unsigned)rows), dim3(THREADS), 0, st,                      \
-                     static_cast<const E *>(X), ldx, static_cast<const E *>(R), ldr, w, w_bf16, (int)wide, (int)w_wide, cols, \
-                     per_row, eps, static_cast<E *>(total), ldt, static_cast<E *>(Y), y_row, y_col, (int)y_wide, Q, ldq, S, s_row, s_blk)
+#define XORENC_RMSNORM(THREADS, PASSES, ROWS)                                                                                     \
+  hipLaunchKernelGGL((rmsnorm_kernel<T, THREADS, PASSES, ROWS, (STREAM && PASSES > 0)>), dim3((unsigned)((rows + ROWS - 1) / ROWS)), dim3(THREADS * ROWS), 0, st, \
+                     static_cast<const E *>(X), ldx, static_cast<const E *>(R), ldr, w, w_bf16, (int)rows, cols, \
+                     eps, static_cast<E *>(total), ldt, static_cast<E *>(Y), y_row, y_col, Q, ldq, S, s_row, s_blk)
   if (cols <= 512)
-    XORENC_RMSNORM(64, 1);
+    XORENC_RMSNORM(64, 1, 4);
+  else if (cols <= 1024)
+    XORENC_RMSNORM(64, 2, 4);
+  else if (cols <= 1536)
+    XORENC_RMSNORM(64, 3, 4);
   else if (cols <= 2048)
-    XORENC_RMSNORM(256, 1);
+    XORENC_RMSNORM(256, 1, 1);
   else if (cols <= 4096)
-    XORENC_RMSNORM(256, 2);
+    XORENC_RMSNORM(256, 2, 1);
   else if (cols <= 6144)
-    XORENC_RMSNORM(256, 3);
+    XORENC_RMSNORM(256, 3, 1);
   else if (cols <= 8192)
-    XORENC_RMSNORM(256, 4);
+    XORENC_RMSNORM(256, 4, 1);
+  else if (cols <= 10240)
+    XORENC_RMSNORM(256, 5, 1);
+  else if (cols <= 12288)
+    XORENC_RMSNORM(256, 6, 1);
   else if (cols <= 16384)
-    XORENC_RMSNORM(1024, 2);
+    XORENC_RMSNORM(256, 8, 1);
   else
-    XORENC_RMSNORM(1024, 0);
+    XORENC_RMSNORM(1024, 0, 1);
 #undef XORENC_RMSNORM
   return xorenc_internal_check_launch();
 }
@@ -312,14 +359,11 @@ extern "C" int32_t xorenc_add_rmsnorm_fp8(const void *X, int32_t x_dtype, int64_
   if (!aligned_to(X, esz) || !aligned_to(residual, esz) || !aligned_to(total, esz) || !aligned_to(Y, esz) ||
       !aligned_to(weight, dtype_bytes(w_dtype)))
     return XORENC_EALIGN;
-  const bool wide = wide_rows(X, ldx, x_dtype) && (!residual || wide_rows(residual, ldr, x_dtype)) &&
-                    (!total || wide_rows(total, ldt, x_dtype));
-  const bool w_wide = aligned_to(weight, 16), y_wide = wide_rows(Y, y_row, x_dtype);
   hipStream_t st = static_cast<hipStream_t>(hip_stream);
   xorenc_internal_begin_call();
-  return x_dtype == XORENC_X_F32
-             ? launch_rmsnorm<F32>(X, ldx, residual, ldr, weight, w_dtype == XORENC_X_BF16, wide, w_wide, rows, cols, eps, total, ldt, Y,
-                                   y_row, y_col, y_wide, Q, ldq, S, s_row, s_blk, st)
-             : launch_rmsnorm<BF16>(X, ldx, residual, ldr, weight, w_dtype == XORENC_X_BF16, wide, w_wide, rows, cols, eps, total, ldt,
-                                    Y, y_row, y_col, y_wide, Q, ldq, S, s_row, s_blk, st);
+  const int moved = 1 + esz * (1 + (residual != nullptr) + (total != nullptr) + (Y != nullptr));
+  return for_type(x_dtype, streams(rows * cols, moved), [&](auto type, auto stream) {
+    return launch_rmsnorm<decltype(type), kStreamsRows<decltype(type), decltype(stream)::value>>(
+        X, ldx, residual, ldr, weight, w_dtype == XORENC_X_BF16, rows, cols, eps, total, ldt, Y, y_row, y_col, Q, ldq, S, s_row, s_blk, st);
+  });
 }

@@ -31,9 +31,13 @@ struct MatmulArgs {
 
 // A wave's 16 TN x 16 TM results, from row n_first of W and m_first of A on.  A lane holds four neighbours of a row of Y in
 // each 16 x 16 tile.  They change places in LDS (`out`, the wave's own; 16-byte chunks of row m at chunk ^ m), so that a store
-// writes 16 bytes a lane and whole runs of 16 TN results (8192 x 16384 x 4096 bf16: 569 -> 539 us).
+// writes 16 bytes a lane and whole runs of 16 TN results (8192 x 16384 x 4096 bf16: 569 -> 539 us).  Stores that pass the caches
+// by leave them to A and W, and are not waited for by the next tile's loads: the same shape 547 -> 486 us, 4096 x 2048 x 512 11.2 ->
+// 9.4, 4096 x 1024 x 1024 12.1 -> 11.5; 4096 x 8192 x 1024 42.1 -> 42.8.  (What reads Y next finds less of it in the caches: the
+// product and the gate behind it 609 -> 599 us for 8192 x 16384 x 4096, 301 -> 306 for 4096, 154 -> 151 for 2048 tokens, 17.3 -> 16.2 for
+// 4096 x 2048 x 512.)
 template <int TN, int TM, bool EXACT>
-__device__ inline void store_tile(const MatmulArgs &g, const f32x4 (&acc)[TN][TM], uint8_t *out, int m_first, int n_first, int lane, int wide) {
+__device__ inline void store_tile(const MatmulArgs &g, const f32x4 (&acc)[TN][TM], uint8_t *out, int m_first, int n_first, int lane) {
   typedef typename std::conditional<EXACT, float, uint16_t>::type Out;
   constexpr int WIDTH = 16 * TN, ROW = WIDTH * (int)sizeof(Out), CHUNKS = ROW / 16, PER_CHUNK = 16 / (int)sizeof(Out);
   const int r = lane & 15;
@@ -50,28 +54,20 @@ __device__ inline void store_tile(const MatmulArgs &g, const f32x4 (&acc)[TN][TM
         *reinterpret_cast<u32x2 *>(p) = u32x2{to_bf16x2(v[0], v[1]), to_bf16x2(v[2], v[3])};
     }
   Out *const Y = static_cast<Out *>(g.Y);
-  if (wide) {
-    const int c = lane % CHUNKS, n = n_first + c * PER_CHUNK;
+  const int c = lane % CHUNKS, n = n_first + c * PER_CHUNK;
 #pragma unroll
-    for (int k = 0; k < (16 * TM * CHUNKS + 63) / 64; ++k) {
-      const int m = k * (64 / CHUNKS) + lane / CHUNKS;
-      if (m >= 16 * TM) break;
-      const u32x4 v = *reinterpret_cast<const u32x4 *>(out + m * ROW + (c ^ (m & (CHUNKS - 1))) * 16);
-      if (m_first + m >= g.M) continue;
-      Out *const y = Y + (int64_t)(m_first + m) * g.ldy + n;
-      if (n + PER_CHUNK <= g.N) {
-        *reinterpret_cast<u32x4 *>(y) = v;
-      } else {
+  for (int k = 0; k < (16 * TM * CHUNKS + 63) / 64; ++k) {
+    const int m = k * (64 / CHUNKS) + lane / CHUNKS;
+    if (m >= 16 * TM) break;
+    const u32x4 v = *reinterpret_cast<const u32x4 *>(out + m * ROW + (c ^ (m & (CHUNKS - 1))) * 16);
+    if (m_first + m >= g.M) continue;
+    Out *const y = Y + (int64_t)(m_first + m) * g.ldy + n;
+    if (n + PER_CHUNK <= g.N) {
+      __builtin_nontemporal_store(v, reinterpret_cast<u32x4_anywhere *>(y));
+    } else {
 #pragma unroll
-        for (int e = 0; e < PER_CHUNK; ++e)
-          if (n + e < g.N) y[e] = EXACT ? (Out)__uint_as_float(v[e & 3]) : (Out)(v[(e / 2) & 3] >> (16 * (e & 1)));
-      }
-    }
-  } else {  // rows of Y that do not start on 16-byte boundaries
-    for (int k = lane; k < 16 * TM * WIDTH; k += 64) {
-      const int m = k / WIDTH, n = k % WIDTH, byte = n * (int)sizeof(Out);
-      const Out v = *reinterpret_cast<const Out *>(out + m * ROW + ((byte / 16) ^ (m & (CHUNKS - 1))) * 16 + byte % 16);
-      if (m_first + m < g.M && n_first + n < g.N) Y[(int64_t)(m_first + m) * g.ldy + n_first + n] = v;
+      for (int e = 0; e < PER_CHUNK; ++e)
+        if (n + e < g.N) y[e] = EXACT ? (Out)__uint_as_float(v[e & 3]) : (Out)(v[(e / 2) & 3] >> (16 * (e & 1)));
     }
   }
 }
@@ -88,7 +84,7 @@ struct TileShape {
 };
 
 template <int TN, int TM, int WN, int WM, bool EXACT>
-__global__ __launch_bounds__(WN *WM * 64, 2) void matmul_tile_kernel(MatmulArgs g, int wide, int n_tiles, int m_tiles, int per_xcd) {
+__global__ __launch_bounds__(WN *WM * 64, 2) void matmul_tile_kernel(MatmulArgs g, int n_tiles, int m_tiles, int per_xcd) {
   typedef TileShape<TN, TM, WN, WM, EXACT> Shape;
   constexpr int BN = Shape::BN, BM = Shape::BM, STAGE = Shape::STAGE, N1 = Shape::GROUP1, N2 = Shape::GROUP2;
   extern __shared__ __attribute__((aligned(1024))) uint8_t tile_lds[];
@@ -264,7 +260,7 @@ __global__ __launch_bounds__(WN *WM * 64, 2) void matmul_tile_kernel(MatmulArgs 
     for (int k = 0; k < 4; ++k) acc[TN - 1][j][k] += f[j] * d[(TN - 1) & 1][j][k];
   static_assert(BN * BM * (EXACT ? 4 : 2) <= 2 * STAGE, "the results of a tile fit");
   __syncthreads();
-  store_tile<TN, TM, EXACT>(g, acc, tile_lds + wave * (16 * TM * 16 * TN * (EXACT ? 4 : 2)), m0 + wm * (16 * TM), n0 + wn * (16 * TN), lane, wide);
+  store_tile<TN, TM, EXACT>(g, acc, tile_lds + wave * (16 * TM * 16 * TN * (EXACT ? 4 : 2)), m0 + wm * (16 * TM), n0 + wn * (16 * TN), lane);
 }
 
 }  // namespace xorenc_fp8_detail

@@ -61,8 +61,8 @@ __device__ inline float rest_of_bf16(float v) {
 // Logits in fp32: a workgroup per expert and four tokens, its waves share the columns.  The workgroups behind them write the
 // bf16 terms of x; the first one clears the tickets.
 template <class T, int TERMS>
-__global__ __launch_bounds__(256) void router_kernel(const typename T::Elem *__restrict__ X, int64_t ldx, int wide,
-                                                     const typename T::Elem *__restrict__ router, int64_t ldr, int r_wide, int tokens,
+__global__ __launch_bounds__(256) void router_kernel(const typename T::Elem *__restrict__ X, int64_t ldx,
+                                                     const typename T::Elem *__restrict__ router, int64_t ldr, int tokens,
                                                      int H, int E, float *__restrict__ logits, uint16_t *__restrict__ terms,
                                                      int logit_groups, uint32_t *__restrict__ tickets, int n_tickets) {
   __shared__ float part[4][4];
@@ -75,7 +75,7 @@ __global__ __launch_bounds__(256) void router_kernel(const typename T::Elem *__r
     if (i >= (int64_t)tokens * pieces) return;
     const int t = (int)(i / pieces), c = (int)(i - (int64_t)t * pieces) * 8;
     float v[8];
-    load_piece<T>(X + t * ldx, c, H, wide, v);
+    piece_of<T>(load_piece<T>(X + t * ldx, c, H), c, H, v);
     uint16_t *const dst = terms + ((int64_t)t * (pieces / 16) + c / kBlock) * (TERMS * kBlock) + term_place(c % kBlock);
 #pragma unroll
     for (int k = 0; k < TERMS; ++k) {
@@ -90,9 +90,13 @@ __global__ __launch_bounds__(256) void router_kernel(const typename T::Elem *__r
   float acc[4] = {0.f, 0.f, 0.f, 0.f};
   for (int c = threadIdx.x * 8; c < H; c += 2048) {
     float r[8], v[4][8];
-    load_piece<T>(router + e * ldr, c, H, r_wide, r);
+    typename T::Raw raw[5];
+    raw[4] = load_piece<T>(router + e * ldr, c, H);
 #pragma unroll
-    for (int k = 0; k < 4; ++k) load_piece<T>(X + min(t0 + k, tokens - 1) * ldx, c, H, wide, v[k]);
+    for (int k = 0; k < 4; ++k) raw[k] = load_piece<T>(X + min(t0 + k, tokens - 1) * ldx, c, H);
+    piece_of<T>(raw[4], c, H, r);
+#pragma unroll
+    for (int k = 0; k < 4; ++k) piece_of<T>(raw[k], c, H, v[k]);
 #pragma unroll
     for (int k = 0; k < 4; ++k)
 #pragma unroll
@@ -794,12 +798,12 @@ void launch_products(const MoeArgs &g, void *Y, int64_t ldy, hipStream_t st) {
 }
 
 template <class T, int TERMS, int H_TERMS>
-int32_t launch_moe(const MoeArgs &g, const void *X, int64_t ldx, bool wide, const void *router, int64_t ldr, bool r_wide, void *Y, int64_t ldy, hipStream_t st) {
+int32_t launch_moe(const MoeArgs &g, const void *X, int64_t ldx, const void *router, int64_t ldr, void *Y, int64_t ldy, hipStream_t st) {
   typedef typename T::Elem E;
   const int groups = g.E * ((g.T + 3) / 4);
   const int64_t pieces = (int64_t)g.T * ((g.H + kBlock - 1) / kBlock) * 16;
   hipLaunchKernelGGL((router_kernel<T, TERMS>), dim3((unsigned)(groups + (pieces + 255) / 256)), dim3(256), 0, st,
-                     static_cast<const E *>(X), ldx, (int)wide, static_cast<const E *>(router), ldr, (int)r_wide, g.T, g.H, g.E, g.logits,
+                     static_cast<const E *>(X), ldx, static_cast<const E *>(router), ldr, g.T, g.H, g.E, g.logits,
                      g.x_terms, groups, g.tickets, g.row_groups);
   if (!g.plans) hipLaunchKernelGGL(picks_kernel, dim3(1), dim3(1024), 0, st, g);
   int32_t rc = xorenc_internal_check_launch();
@@ -856,7 +860,6 @@ extern "C" int32_t xorenc_moe_fp8(const xorenc_moe *L, const void *X, int32_t x_
       !aligned_to(L->S2, 4) || !aligned_to(workspace, 16))
     return XORENC_EALIGN;
   unsigned char *const ws = static_cast<unsigned char *>(workspace);
-  const bool wide = wide_rows(X, ldx, x_dtype);
   MoeArgs g;
   g.W13 = L->W13, g.W2 = L->W2, g.S13 = L->S13, g.S2 = L->S2;
   g.ldw13 = L->ld_w13, g.w13_stride = L->w13_stride, g.lds13 = L->ld_s13, g.s13_stride = L->s13_stride;
@@ -875,10 +878,9 @@ extern "C" int32_t xorenc_moe_fp8(const xorenc_moe *L, const void *X, int32_t x_
   // Up to four tokens, up to 1024 workgroups: a launch less for a longer start of each (us: two tokens, four of 16 experts of 1024 x
   // 1024 22.2 and 23.4; four tokens, six of 64 of 2048 x 1024, 1536 workgroups, 45.0 and 43.9)
   g.plans = tokens == 1 || (tokens <= 4 && (int64_t)((I + 15) / 16) * p.most_uses <= 1024);
-  const bool r_wide = wide_rows(L->router, L->ld_router, x_dtype);
   hipStream_t st = static_cast<hipStream_t>(hip_stream);
   xorenc_internal_begin_call();
   return x_dtype == XORENC_X_F32
-             ? launch_moe<F32, 3, 3>(g, X, ldx, wide, L->router, L->ld_router, r_wide, Y, ldy, st)
-             : launch_moe<BF16, 1, 2>(g, X, ldx, wide, L->router, L->ld_router, r_wide, Y, ldy, st);
+             ? launch_moe<F32, 3, 3>(g, X, ldx, L->router, L->ld_router, Y, ldy, st)
+             : launch_moe<BF16, 1, 2>(g, X, ldx, L->router, L->ld_router, Y, ldy, st);
 }
