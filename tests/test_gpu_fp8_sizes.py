@@ -99,6 +99,13 @@ def test_stacks_beyond_32_bits():
     assert torch.equal(xe.moe_fp8(tokens, router, apart(W13), S13, apart(W2), S2, 3), plain)
 
 
+@pytest.mark.parametrize("out", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("M,N,K", [(648, 9046, 68), (1080, 11586, 129), (1052, 7849, 302), (334, 10347, 931), (3000, 3000, 1000), (1934, 1568, 69),
+                                   (17, 4576, 513), (74, 8202, 424), (1, 8219, 398), (1, 14874, 136), (700, 4096, 1111), (2048, 5000, 300)])
+def test_product_of_middling_sizes(M, N, K, out):
+    test_product(M, N, K, out)
+
+
 # tokens per expert beyond one pass, one expert for all, one workgroup to 32 for a sum, few and many rows of inner features
 @pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
 @pytest.mark.parametrize("T,H,I,E,n", [(64, 144, 72, 2, 2), (64, 130, 40, 1, 1), (63, 96, 56, 3, 3), (33, 128, 264, 2, 1), (1, 128, 4200, 3, 2),
