@@ -367,7 +367,7 @@ XORENC_API int32_t xorenc_quant_fp8(const void *X, int32_t x_dtype, int64_t ldx,
 /*
  * The residual's addition and the RMS norm, with the result in 8 bits (blocks of 1 x 128):
  *   t = X + residual;  y = t / sqrt(mean(t^2) + eps) * weight;  Q, S = y
- * in fp32 (t is not rounded before it is normed).  residual, total and Y may be NULL: nothing is added, t or y is not stored.
+ * in fp32 (t is not rounded before it is normed; a row's result does not depend on how many there are).  residual, total and Y may be NULL: nothing is added, t or y is not stored.
  * total and Y have X's type; weight (cols values, contiguous) has its own.  total may be X or residual itself.  Y[r * y_row +
  * c * y_col]: with y_col = 1 rows of features, with y_row = 1 the columns that xorenc_spmm multiplies.  XORENC_ELIMIT from 2^22 rows on.
  */

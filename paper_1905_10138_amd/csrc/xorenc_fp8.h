@@ -3,6 +3,8 @@
 #ifndef XORENC_FP8_H
 #define XORENC_FP8_H
 
+#include <type_traits>
+
 #include <hip/hip_runtime.h>
 
 #include "xorenc_internal.h"
@@ -156,6 +158,19 @@ __device__ inline uint32_t max_of_16_lanes(uint32_t v) {
   v = max(v, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0x141, 0xf, 0xf, true));  // half row mirrored
   v = max(v, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0x140, 0xf, 0xf, true));  // row mirrored
   return v;
+}
+
+// Sum of a wave's values, on all lanes: the same tree wherever the wave is.
+__device__ inline float sum_of_wave(float v) {
+  auto moved = [&](auto pattern) {
+    return __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(v), decltype(pattern)::value, 0xf, 0xf, true));
+  };
+  v += moved(std::integral_constant<int, 0xB1>());
+  v += moved(std::integral_constant<int, 0x4E>());
+  v += moved(std::integral_constant<int, 0x141>());
+  v += moved(std::integral_constant<int, 0x140>());
+  v += __shfl_xor(v, 16);
+  return v + __shfl_xor(v, 32);
 }
 
 // Operands of the matrix instructions for 128 columns of 16 rows.  Lane l holds 32 values of row l % 16: columns

@@ -91,7 +91,9 @@ __global__ __launch_bounds__(256) void quant_square_kernel(const typename T::Ele
 // residual are read once more for the second half (from the caches; a `total` that is stored over one of them is not read
 // back, it may be rounded).  Up to 1536 columns a wave holds a row: no barrier, and a quarter of the workgroups (8192 x 600
 // 15.4 -> 12.0 us, 8192 x 1200 without a residual 14.9 -> 11.0; 8192 x 2000 a wave a row 32.8, four 29.4).  Beyond, 256 threads: several
-// rows a CU hide each other's loads (8192 x 9216 without a residual 54 us; 1024 threads 76).
+// rows a CU hide each other's loads (8192 x 9216 without a residual 54 us; 1024 threads 76).  Up to 512 rows there are no others, and
+// more threads a row are faster: 512 for 9216 columns of one token 6.6 -> 5.4 us, of 64 6.6 -> 5.6, of 1000 15.3 and 15.2; 256, not a
+// wave, for 500 x 1500 5.6 -> 4.2.
 template <class T, int THREADS, int PASSES, int ROWS, bool STREAM>
 __global__ __launch_bounds__(THREADS *ROWS) void rmsnorm_kernel(const typename T::Elem *X, int64_t ldx,
                                                           const typename T::Elem *R, int64_t ldr, const void *__restrict__ w,
@@ -101,7 +103,7 @@ __global__ __launch_bounds__(THREADS *ROWS) void rmsnorm_kernel(const typename T
                                                           float *__restrict__ S, int64_t s_row, int64_t s_blk) {
   static_assert(ROWS == 1 || THREADS == 64, "a barrier is for the row's threads");
   constexpr int STEP = THREADS * 8, WAVES = THREADS / 64;
-  __shared__ float wave_sum[WAVES];
+  __shared__ float chunk_sum[WAVES * (PASSES > 0 ? PASSES : 1)];
   const int64_t r = (int64_t)blockIdx.x * ROWS + threadIdx.x / THREADS;
   const int t = threadIdx.x % THREADS;
   if (ROWS > 1 && r >= rows) return;
@@ -139,7 +141,12 @@ __global__ __launch_bounds__(THREADS *ROWS) void rmsnorm_kernel(const typename T
       float of_pass = 0.f;
 #pragma unroll
       for (int i = 0; i < 8; ++i) of_pass += s[p][i] * s[p][i];
-      sq += of_pass;
+      of_pass = sum_of_wave(of_pass);
+      if constexpr (WAVES > 1) {
+        if ((t & 63) == 0) chunk_sum[p * WAVES + (t >> 6)] = of_pass;
+      } else {
+        sq += of_pass;
+      }
       if (total) store_piece<T>(total, p * STEP + t * 8, cols, s[p]);
     }
   } else {
@@ -151,14 +158,16 @@ __global__ __launch_bounds__(THREADS *ROWS) void rmsnorm_kernel(const typename T
       sq += of_pass;
     }
   }
-#pragma unroll
-  for (int o = 32; o > 0; o >>= 1) sq += __shfl_xor(sq, o);
+  // A row's sum is that of its chunks of 512 columns (a wave and pass each), one after the other, however many threads it has.
+  if constexpr (PASSES == 0) {
+    sq = sum_of_wave(sq);
+    if ((t & 63) == 0) chunk_sum[t >> 6] = sq;
+  }
   if constexpr (WAVES > 1) {
-    if ((t & 63) == 0) wave_sum[t >> 6] = sq;
     __syncthreads();
     sq = 0.f;
 #pragma unroll
-    for (int i = 0; i < WAVES; ++i) sq += wave_sum[i];
+    for (int i = 0; i < WAVES * (PASSES > 0 ? PASSES : 1); ++i) sq += chunk_sum[i];
   }
   const float rstd = 1.f / sqrtf(sq / (float)cols + eps);
   auto finish = [&](int c, float *v) {
@@ -315,9 +324,20 @@ int32_t launch_rmsnorm(const void *X, int64_t ldx, const void *R, int64_t ldr, c
   hipLaunchKernelGGL((rmsnorm_kernel<T, THREADS, PASSES, ROWS, (STREAM && PASSES > 0)>), dim3((unsigned)((rows + ROWS - 1) / ROWS)), dim3(THREADS * ROWS), 0, st, \
                      static_cast<const E *>(X), ldx, static_cast<const E *>(R), ldr, w, w_bf16, (int)rows, cols, \
                      eps, static_cast<E *>(total), ldt, static_cast<E *>(Y), y_row, y_col, Q, ldq, S, s_row, s_blk)
-  if (cols <= 512)
+  if (cols > 16384)
+    XORENC_RMSNORM(1024, 0, 1);
+  else if (cols <= 512)
     XORENC_RMSNORM(64, 1, 4);
-  else if (cols <= 1024)
+  else if (rows <= 512 && cols <= 12288) {  // two a CU: what counts is how long a row takes
+    if (cols <= 2048)
+      XORENC_RMSNORM(256, 1, 1);
+    else if (cols <= 4096)
+      XORENC_RMSNORM(512, 1, 1);
+    else if (cols <= 8192)
+      XORENC_RMSNORM(512, 2, 1);
+    else
+      XORENC_RMSNORM(512, 3, 1);
+  } else if (cols <= 1024)
     XORENC_RMSNORM(64, 2, 4);
   else if (cols <= 1536)
     XORENC_RMSNORM(64, 3, 4);
@@ -333,10 +353,8 @@ int32_t launch_rmsnorm(const void *X, int64_t ldx, const void *R, int64_t ldr, c
     XORENC_RMSNORM(256, 5, 1);
   else if (cols <= 12288)
     XORENC_RMSNORM(256, 6, 1);
-  else if (cols <= 16384)
-    XORENC_RMSNORM(256, 8, 1);
   else
-    XORENC_RMSNORM(1024, 0, 1);
+    XORENC_RMSNORM(256, 8, 1);
 #undef XORENC_RMSNORM
   return xorenc_internal_check_launch();
 }

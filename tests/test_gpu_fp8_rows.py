@@ -74,3 +74,21 @@ def test_many_rows(dtype, rows, cols):
         assert torch.equal(whole[1][50:51] if rest else whole[1][part], some[1])
         if len(whole) == 4:
             assert torch.equal(whole[2][part], some[2]) and torch.equal(whole[3][part], some[3])
+
+
+# up to 512 rows and beyond: a row's threads, or several rows a workgroup
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("cols", [600, 1300, 2000, 4000, 6001, 9000, 12000])
+def test_norm_of_many_rows_is_that_of_each(cols, dtype):
+    g = gen(cols)
+    x, r = normal(g, 515, cols, dtype=dtype).to(DEV), normal(g, 515, cols, dtype=dtype).to(DEV)
+    w = normal(g, cols).to(DEV)
+    whole = xe.add_rmsnorm_fp8(x, w, r, normed=True)
+    part = xe.add_rmsnorm_fp8(x[500:], w, r[500:], normed=True)
+    # two orders of the sum of squares: both within the tolerance of the definition
+    _, want = ref.rmsnorm(x[500:].cpu(), r[500:].cpu(), w.cpu(), 1e-6)
+    half = 2.0 ** -8 if dtype is torch.bfloat16 else 0.0
+    for out in ([t[500:] for t in whole], part):
+        assert torch.equal(out[2], (x[500:].float() + r[500:].float()).to(dtype))
+        assert ((out[3].cpu().double() - want).abs() <= (half + 40 * U) * want.abs() + 1e-30).all()
+        ref.check_quantised(want, out[0], out[1], 1, 40 * U)
