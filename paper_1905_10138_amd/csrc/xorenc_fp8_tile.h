@@ -95,7 +95,11 @@ __global__ __launch_bounds__(WN *WM * 64, 2) void matmul_tile_kernel(MatmulArgs 
   constexpr int GROUP = 4;
   const int strip = tile / (GROUP * n_tiles), in_strip = tile - strip * (GROUP * n_tiles);
   const int strip_m = min(GROUP, m_tiles - strip * GROUP);
-  const int tile_n = in_strip / strip_m, tile_m = strip * GROUP + in_strip - tile_n * strip_m;
+  // ... and each strip begins where an XCD's 32 CUs end that began with the strip before: rows of W that come from memory, not from
+  // the cache behind the L2s, are then waited for by one XCD, and in the first round (8192 x 16384 x 4096, three sets of operands in turn
+  // 553 -> 527 us, 4096 x 9216 x 8192 368 -> 344; one set, which that cache holds, 514 and 521)
+  const int at_n = in_strip / strip_m, tile_m = strip * GROUP + in_strip - at_n * strip_m;
+  const int tile_n = (at_n + strip * (32 / GROUP)) % n_tiles;
   const int n0 = tile_n * BN, m0 = tile_m * BM;
 
   const int tid = threadIdx.x, lane = tid & 63;
