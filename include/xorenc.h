@@ -346,7 +346,7 @@ XORENC_API int32_t xorenc_spmm_ws(const xorenc_layer *layer, const void *X, int3
  *
  * Rules beside the general ones above:
  *   - matrices are row-major, leading dimensions are in elements; rows of e4m3 matrices start on 16-byte boundaries (base address
- *     and leading dimension), other rows may start anywhere (16-byte boundaries are faster).  Bytes between a row's last
+ *     and leading dimension), other rows may start on any element (16-byte boundaries are a little faster).  Bytes between a row's last
  *     element and the next multiple of 16 may be read, and never reach a result;
  *   - S has two strides where it belongs to activations: element (r, b) is S[r * s_row + b * s_blk].  s_row = 1 (block column
  *     by block column) is what the kernels write and read fastest;
@@ -367,9 +367,10 @@ XORENC_API int32_t xorenc_quant_fp8(const void *X, int32_t x_dtype, int64_t ldx,
 /*
  * The residual's addition and the RMS norm, with the result in 8 bits (blocks of 1 x 128):
  *   t = X + residual;  y = t / sqrt(mean(t^2) + eps) * weight;  Q, S = y
- * in fp32 (t is not rounded before it is normed; a row's result does not depend on how many there are).  residual, total and Y may be NULL: nothing is added, t or y is not stored.
- * total and Y have X's type; weight (cols values, contiguous) has its own.  total may be X or residual itself.  Y[r * y_row +
- * c * y_col]: with y_col = 1 rows of features, with y_row = 1 the columns that xorenc_spmm multiplies.  XORENC_ELIMIT from 2^22 rows on.
+ * in fp32 (t is not rounded before it is normed; a row's result does not depend on how many there are).  residual, total and Y
+ * may be NULL: nothing is added, t or y is not stored.  total and Y have X's type; weight (cols values, contiguous) has its own.
+ * total may be X or residual itself.  Y[r * y_row + c * y_col]: with y_col = 1 rows of features, with y_row = 1 the columns that
+ * xorenc_spmm multiplies.  XORENC_ELIMIT from 2^22 rows on.
  */
 XORENC_API int32_t xorenc_add_rmsnorm_fp8(const void *X, int32_t x_dtype, int64_t ldx, const void *residual, int64_t ldr,
                                           const void *weight, int32_t w_dtype, int64_t rows, int32_t cols, float eps, void *total,
