@@ -107,17 +107,18 @@ struct BF16 {
 
 // Eight values of a row from column c on; columns from `cols` on are zero.  The load comes first, without a branch (so that
 // several are on their way together), and takes the row's last eight elements where fewer are left behind c; the values
-// come from it.  STREAM: they are not kept in caches.
+// come from it.  STREAM: they are not kept in caches.  whole (a constant): c + 8 <= cols is known.
 template <class T, bool STREAM = false>
-__device__ inline typename T::Raw load_piece(const typename T::Elem *row, int c, int cols) {
+__device__ inline typename T::Raw load_piece(const typename T::Elem *row, int c, int cols, bool whole = false) {
+  if (whole) return T::template load8<STREAM>(row + c);
   return cols >= 8 ? T::template load8<STREAM>(row + min(c, cols - 8)) : T::first_of(row, c ? 0 : cols);
 }
 
 template <class T>
-__device__ inline void piece_of(const typename T::Raw &raw, int c, int cols, float *v) {
+__device__ inline void piece_of(const typename T::Raw &raw, int c, int cols, float *v, bool whole = false) {
   T::widen(raw, v);
   const int off = c + 8 - cols;  // elements before column c
-  if (off > 0 && cols >= 8) {
+  if (!whole && off > 0 && cols >= 8) {
 #pragma unroll
     for (int d = 1; d < 8; d *= 2)
 #pragma unroll
@@ -128,8 +129,8 @@ __device__ inline void piece_of(const typename T::Raw &raw, int c, int cols, flo
 }
 
 template <class T>
-__device__ inline void store_piece(typename T::Elem *row, int c, int cols, const float *v) {
-  if (c + 8 <= cols) {
+__device__ inline void store_piece(typename T::Elem *row, int c, int cols, const float *v, bool whole = false) {
+  if (whole || c + 8 <= cols) {
     T::store8(row + c, v);
   } else {
 #pragma unroll
@@ -139,10 +140,10 @@ __device__ inline void store_piece(typename T::Elem *row, int c, int cols, const
 }
 
 // Eight values as e4m3 to row[c ..].  Rows of Q start on 16-byte boundaries and c is a multiple of eight.
-__device__ inline void store_e4m3_piece(uint8_t *row, int c, int cols, const float *v, float inv) {
+__device__ inline void store_e4m3_piece(uint8_t *row, int c, int cols, const float *v, float inv, bool whole = false) {
   const u32x2 w = {pack_e4m3(v[0] * inv, v[1] * inv, v[2] * inv, v[3] * inv),
                    pack_e4m3(v[4] * inv, v[5] * inv, v[6] * inv, v[7] * inv)};
-  if (c + 8 <= cols) {
+  if (whole || c + 8 <= cols) {
     *reinterpret_cast<u32x2 *>(row + c) = w;
   } else {
 #pragma unroll

@@ -89,11 +89,12 @@ __global__ __launch_bounds__(256) void quant_square_kernel(const typename T::Ele
 // THREADS per row, ROWS rows a workgroup (more than one only where a row is a wave's): s = x + residual, y = s / sqrt(mean s^2 +
 // eps) * w.  PASSES > 0: the row's sums stay in registers, eight per thread and pass.  PASSES = 0, rows that do not fit: x and the
 // residual are read once more for the second half (from the caches; a `total` that is stored over one of them is not read
-// back, it may be rounded).  Up to 1536 columns a wave holds a row: no barrier, and a quarter of the workgroups (8192 x 600
+// back, it may be rounded).  A row is wider than all passes but the last, which alone has to look where it ends: its code is four times
+// as long, and a single row waits for code (one token of 9216 5.4 -> 5.1 us, of 16000 8.8 -> 7.8).  Up to 1536 columns a wave holds a row: no barrier, and a quarter of the workgroups (8192 x 600
 // 15.4 -> 12.0 us, 8192 x 1200 without a residual 14.9 -> 11.0; 8192 x 2000 a wave a row 32.8, four 29.4).  Beyond, 256 threads: several
 // rows a CU hide each other's loads (8192 x 9216 without a residual 54 us; 1024 threads 76).  Up to 512 rows there are no others, and
-// more threads a row are faster: 512 for 9216 columns of one token 6.6 -> 5.4 us, of 64 6.6 -> 5.6, of 1000 15.3 and 15.2; 256, not a
-// wave, for 500 x 1500 5.6 -> 4.2.
+// more threads a row are faster: 512 for 9216 columns of one token 6.6 -> 5.4 us (1024 5.5), of 64 6.6 -> 5.6, of 1000 15.3 and 15.2;
+// 1024 for 16000 columns of one token 7.8 -> 5.0, of 500 14.9 -> 12.9; 256, not a wave, for 500 x 1500 5.6 -> 4.2.
 template <class T, int THREADS, int PASSES, int ROWS, bool STREAM>
 __global__ __launch_bounds__(THREADS *ROWS) void rmsnorm_kernel(const typename T::Elem *X, int64_t ldx,
                                                           const typename T::Elem *R, int64_t ldr, const void *__restrict__ w,
@@ -113,17 +114,17 @@ __global__ __launch_bounds__(THREADS *ROWS) void rmsnorm_kernel(const typename T
   struct Pair {
     typename T::Raw x, r;
   };
-  auto load = [&](int c) {
+  auto load = [&](int c, bool whole) {
     Pair p;
-    p.x = load_piece<T, STREAM>(X, c, cols);
-    if (R) p.r = load_piece<T, STREAM>(R, c, cols);
+    p.x = load_piece<T, STREAM>(X, c, cols, whole);
+    if (R) p.r = load_piece<T, STREAM>(R, c, cols, whole);
     return p;
   };
-  auto sums = [&](const Pair &p, int c, float *s) {
-    piece_of<T>(p.x, c, cols, s);
+  auto sums = [&](const Pair &p, int c, float *s, bool whole) {
+    piece_of<T>(p.x, c, cols, s, whole);
     if (R) {
       float u[8];
-      piece_of<T>(p.r, c, cols, u);
+      piece_of<T>(p.r, c, cols, u, whole);
 #pragma unroll
       for (int i = 0; i < 8; ++i) s[i] += u[i];
     }
@@ -134,10 +135,10 @@ __global__ __launch_bounds__(THREADS *ROWS) void rmsnorm_kernel(const typename T
   if constexpr (PASSES > 0) {
     Pair held[PASSES];
 #pragma unroll
-    for (int p = 0; p < PASSES; ++p) held[p] = load(p * STEP + t * 8);
+    for (int p = 0; p < PASSES; ++p) held[p] = load(p * STEP + t * 8, p + 1 < PASSES);
 #pragma unroll
     for (int p = 0; p < PASSES; ++p) {
-      sums(held[p], p * STEP + t * 8, s[p]);
+      sums(held[p], p * STEP + t * 8, s[p], p + 1 < PASSES);
       float of_pass = 0.f;
 #pragma unroll
       for (int i = 0; i < 8; ++i) of_pass += s[p][i] * s[p][i];
@@ -147,11 +148,11 @@ __global__ __launch_bounds__(THREADS *ROWS) void rmsnorm_kernel(const typename T
       } else {
         sq += of_pass;
       }
-      if (total) store_piece<T>(total, p * STEP + t * 8, cols, s[p]);
+      if (total) store_piece<T>(total, p * STEP + t * 8, cols, s[p], p + 1 < PASSES);
     }
   } else {
     for (int c = t * 8; c < cols; c += STEP) {
-      sums(load(c), c, s[0]);
+      sums(load(c, false), c, s[0], false);
       float of_pass = 0.f;
 #pragma unroll
       for (int i = 0; i < 8; ++i) of_pass += s[0][i] * s[0][i];
@@ -170,12 +171,12 @@ __global__ __launch_bounds__(THREADS *ROWS) void rmsnorm_kernel(const typename T
     for (int i = 0; i < WAVES * (PASSES > 0 ? PASSES : 1); ++i) sq += chunk_sum[i];
   }
   const float rstd = 1.f / sqrtf(sq / (float)cols + eps);
-  auto finish = [&](int c, float *v) {
+  auto finish = [&](int c, float *v, bool whole) {
     float g[8];
     if (w_bf16)
-      piece_of<BF16>(load_piece<BF16>(static_cast<const uint16_t *>(w), c, cols), c, cols, g);
+      piece_of<BF16>(load_piece<BF16>(static_cast<const uint16_t *>(w), c, cols, whole), c, cols, g, whole);
     else
-      piece_of<F32>(load_piece<F32>(static_cast<const float *>(w), c, cols), c, cols, g);
+      piece_of<F32>(load_piece<F32>(static_cast<const float *>(w), c, cols, whole), c, cols, g, whole);
     uint32_t a = 0;
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
@@ -183,29 +184,29 @@ __global__ __launch_bounds__(THREADS *ROWS) void rmsnorm_kernel(const typename T
       a = max(a, magnitude_bits(v[i]));
     }
     const float sc = block_scale(max_of_16_lanes(a));
-    if (c >= cols) return;
-    store_e4m3_piece(Q + r * ldq, c, cols, v, 1.f / sc);
+    if (!whole && c >= cols) return;
+    store_e4m3_piece(Q + r * ldq, c, cols, v, 1.f / sc, whole);
     if ((t & 15) == 0) S[r * s_row + (int64_t)(c / kBlock) * s_blk] = sc;
     if (Y) {
       if (y_col == 1) {
-        store_piece<T>(Y + r * y_row, c, cols, v);
+        store_piece<T>(Y + r * y_row, c, cols, v, whole);
       } else {
 #pragma unroll
         for (int i = 0; i < 8; ++i)
-          if (c + i < cols) T::store(Y + r * y_row + (c + i) * y_col, v[i]);
+          if (whole || c + i < cols) T::store(Y + r * y_row + (c + i) * y_col, v[i]);
       }
     }
   };
   if constexpr (PASSES > 0) {
 #pragma unroll
     for (int p = 0; p < PASSES; ++p)
-      if (p * STEP < cols) finish(p * STEP + t * 8, s[p]);
+      finish(p * STEP + t * 8, s[p], p + 1 < PASSES);
   } else {
     for (int c0 = 0; c0 < cols; c0 += STEP) {  // uniform: whole rows of 16 lanes take part in a block's maximum
       const int c = c0 + t * 8;
-      sums(load(c), c, s[0]);
+      sums(load(c, false), c, s[0], false);
       if (total) store_piece<T>(total, c, cols, s[0]);
-      finish(c, s[0]);
+      finish(c, s[0], false);
     }
   }
 }
@@ -328,15 +329,17 @@ int32_t launch_rmsnorm(const void *X, int64_t ldx, const void *R, int64_t ldr, c
     XORENC_RMSNORM(1024, 0, 1);
   else if (cols <= 512)
     XORENC_RMSNORM(64, 1, 4);
-  else if (rows <= 512 && cols <= 12288) {  // two a CU: what counts is how long a row takes
+  else if (rows <= 512) {  // two a CU: what counts is how long a row takes
     if (cols <= 2048)
       XORENC_RMSNORM(256, 1, 1);
     else if (cols <= 4096)
       XORENC_RMSNORM(512, 1, 1);
     else if (cols <= 8192)
-      XORENC_RMSNORM(512, 2, 1);
-    else
+      XORENC_RMSNORM(1024, 1, 1);
+    else if (cols <= 12288)
       XORENC_RMSNORM(512, 3, 1);
+    else
+      XORENC_RMSNORM(1024, 2, 1);
   } else if (cols <= 1024)
     XORENC_RMSNORM(64, 2, 4);
   else if (cols <= 1536)
@@ -353,6 +356,8 @@ int32_t launch_rmsnorm(const void *X, int64_t ldx, const void *R, int64_t ldr, c
     XORENC_RMSNORM(256, 5, 1);
   else if (cols <= 12288)
     XORENC_RMSNORM(256, 6, 1);
+  else if (cols <= 14336)
+    XORENC_RMSNORM(256, 7, 1);
   else
     XORENC_RMSNORM(256, 8, 1);
 #undef XORENC_RMSNORM
