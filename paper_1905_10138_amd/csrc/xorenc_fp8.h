@@ -63,9 +63,9 @@ struct F32 {
     return {q[0], q[1]};
   }
   static __device__ inline Raw first_of(const Elem *p, int n) {  // those from the n-th on are zero
-    Raw r;
-#pragma unroll
-    for (int i = 0; i < 4; ++i) r.a[i] = i < n ? p[i] : 0.f, r.b[i] = 4 + i < n ? p[4 + i] : 0.f;
+    Raw r = {f32x4{0.f, 0.f, 0.f, 0.f}, f32x4{0.f, 0.f, 0.f, 0.f}};
+#pragma unroll 1
+    for (int k = n - 1; k >= 0; --k) r.b = f32x4{r.a[3], r.b[0], r.b[1], r.b[2]}, r.a = f32x4{p[k], r.a[0], r.a[1], r.a[2]};
     return r;
   }
   static __device__ inline void widen(const Raw &r, float *v) {
@@ -89,9 +89,10 @@ struct BF16 {
     return *q;
   }
   static __device__ inline Raw first_of(const Elem *p, int n) {
-    Raw r;
-#pragma unroll
-    for (int i = 0; i < 4; ++i) r[i] = (2 * i < n ? (uint32_t)p[2 * i] : 0u) | (2 * i + 1 < n ? (uint32_t)p[2 * i + 1] << 16 : 0u);
+    Raw r = {0u, 0u, 0u, 0u};
+#pragma unroll 1
+    for (int k = n - 1; k >= 0; --k)
+      r = Raw{r[0] << 16 | p[k], r[1] << 16 | r[0] >> 16, r[2] << 16 | r[1] >> 16, r[3] << 16 | r[2] >> 16};
     return r;
   }
   static __device__ inline void widen(const Raw &r, float *v) {
@@ -107,22 +108,35 @@ struct BF16 {
 
 // Eight values of a row from column c on; columns from `cols` on are zero.  The load comes first, without a branch (so that
 // several are on their way together), and takes the row's last eight elements where fewer are left behind c; the values
-// come from it.  STREAM: they are not kept in caches.  whole (a constant): c + 8 <= cols is known.
+// come from it.  STREAM: they are not kept in caches.  whole (a constant): c + 8 <= cols is known;
+// brief (a constant): in short code, which takes longer at a row's end.
 template <class T, bool STREAM = false>
 __device__ inline typename T::Raw load_piece(const typename T::Elem *row, int c, int cols, bool whole = false) {
   if (whole) return T::template load8<STREAM>(row + c);
   return cols >= 8 ? T::template load8<STREAM>(row + min(c, cols - 8)) : T::first_of(row, c ? 0 : cols);
 }
 
+// Stores of a row's end are short loops, not straight code: a kernel that few waves run waits for its code.
+__device__ inline void shift_down(float *v) {
+#pragma unroll
+  for (int i = 0; i < 7; ++i) v[i] = v[i + 1];
+  v[7] = 0.f;
+}
+
 template <class T>
-__device__ inline void piece_of(const typename T::Raw &raw, int c, int cols, float *v, bool whole = false) {
+__device__ inline void piece_of(const typename T::Raw &raw, int c, int cols, float *v, bool whole = false, bool brief = false) {
   T::widen(raw, v);
   const int off = c + 8 - cols;  // elements before column c
   if (!whole && off > 0 && cols >= 8) {
+    if (brief) {
+#pragma unroll 1
+      for (int k = off & 7; k > 0; --k) shift_down(v);
+    } else {
 #pragma unroll
-    for (int d = 1; d < 8; d *= 2)
+      for (int d = 1; d < 8; d *= 2)
 #pragma unroll
-      for (int i = 0; i < 8; ++i) v[i] = off & d ? (i + d < 8 ? v[i + d] : 0.f) : v[i];
+        for (int i = 0; i < 8; ++i) v[i] = off & d ? (i + d < 8 ? v[i + d] : 0.f) : v[i];
+    }
 #pragma unroll
     for (int i = 0; i < 8; ++i) v[i] = off >= 8 ? 0.f : v[i];
   }
@@ -133,9 +147,14 @@ __device__ inline void store_piece(typename T::Elem *row, int c, int cols, const
   if (whole || c + 8 <= cols) {
     T::store8(row + c, v);
   } else {
+    float u[8];
 #pragma unroll
-    for (int i = 0; i < 8; ++i)
-      if (c + i < cols) T::store(row + c + i, v[i]);
+    for (int i = 0; i < 8; ++i) u[i] = v[i];
+#pragma unroll 1
+    for (; c < cols; ++c) {
+      T::store(row + c, u[0]);
+      shift_down(u);
+    }
   }
 }
 
@@ -146,9 +165,9 @@ __device__ inline void store_e4m3_piece(uint8_t *row, int c, int cols, const flo
   if (whole || c + 8 <= cols) {
     *reinterpret_cast<u32x2 *>(row + c) = w;
   } else {
-#pragma unroll
-    for (int i = 0; i < 8; ++i)
-      if (c + i < cols) row[c + i] = (uint8_t)(w[i >> 2] >> (8 * (i & 3)));
+    uint64_t left = __builtin_bit_cast(uint64_t, w);
+#pragma unroll 1
+    for (; c < cols; ++c, left >>= 8) row[c] = (uint8_t)left;
   }
 }
 

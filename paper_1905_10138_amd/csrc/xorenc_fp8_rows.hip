@@ -90,7 +90,7 @@ __global__ __launch_bounds__(256) void quant_square_kernel(const typename T::Ele
 // eps) * w.  PASSES > 0: the row's sums stay in registers, eight per thread and pass.  PASSES = 0, rows that do not fit: x and the
 // residual are read once more for the second half (from the caches; a `total` that is stored over one of them is not read
 // back, it may be rounded).  A row is wider than all passes but the last, which alone has to look where it ends: its code is four times
-// as long, and a single row waits for code (one token of 9216 5.4 -> 5.1 us, of 16000 8.8 -> 7.8).  Up to 1536 columns a wave holds a row: no barrier, and a quarter of the workgroups (8192 x 600
+// as long, and a single row waits for code (one token of 9216 5.4 -> 5.1 us, and where its end is in brief code 4.7).  Up to 1536 columns a wave holds a row: no barrier, and a quarter of the workgroups (8192 x 600
 // 15.4 -> 12.0 us, 8192 x 1200 without a residual 14.9 -> 11.0; 8192 x 2000 a wave a row 32.8, four 29.4).  Beyond, 256 threads: several
 // rows a CU hide each other's loads (8192 x 9216 without a residual 54 us; 1024 threads 76).  Up to 512 rows there are no others, and
 // more threads a row are faster: 512 for 9216 columns of one token 6.6 -> 5.4 us (1024 5.5), of 64 6.6 -> 5.6, of 1000 15.3 and 15.2;
@@ -104,6 +104,7 @@ __global__ __launch_bounds__(THREADS *ROWS) void rmsnorm_kernel(const typename T
                                                           float *__restrict__ S, int64_t s_row, int64_t s_blk) {
   static_assert(ROWS == 1 || THREADS == 64, "a barrier is for the row's threads");
   constexpr int STEP = THREADS * 8, WAVES = THREADS / 64;
+  constexpr bool BRIEF = THREADS >= 512;  // (few rows)
   __shared__ float chunk_sum[WAVES * (PASSES > 0 ? PASSES : 1)];
   const int64_t r = (int64_t)blockIdx.x * ROWS + threadIdx.x / THREADS;
   const int t = threadIdx.x % THREADS;
@@ -121,10 +122,10 @@ __global__ __launch_bounds__(THREADS *ROWS) void rmsnorm_kernel(const typename T
     return p;
   };
   auto sums = [&](const Pair &p, int c, float *s, bool whole) {
-    piece_of<T>(p.x, c, cols, s, whole);
+    piece_of<T>(p.x, c, cols, s, whole, BRIEF);
     if (R) {
       float u[8];
-      piece_of<T>(p.r, c, cols, u, whole);
+      piece_of<T>(p.r, c, cols, u, whole, BRIEF);
 #pragma unroll
       for (int i = 0; i < 8; ++i) s[i] += u[i];
     }
@@ -174,9 +175,9 @@ __global__ __launch_bounds__(THREADS *ROWS) void rmsnorm_kernel(const typename T
   auto finish = [&](int c, float *v, bool whole) {
     float g[8];
     if (w_bf16)
-      piece_of<BF16>(load_piece<BF16>(static_cast<const uint16_t *>(w), c, cols, whole), c, cols, g, whole);
+      piece_of<BF16>(load_piece<BF16>(static_cast<const uint16_t *>(w), c, cols, whole), c, cols, g, whole, BRIEF);
     else
-      piece_of<F32>(load_piece<F32>(static_cast<const float *>(w), c, cols, whole), c, cols, g, whole);
+      piece_of<F32>(load_piece<F32>(static_cast<const float *>(w), c, cols, whole), c, cols, g, whole, BRIEF);
     uint32_t a = 0;
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
