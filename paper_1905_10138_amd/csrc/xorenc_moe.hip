@@ -1,9 +1,9 @@
 // A mixture-of-experts layer for a few tokens: Y = sum over a token's picks of share * W2_e (silu(G_e x) * (U_e x)), with
 // expert weights in e4m3 (a scale per 128 x 128 block) and everything else in 16 or 32 bits.
 //
-// Four launches: the router's logits; the picks (not for very few tokens, whose picks every workgroup finds by itself); the gated
-// activations h of the picked experts; their second product and the sum over picks.  The bytes of the picked experts'
-// weights bound the last two.  Weights go from memory to a ring of stages in LDS (eight lanes fetch 128 bytes of a row; loads to
+// Five launches: the router's logits; the picks (not for very few tokens, whose picks every workgroup finds by itself); the gated
+// activations h of the picked experts; their second product and the sum over picks; the sum of that product's parts (where it
+// has any).  The bytes of the picked experts' weights bound the two products.  Weights go from memory to a ring of stages in LDS (eight lanes fetch 128 bytes of a row; loads to
 // registers, where a lane needs 32 bytes of one row of 16, take the address units twice as long: 250 us for 32 tokens and
 // eight experts of 4096 x 9216, 207 this way), and so do the activations that multiply them.  e4m3 values become bf16 exactly
 // and multiply bf16 terms of the activations (one for bf16 activations, three for fp32, which sum to the value exactly), so
@@ -40,7 +40,6 @@ struct MoeArgs {
   Use *uses;
   uint8_t *pair_tokens;
   float *shares;            // of the pairs
-  uint32_t *tickets;        // of the second product: workgroups that are done with 128 columns of Y, zero before it
   float *parts;             // [splits][T][H rounded up to 128]: their sums
   int splits, row_groups;
   uint16_t *x_terms, *h_terms;  // rows of tokens, and of pairs
@@ -59,16 +58,14 @@ __device__ inline float rest_of_bf16(float v) {
 // ---------------------------------------------------------------------------------------------- router
 
 // Logits in fp32: a workgroup per expert and four tokens, its waves share the columns.  The workgroups behind them write the
-// bf16 terms of x; the first one clears the tickets.
+// bf16 terms of x.
 template <class T, int TERMS>
 __global__ __launch_bounds__(256) void router_kernel(const typename T::Elem *__restrict__ X, int64_t ldx,
                                                      const typename T::Elem *__restrict__ router, int64_t ldr, int tokens,
                                                      int H, int E, float *__restrict__ logits, uint16_t *__restrict__ terms,
-                                                     int logit_groups, uint32_t *__restrict__ tickets, int n_tickets) {
+                                                     int logit_groups) {
   __shared__ float part[4][4];
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  if (blockIdx.x == 0)
-    for (int i = threadIdx.x; i < n_tickets; i += 256) tickets[i] = 0u;
   if ((int)blockIdx.x >= logit_groups) {  // eight columns a thread
     const int pieces = (H + kBlock - 1) / kBlock * 16;
     const int64_t i = (int64_t)(blockIdx.x - logit_groups) * 256 + threadIdx.x;
@@ -123,50 +120,59 @@ __device__ inline uint32_t ordered(float v) {
 }
 __device__ inline float from_ordered(uint32_t k) { return __uint_as_float(k & 0x80000000u ? k & 0x7fffffffu : ~k); }
 
-// A token's picks, by one wave: lane j gets the j-th (`expert`, `share`).
-__device__ inline void picks_of_token(const MoeArgs &g, int t, int lane, int &expert, float &share) {
+// A token's picks, by one wave: lane j gets the j-th (`expert`, `share`).  A lane holds the keys of GROUPS experts, 64 apart; zero, which
+// is no number's key, stands for those that are not there or picked already.
+template <int GROUPS>
+__device__ inline void picks_among(const MoeArgs &g, int t, int lane, int &expert, float &share) {
   const float *const row = g.logits + t * g.E;
-  uint32_t key[4];
-  bool left[4];
+  uint32_t key[GROUPS];
 #pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    const int e = lane + 64 * i;
-    left[i] = e < g.E;
-    key[i] = left[i] ? ordered(row[e]) : 0u;
-  }
-  auto largest = [&]() {  // of the keys that are left, the same on all lanes
-    uint32_t m = 0u;
+  for (int i = 0; i < GROUPS; ++i) key[i] = lane + 64 * i < g.E ? ordered(row[lane + 64 * i]) : 0u;
+  uint32_t own;  // this lane's largest key, and the group that it is in (the first of equals)
+  int group;
+  auto find = [&]() {
+    own = key[0], group = 0;
 #pragma unroll
-    for (int i = 0; i < 4; ++i) m = left[i] ? max(m, key[i]) : m;
-    m = max_of_16_lanes(m);
+    for (int i = 1; i < GROUPS; ++i) {
+      group = key[i] > own ? i : group;
+      own = max(own, key[i]);
+    }
+    const uint32_t m = max_of_16_lanes(own);
     return max(max((uint32_t)__builtin_amdgcn_readlane((int)m, 0), (uint32_t)__builtin_amdgcn_readlane((int)m, 16)),
                max((uint32_t)__builtin_amdgcn_readlane((int)m, 32), (uint32_t)__builtin_amdgcn_readlane((int)m, 48)));
   };
-  const float most = from_ordered(largest());
+  uint32_t largest = find(), mine = 0u;
+  const float most = from_ordered(largest);
   float sum = 0.f;
   if (!g.renormalise) {  // shares of a softmax over all experts
 #pragma unroll
-    for (int i = 0; i < 4; ++i)
-      if (left[i]) sum += expf(from_ordered(key[i]) - most);
-#pragma unroll
-    for (int o = 32; o > 0; o >>= 1) sum += __shfl_xor(sum, o);
+    for (int i = 0; i < GROUPS; ++i)
+      if (key[i]) sum += expf(from_ordered(key[i]) - most);
+    sum = sum_of_wave(sum);
   }
-  expert = 0, share = 0.f;
+  expert = 0;
   for (int j = 0; j < g.top; ++j) {  // the largest that is left; the lowest index of equals
-    const uint32_t m = largest();
     int e = 0;
 #pragma unroll
-    for (int i = 3; i >= 0; --i) {
-      const uint64_t at = __ballot(left[i] && key[i] == m);
+    for (int i = GROUPS - 1; i >= 0; --i) {
+      const uint64_t at = __ballot(own == largest && group == i);
       if (at) e = 64 * i + __builtin_ctzll(at);
     }
+    if (lane == j) expert = e, mine = largest;
 #pragma unroll
-    for (int i = 0; i < 4; ++i) left[i] = left[i] && e != lane + 64 * i;
-    const float v = expf(from_ordered(m) - most);
-    if (g.renormalise) sum += v;
-    if (lane == j) expert = e, share = v;
+    for (int i = 0; i < GROUPS; ++i) key[i] = e == lane + 64 * i ? 0u : key[i];
+    if (j + 1 < g.top) largest = find();
   }
+  share = lane < g.top ? expf(from_ordered(mine) - most) : 0.f;
+  if (g.renormalise) sum = sum_of_wave(share);
   share /= sum;
+}
+
+__device__ inline void picks_of_token(const MoeArgs &g, int t, int lane, int &expert, float &share) {
+  if (g.E <= 64)
+    picks_among<1>(g, t, lane, expert, share);
+  else
+    picks_among<4>(g, t, lane, expert, share);
 }
 
 template <int TOKENS>
@@ -484,7 +490,6 @@ __global__ __launch_bounds__(kDownWaves * 64) void moe_down_kernel(MoeArgs g, ty
   extern __shared__ __attribute__((aligned(1024))) uint8_t down_lds[];
   __shared__ Use uses[XORENC_MOE_MAX_EXPERTS + kMostTokens * kMostPicks / 16];
   __shared__ uint8_t pair_tokens[kMostTokens * kMostPicks];
-  __shared__ uint32_t ticket;
   float *const sums = reinterpret_cast<float *>(down_lds + Shape::RING);  // [token][128 rows]
   const int tid = threadIdx.x, lane = tid & 63, r = lane & 15;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -592,29 +597,33 @@ __global__ __launch_bounds__(kDownWaves * 64) void moe_down_kernel(MoeArgs g, ty
       if (n < g.H) T::store(Y + t * ldy + n, sums[t * 128 + (tid & 127)]);
     return;
   }
-  // ---- the parts' sums, past the L2 (workgroups of other XCDs read them); who comes last adds them, in the order of the parts
   const int64_t row = (int64_t)g.row_groups * 128, part = g.T * row;
-  for (int t = tid >> 7; t < g.T; t += kDownWaves / 2)
-    __hip_atomic_store(g.parts + blockIdx.y * part + t * row + n, sums[t * 128 + (tid & 127)], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-  asm volatile("s_waitcnt vmcnt(0)" ::: "memory");  // (once they are acknowledged the ticket may be taken)
-  __syncthreads();
-  if (tid == 0) ticket = __hip_atomic_fetch_add(g.tickets + blockIdx.x, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-  __syncthreads();
-  if (ticket != (uint32_t)g.splits - 1) return;
-  for (int t = tid >> 7; t < g.T; t += kDownWaves / 2) {
-    const float *const p = g.parts + t * row + n;
-    float v = 0.f;
-    int k = 0;
-    for (; k + 8 <= g.splits; k += 8) {
-      float q[8];
+  for (int i = tid; i < g.T * 32; i += kDownWaves * 64)
+    *reinterpret_cast<f32x4 *>(g.parts + blockIdx.y * part + (i >> 5) * row + n0 + (i & 31) * 4) = *reinterpret_cast<const f32x4 *>(sums + i * 4);
+}
+
+// Adds the parts, in their order: four columns a thread, eight tokens a workgroup.  (The last workgroup of the parts, which a ticket
+// tells that it is the last, takes as long for one token, 36 us with this launch and 37 without for eight of 16 experts of 1024 x 4096,
+// and longer for more: 64 tokens, two of 16 of 512 x 512 31.6 and 52.9.)
+template <class T>
+__global__ __launch_bounds__(256) void moe_join_kernel(MoeArgs g, typename T::Elem *__restrict__ Y, int64_t ldy) {
+  const int t = blockIdx.y * 8 + (threadIdx.x >> 5), n = blockIdx.x * 128 + (threadIdx.x & 31) * 4;
+  if (t >= g.T) return;
+  const int64_t row = (int64_t)g.row_groups * 128, part = g.T * row;
+  const float *const p = g.parts + t * row + n;
+  f32x4 v = {0.f, 0.f, 0.f, 0.f};
+  int k = 0;
+  for (; k + 8 <= g.splits; k += 8) {
+    f32x4 q[8];
 #pragma unroll
-      for (int j = 0; j < 8; ++j) q[j] = __hip_atomic_load(p + (k + j) * part, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    for (int j = 0; j < 8; ++j) q[j] = *reinterpret_cast<const f32x4 *>(p + (k + j) * part);
 #pragma unroll
-      for (int j = 0; j < 8; ++j) v += q[j];
-    }
-    for (; k < g.splits; ++k) v += __hip_atomic_load(p + k * part, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-    if (n < g.H) T::store(Y + t * ldy + n, v);
+    for (int j = 0; j < 8; ++j) v += q[j];
   }
+  for (; k < g.splits; ++k) v += *reinterpret_cast<const f32x4 *>(p + k * part);
+#pragma unroll
+  for (int j = 0; j < 4; ++j)
+    if (n + j < g.H) T::store(Y + t * ldy + n + j, v[j]);
 }
 
 // The same for at most XR <= 4 tokens and rows enough: a workgroup takes 16 rows of W2, and its eight waves take the blocks of
@@ -720,7 +729,7 @@ __global__ __launch_bounds__(kDownWaves * 64) void moe_down_few_kernel(MoeArgs g
 constexpr int64_t round_up(int64_t n, int64_t d) { return (n + d - 1) / d * d; }
 
 struct MoePlan {
-  int64_t logits, n_uses, uses, pair_tokens, shares, tickets, parts, x, h, total;  // bytes: where they start, and in all
+  int64_t logits, n_uses, uses, pair_tokens, shares, parts, x, h, total;  // bytes: where they start, and in all
   int x_row, h_row, most_uses, pass, splits, row_groups;
 };
 
@@ -746,8 +755,7 @@ MoePlan plan_of(int T, int H, int I, int E, int top, int32_t dtype) {
   p.uses = p.n_uses + 16;
   p.pair_tokens = p.uses + p.most_uses * (int64_t)sizeof(Use);
   p.shares = round_up(p.pair_tokens + pairs, 16);
-  p.tickets = p.shares + pairs * 4;
-  p.parts = round_up(p.tickets + p.row_groups * 4, 256);
+  p.parts = round_up(p.shares + pairs * 4, 256);
   p.x = p.parts + (p.splits > 1 ? (int64_t)p.splits * T * p.row_groups * 512 : 0);
   p.h = p.x + (int64_t)T * p.x_row;
   p.total = p.h + (int64_t)pairs * p.h_row;
@@ -783,9 +791,9 @@ void launch_products(const MoeArgs &g, void *Y, int64_t ldy, hipStream_t st) {
   else
     launch_up<XR, TERMS, H_TERMS, (XR == 32 ? 4 : 2), (XR == 32 ? 1 : 2)>(g, st);
   if constexpr (XR == 4) {
-    // No sums across workgroups where each has few steps (us, against the other kernel: one token, six of 64 experts of 2048 x
-    // 1024 21.5 and 22.4, two of 16 of 512 x 512 12.5 and 13.7, four of 16 of 2048 x 4096 34.9 and 33.8; four tokens, two of
-    // 16 of 512 x 512 17.6 and 19.1, eight of 32 of 1024 x 256 24.8 and 23.5)
+    // No sums across workgroups where each has few steps (us, against the other kernels: one token, six of 64 experts of 2048 x
+    // 1024 20.5 and 21.3, two of 16 of 512 x 512 12.1 and 13.9, four of 16 of 2048 x 4096 33.8 and 32.0; four tokens, two of
+    // 16 of 512 x 512 15.9 and 17.0, eight of 32 of 1024 x 256 21.5 and 20.2)
     const int64_t steps = (int64_t)(g.E < g.T * g.top ? g.E : g.T * g.top) * ((g.I + kBlock - 1) / kBlock);
     if (g.T == 1 && steps <= 96) return launch_down_few<T, 1, H_TERMS>(g, Y, ldy, st);
     if (g.T > 1 && steps <= 48) return launch_down_few<T, 4, H_TERMS>(g, Y, ldy, st);
@@ -795,6 +803,9 @@ void launch_products(const MoeArgs &g, void *Y, int64_t ldy, hipStream_t st) {
   static_assert(Shape::RING + kMostTokens * 512 <= 150 * 1024, "a CU's, less what is declared in the kernel");
   hipLaunchKernelGGL((moe_down_kernel<T, XR, H_TERMS, NS>), dim3((unsigned)g.row_groups, (unsigned)g.splits), dim3(kDownWaves * 64),
                      (unsigned)(Shape::RING + g.T * 512), st, g, static_cast<typename T::Elem *>(Y), ldy);
+  if (g.splits > 1)
+    hipLaunchKernelGGL((moe_join_kernel<T>), dim3((unsigned)g.row_groups, (unsigned)((g.T + 7) / 8)), dim3(256), 0, st, g,
+                       static_cast<typename T::Elem *>(Y), ldy);
 }
 
 template <class T, int TERMS, int H_TERMS>
@@ -804,7 +815,7 @@ int32_t launch_moe(const MoeArgs &g, const void *X, int64_t ldx, const void *rou
   const int64_t pieces = (int64_t)g.T * ((g.H + kBlock - 1) / kBlock) * 16;
   hipLaunchKernelGGL((router_kernel<T, TERMS>), dim3((unsigned)(groups + (pieces + 255) / 256)), dim3(256), 0, st,
                      static_cast<const E *>(X), ldx, static_cast<const E *>(router), ldr, g.T, g.H, g.E, g.logits,
-                     g.x_terms, groups, g.tickets, g.row_groups);
+                     g.x_terms, groups);
   if (!g.plans) hipLaunchKernelGGL(picks_kernel, dim3(1), dim3(1024), 0, st, g);
   int32_t rc = xorenc_internal_check_launch();
   if (rc != XORENC_OK) return rc;
@@ -870,7 +881,6 @@ extern "C" int32_t xorenc_moe_fp8(const xorenc_moe *L, const void *X, int32_t x_
   g.uses = reinterpret_cast<Use *>(ws + p.uses);
   g.pair_tokens = ws + p.pair_tokens;
   g.shares = reinterpret_cast<float *>(ws + p.shares);
-  g.tickets = reinterpret_cast<uint32_t *>(ws + p.tickets);
   g.parts = reinterpret_cast<float *>(ws + p.parts);
   g.x_terms = reinterpret_cast<uint16_t *>(ws + p.x);
   g.h_terms = reinterpret_cast<uint16_t *>(ws + p.h);
