@@ -180,15 +180,18 @@ __device__ inline uint32_t max_of_16_lanes(uint32_t v) {
   return v;
 }
 
-// Sum of a wave's values, on all lanes: the same tree wherever the wave is.
-__device__ inline float sum_of_wave(float v) {
+// Sum of 16 neighbouring lanes' values, or of a wave's, on all of them: the same tree wherever they are.
+__device__ inline float sum_of_16_lanes(float v) {
   auto moved = [&](auto pattern) {
     return __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(v), decltype(pattern)::value, 0xf, 0xf, true));
   };
   v += moved(std::integral_constant<int, 0xB1>());
   v += moved(std::integral_constant<int, 0x4E>());
   v += moved(std::integral_constant<int, 0x141>());
-  v += moved(std::integral_constant<int, 0x140>());
+  return v + moved(std::integral_constant<int, 0x140>());
+}
+__device__ inline float sum_of_wave(float v) {
+  v = sum_of_16_lanes(v);
   v += __shfl_xor(v, 16);
   return v + __shfl_xor(v, 32);
 }

@@ -19,7 +19,7 @@ namespace xorenc_fp8_detail {
 namespace {
 
 constexpr int kMostExperts = XORENC_MOE_MAX_EXPERTS, kMostPicks = XORENC_MOE_MAX_PICKS, kMostTokens = XORENC_MOE_MAX_TOKENS;
-static_assert(kMostExperts == 256 && kMostTokens == 64, "four experts per lane, tokens as bits of 64");
+static_assert(kMostExperts == 256 && kMostTokens == 64 && kMostPicks == 16, "four experts per lane, tokens as bits of 64, a pick a lane");
 
 // Tokens that picked an expert, `count` of them (at most as many as one pass multiplies: an expert that more tokens picked has
 // several uses): pairs of a token and an expert that it picked are ordered by expert, then by token, and these are
@@ -120,59 +120,56 @@ __device__ inline uint32_t ordered(float v) {
 }
 __device__ inline float from_ordered(uint32_t k) { return __uint_as_float(k & 0x80000000u ? k & 0x7fffffffu : ~k); }
 
-// A token's picks, by one wave: lane j gets the j-th (`expert`, `share`).  A lane holds the keys of GROUPS experts, 64 apart; zero, which
-// is no number's key, stands for those that are not there or picked already.
-template <int GROUPS>
-__device__ inline void picks_among(const MoeArgs &g, int t, int lane, int &expert, float &share) {
+// A token's picks, by 16 neighbouring lanes (all lanes of a wave take part, for four tokens): lane j gets the j-th (`expert`,
+// `share`).  A lane holds the keys of KEYS experts, 16 apart; zero, which is no number's key, stands for those that are not there or
+// picked already.  (A wave a token, with its maximum by way of scalar registers: 64 tokens, eight of 128 experts 17.7 us and, this
+// way, 8.8.)
+template <int KEYS>
+__device__ inline void picks_among(const MoeArgs &g, int t, int l, int &expert, float &share) {
   const float *const row = g.logits + t * g.E;
-  uint32_t key[GROUPS];
+  uint32_t key[KEYS];
 #pragma unroll
-  for (int i = 0; i < GROUPS; ++i) key[i] = lane + 64 * i < g.E ? ordered(row[lane + 64 * i]) : 0u;
-  uint32_t own;  // this lane's largest key, and the group that it is in (the first of equals)
-  int group;
+  for (int i = 0; i < KEYS; ++i) key[i] = l + 16 * i < g.E ? ordered(row[l + 16 * i]) : 0u;
+  uint32_t own;  // this lane's largest key, and which it is (the first of equals)
+  int which;
   auto find = [&]() {
-    own = key[0], group = 0;
+    own = key[0], which = 0;
 #pragma unroll
-    for (int i = 1; i < GROUPS; ++i) {
-      group = key[i] > own ? i : group;
+    for (int i = 1; i < KEYS; ++i) {
+      which = key[i] > own ? i : which;
       own = max(own, key[i]);
     }
-    const uint32_t m = max_of_16_lanes(own);
-    return max(max((uint32_t)__builtin_amdgcn_readlane((int)m, 0), (uint32_t)__builtin_amdgcn_readlane((int)m, 16)),
-               max((uint32_t)__builtin_amdgcn_readlane((int)m, 32), (uint32_t)__builtin_amdgcn_readlane((int)m, 48)));
+    return max_of_16_lanes(own);
   };
   uint32_t largest = find(), mine = 0u;
   const float most = from_ordered(largest);
   float sum = 0.f;
   if (!g.renormalise) {  // shares of a softmax over all experts
 #pragma unroll
-    for (int i = 0; i < GROUPS; ++i)
+    for (int i = 0; i < KEYS; ++i)
       if (key[i]) sum += expf(from_ordered(key[i]) - most);
-    sum = sum_of_wave(sum);
+    sum = sum_of_16_lanes(sum);
   }
   expert = 0;
   for (int j = 0; j < g.top; ++j) {  // the largest that is left; the lowest index of equals
-    int e = 0;
+    const int e = (int)(kMostExperts - max_of_16_lanes(own == largest ? (uint32_t)(kMostExperts - (l + 16 * which)) : 0u));
+    if (l == j) expert = e, mine = largest;
 #pragma unroll
-    for (int i = GROUPS - 1; i >= 0; --i) {
-      const uint64_t at = __ballot(own == largest && group == i);
-      if (at) e = 64 * i + __builtin_ctzll(at);
-    }
-    if (lane == j) expert = e, mine = largest;
-#pragma unroll
-    for (int i = 0; i < GROUPS; ++i) key[i] = e == lane + 64 * i ? 0u : key[i];
+    for (int i = 0; i < KEYS; ++i) key[i] = e == l + 16 * i ? 0u : key[i];
     if (j + 1 < g.top) largest = find();
   }
-  share = lane < g.top ? expf(from_ordered(mine) - most) : 0.f;
-  if (g.renormalise) sum = sum_of_wave(share);
+  share = l < g.top ? expf(from_ordered(mine) - most) : 0.f;
+  if (g.renormalise) sum = sum_of_16_lanes(share);
   share /= sum;
 }
 
-__device__ inline void picks_of_token(const MoeArgs &g, int t, int lane, int &expert, float &share) {
+__device__ inline void picks_of_token(const MoeArgs &g, int t, int l, int &expert, float &share) {
   if (g.E <= 64)
-    picks_among<1>(g, t, lane, expert, share);
+    picks_among<4>(g, t, l, expert, share);
+  else if (g.E <= 128)
+    picks_among<8>(g, t, l, expert, share);
   else
-    picks_among<4>(g, t, lane, expert, share);
+    picks_among<16>(g, t, l, expert, share);
 }
 
 template <int TOKENS>
@@ -183,21 +180,22 @@ struct Picks {
   uint16_t first[kMostExperts];  // pair of an expert
 };
 
-// The uses in the order of their experts and the pairs in the order of the uses, by a workgroup of WAVES waves, one per token at a
-// time: put_count(uses), put_use(index, use), up to most_uses of them, and put_pair(index, token, share).
+// The uses in the order of their experts and the pairs in the order of the uses, by a workgroup of WAVES waves, each for four tokens
+// at a time: put_count(uses), put_use(index, use), up to most_uses of them, and put_pair(index, token, share).
 template <int WAVES, int TOKENS, class PutCount, class PutUse, class PutPair>
 __device__ inline void plan_uses(const MoeArgs &g, Picks<TOKENS> &p, PutCount put_count, PutUse put_use, PutPair put_pair) {
   const int tid = threadIdx.x, lane = tid & 63;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   if (tid < kMostExperts) p.tokens[tid] = 0u;
   __syncthreads();
-  for (int t = wave; t < g.T; t += WAVES) {
+  for (int t0 = 4 * wave; t0 < g.T; t0 += 4 * WAVES) {
+    const int t = t0 + (lane >> 4), l = lane & 15;
     int e;
     float share;
-    picks_of_token(g, t, lane, e, share);
-    if (lane < g.top) {
-      p.expert[t][lane] = (uint16_t)e;
-      p.share[t][lane] = share;
+    picks_of_token(g, min(t, g.T - 1), l, e, share);
+    if (t < g.T && l < g.top) {
+      p.expert[t][l] = (uint16_t)e;
+      p.share[t][l] = share;
       atomicOr(reinterpret_cast<unsigned long long *>(&p.tokens[e]), 1ull << t);
     }
   }
@@ -298,7 +296,7 @@ __global__ __launch_bounds__(R *S * 64) void moe_up_kernel(MoeArgs g) {
   float share;                     // lane l: of the l-th token
   if (XR == 4 && g.T == 1) {       // the picks are the uses, in their order
     int expert;
-    picks_of_token(g, 0, lane, expert, share);
+    picks_of_token(g, 0, lane & 15, expert, share);
     first = blockIdx.y, count = 1;
     e = __builtin_amdgcn_readlane(expert, first);
     share = __shfl(share, first);
