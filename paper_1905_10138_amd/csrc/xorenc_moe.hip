@@ -4,8 +4,8 @@
 // Five launches: the router's logits; the picks (not for very few tokens, whose picks every workgroup finds by itself); the gated
 // activations h of the picked experts; their second product and the sum over picks; the sum of that product's parts (where it
 // has any).  The bytes of the picked experts' weights bound the two products.  Weights go from memory to a ring of stages in LDS (eight lanes fetch 128 bytes of a row; loads to
-// registers, where a lane needs 32 bytes of one row of 16, take the address units twice as long: 250 us for 32 tokens and
-// eight experts of 4096 x 9216, 207 this way), and so do the activations that multiply them.  e4m3 values become bf16 exactly
+// registers, where a lane needs 32 bytes of one row of 16, take the address units twice as long: 32 tokens and eight experts of
+// 4096 x 9216 250 us, 207 by rings alone and 201 now: 4.5 TB/s of weights over all launches), and so do the activations that multiply them.  e4m3 values become bf16 exactly
 // and multiply bf16 terms of the activations (one for bf16 activations, three for fp32, which sum to the value exactly), so
 // that nothing is rounded to 8 bits on the way; h is kept as bf16 terms that hold 16 (24) bits.  The tokens that picked an
 // expert are the columns of its matrix instructions; rows of tokens that are not there are not loaded.
@@ -742,8 +742,9 @@ MoePlan plan_of(int T, int H, int I, int E, int top, int32_t dtype) {
   p.x_row = (H + kBlock - 1) / kBlock * terms * (2 * kBlock);
   p.h_row = (I + kBlock - 1) / kBlock * h_terms * (2 * kBlock);
   p.row_groups = (H + 127) / 128;
-  // workgroups of the second product: one for each CU (two: 213 against 207 us for 32 tokens and eight experts of 4096 x 9216, 24.9
-  // against 23.5 for one token and six of 2048 x 1024), a block of the reduction each at least, 32 parts at most
+  // workgroups of the second product: one for each CU (two: 205 against 201 us for 32 tokens and eight experts of 4096 x 9216, 33.6
+  // against 32.1 for one token and four of 2048 x 4096), a block of the reduction each at least, 32 parts at most (64: 29 against 26
+  // for 64 tokens and 16 of 512 x 512)
   const int64_t steps = (int64_t)used * ((I + kBlock - 1) / kBlock);
   p.splits = (256 + p.row_groups - 1) / p.row_groups;
   if (p.splits > steps) p.splits = (int)steps;
@@ -781,8 +782,8 @@ void launch_down_few(const MoeArgs &g, void *Y, int64_t ldy, hipStream_t st) {
 template <class T, int XR, int TERMS, int H_TERMS>
 void launch_products(const MoeArgs &g, void *Y, int64_t ldy, hipStream_t st) {
   // Four waves: side by side where x is wide and they share it, in pairs otherwise, and all on the same 16 rows where there
-  // are few of them (us, in this order: 32 tokens, two of eight experts of 4096 x 9216 207, 215, 250; 16 tokens 197, 186,
-  // 191; eight tokens, four of 16 experts of 4096 x 4096 176, 163, 167; one token, six of 2048 x 1024 24, 23, 22.5)
+  // are few of them (us, in this order: 32 tokens, two of eight experts of 4096 x 9216 201, 208, 244; 16 tokens 194, 183,
+  // 190; eight tokens, four of 16 experts of 4096 x 4096 173, 161, 165; one token, six of 2048 x 1024 25, 22, 21)
   const int64_t tiles = (int64_t)((g.I + 15) / 16) * g.most_uses;
   if (tiles < 2048)
     launch_up<XR, TERMS, H_TERMS, 1, 4>(g, st);
