@@ -220,10 +220,16 @@ __device__ inline u32x4 descriptor(const void *p) {
   return u32x4{(uint32_t)__builtin_amdgcn_readfirstlane((int)(uint32_t)a),
                (uint32_t)__builtin_amdgcn_readfirstlane((int)((uint32_t)(a >> 32) & 0xffffu)), (uint32_t)kMostTileBytes, kRawBuffer};
 }
+template <bool STREAM = false>
 __device__ inline void fetch_16(uint32_t to, uint32_t off, const u32x4 &desc, uint32_t more) {
-  asm volatile("s_mov_b32 m0, %0\n\tbuffer_load_dwordx4 %1, %2, %3 offen lds" ::"s"(__builtin_amdgcn_readfirstlane(to)), "v"(off),
-               "s"(desc), "s"(__builtin_amdgcn_readfirstlane(more))
-               : "memory");
+  if constexpr (STREAM)  // not kept in caches
+    asm volatile("s_mov_b32 m0, %0\n\tbuffer_load_dwordx4 %1, %2, %3 offen nt lds" ::"s"(__builtin_amdgcn_readfirstlane(to)), "v"(off),
+                 "s"(desc), "s"(__builtin_amdgcn_readfirstlane(more))
+                 : "memory");
+  else
+    asm volatile("s_mov_b32 m0, %0\n\tbuffer_load_dwordx4 %1, %2, %3 offen lds" ::"s"(__builtin_amdgcn_readfirstlane(to)), "v"(off),
+                 "s"(desc), "s"(__builtin_amdgcn_readfirstlane(more))
+                 : "memory");
 }
 __device__ inline void fetch_4(uint32_t to, uint32_t off, const u32x4 &desc, uint32_t more) {
   asm volatile("s_mov_b32 m0, %0\n\tbuffer_load_dword %1, %2, %3 offen lds" ::"s"(__builtin_amdgcn_readfirstlane(to)), "v"(off),

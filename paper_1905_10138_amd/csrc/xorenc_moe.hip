@@ -283,7 +283,7 @@ struct UpShape {
   static constexpr int LDS = RING > SUMS ? RING : SUMS, LOADS = 4 + PER + 1;
 };
 
-template <int XR, int TERMS, int H_TERMS, int R, int S, int NS>
+template <int XR, int TERMS, int H_TERMS, int R, int S, int NS, bool STREAM>
 __global__ __launch_bounds__(R *S * 64) void moe_up_kernel(MoeArgs g) {
   typedef UpShape<XR, TERMS, R, S, NS> Shape;
   constexpr int N = Shape::N, PER = Shape::PER;
@@ -375,8 +375,8 @@ __global__ __launch_bounds__(R *S * 64) void moe_up_kernel(MoeArgs g) {
 #pragma unroll
     for (int p = 0; p < 2; ++p) {
       const uint32_t off = chunk[p] >= most ? kBeyond : w_at[p];
-      fetch_16(to + rt * 4096 + p * 1024, off, gate_desc, at * kBlock);
-      fetch_16(to + rt * 4096 + 2048 + p * 1024, off, up_desc, at * kBlock);
+      fetch_16<STREAM>(to + rt * 4096 + p * 1024, off, gate_desc, at * kBlock);
+      fetch_16<STREAM>(to + rt * 4096 + 2048 + p * 1024, off, up_desc, at * kBlock);
     }
 #pragma unroll
     for (int j = 0; j < PER; ++j)
@@ -481,7 +481,7 @@ struct DownShape {
   static constexpr int N = XR <= 16 ? 1 : XR / 16, LOADS = 2 + PER + 1;
 };
 
-template <class T, int XR, int H_TERMS, int NS>
+template <class T, int XR, int H_TERMS, int NS, bool STREAM>
 __global__ __launch_bounds__(kDownWaves * 64) void moe_down_kernel(MoeArgs g, typename T::Elem *__restrict__ Y, int64_t ldy) {
   typedef DownShape<XR, H_TERMS, NS> Shape;
   constexpr int N = Shape::N, PER = Shape::PER;
@@ -531,7 +531,7 @@ __global__ __launch_bounds__(kDownWaves * 64) void moe_down_kernel(MoeArgs g, ty
     const int most = s >= s1 ? 0 : tail && fb == blocks - 1 ? tail : kBlock;
     const uint32_t at = most ? (uint32_t)fb : 0u;
 #pragma unroll
-    for (int p = 0; p < 2; ++p) fetch_16(to + wave * 2048 + p * 1024, chunk[p] >= most ? kBeyond : w_at[p], w_desc, at * kBlock);
+    for (int p = 0; p < 2; ++p) fetch_16<STREAM>(to + wave * 2048 + p * 1024, chunk[p] >= most ? kBeyond : w_at[p], w_desc, at * kBlock);
 #pragma unroll
     for (int j = 0; j < PER; ++j)
       fetch_16(to + kDownWaves * 2048 + (x_load(j) % H_TERMS * XR + x_load(j) / H_TERMS * 4) * 256, most ? x_at[j] : kBeyond, h_desc,
@@ -632,7 +632,7 @@ struct FewShape {
   static constexpr int LOADS = 2 + X_LOADS + 1;
 };
 
-template <class T, int XR, int H_TERMS, int NS>
+template <class T, int XR, int H_TERMS, int NS, bool STREAM>
 __global__ __launch_bounds__(kDownWaves * 64) void moe_down_few_kernel(MoeArgs g, typename T::Elem *__restrict__ Y, int64_t ldy) {
   typedef FewShape<XR, H_TERMS, NS> Shape;
   constexpr int X_LOADS = Shape::X_LOADS;
@@ -671,7 +671,7 @@ __global__ __launch_bounds__(kDownWaves * 64) void moe_down_few_kernel(MoeArgs g
     const int most = fs >= steps ? 0 : tail && fb == blocks - 1 ? tail : kBlock;
     const uint32_t at = most ? (uint32_t)fb : 0u;
 #pragma unroll
-    for (int p = 0; p < 2; ++p) fetch_16(to + p * 1024, chunk[p] >= most ? kBeyond : w_at[p], w_desc, at * kBlock);
+    for (int p = 0; p < 2; ++p) fetch_16<STREAM>(to + p * 1024, chunk[p] >= most ? kBeyond : w_at[p], w_desc, at * kBlock);
 #pragma unroll
     for (int j = 0; j < X_LOADS; ++j) {
       const int line = 4 * j + (lane >> 4), row = line % XR, k = line / XR;
@@ -761,46 +761,46 @@ MoePlan plan_of(int T, int H, int I, int E, int top, int32_t dtype) {
   return p;
 }
 
-template <int XR, int TERMS, int H_TERMS, int R, int S>
+template <bool STREAM, int XR, int TERMS, int H_TERMS, int R, int S>
 void launch_up(const MoeArgs &g, hipStream_t st) {
   constexpr int NS = R > 1 && UpShape<XR, TERMS, R, S, 3>::RING <= 80 * 1024 ? 3 : 2;  // (two workgroups a CU, three with R = 1)
   typedef UpShape<XR, TERMS, R, S, NS> Shape;
   static_assert(Shape::LDS <= 160 * 1024, "a CU's");
   const int tiles = (g.I + kBlock - 1) / kBlock * (kBlock / 16);
-  hipLaunchKernelGGL((moe_up_kernel<XR, TERMS, H_TERMS, R, S, NS>), dim3((unsigned)((tiles + R - 1) / R), (unsigned)g.most_uses), dim3(R * S * 64),
+  hipLaunchKernelGGL((moe_up_kernel<XR, TERMS, H_TERMS, R, S, NS, STREAM>), dim3((unsigned)((tiles + R - 1) / R), (unsigned)g.most_uses), dim3(R * S * 64),
                      Shape::LDS, st, g);
 }
 
-template <class T, int XR, int H_TERMS>
+template <bool STREAM, class T, int XR, int H_TERMS>
 void launch_down_few(const MoeArgs &g, void *Y, int64_t ldy, hipStream_t st) {
   constexpr int NS = FewShape<XR, H_TERMS, 4>::RING <= 150 * 1024 ? 4 : 3;
   static_assert(FewShape<XR, H_TERMS, NS>::RING <= 150 * 1024, "a CU's, less what is declared in the kernel");
-  hipLaunchKernelGGL((moe_down_few_kernel<T, XR, H_TERMS, NS>), dim3((unsigned)((g.H + 15) / 16)), dim3(kDownWaves * 64),
+  hipLaunchKernelGGL((moe_down_few_kernel<T, XR, H_TERMS, NS, STREAM>), dim3((unsigned)((g.H + 15) / 16)), dim3(kDownWaves * 64),
                      (FewShape<XR, H_TERMS, NS>::RING), st, g, static_cast<typename T::Elem *>(Y), ldy);
 }
 
-template <class T, int XR, int TERMS, int H_TERMS>
+template <bool STREAM, class T, int XR, int TERMS, int H_TERMS>
 void launch_products(const MoeArgs &g, void *Y, int64_t ldy, hipStream_t st) {
   // Four waves: side by side where x is wide and they share it, in pairs otherwise, and all on the same 16 rows where there
   // are few of them (us, in this order: 32 tokens, two of eight experts of 4096 x 9216 201, 208, 244; 16 tokens 194, 183,
   // 190; eight tokens, four of 16 experts of 4096 x 4096 173, 161, 165; one token, six of 2048 x 1024 25, 22, 21)
   const int64_t tiles = (int64_t)((g.I + 15) / 16) * g.most_uses;
   if (tiles < 2048)
-    launch_up<XR, TERMS, H_TERMS, 1, 4>(g, st);
+    launch_up<STREAM, XR, TERMS, H_TERMS, 1, 4>(g, st);
   else
-    launch_up<XR, TERMS, H_TERMS, (XR == 32 ? 4 : 2), (XR == 32 ? 1 : 2)>(g, st);
+    launch_up<STREAM, XR, TERMS, H_TERMS, (XR == 32 ? 4 : 2), (XR == 32 ? 1 : 2)>(g, st);
   if constexpr (XR == 4) {
     // No sums across workgroups where each has few steps (us, against the other kernels: one token, six of 64 experts of 2048 x
     // 1024 20.5 and 21.3, two of 16 of 512 x 512 12.1 and 13.9, four of 16 of 2048 x 4096 33.8 and 32.0; four tokens, two of
     // 16 of 512 x 512 15.9 and 17.0, eight of 32 of 1024 x 256 21.5 and 20.2)
     const int64_t steps = (int64_t)(g.E < g.T * g.top ? g.E : g.T * g.top) * ((g.I + kBlock - 1) / kBlock);
-    if (g.T == 1 && steps <= 96) return launch_down_few<T, 1, H_TERMS>(g, Y, ldy, st);
-    if (g.T > 1 && steps <= 48) return launch_down_few<T, 4, H_TERMS>(g, Y, ldy, st);
+    if (g.T == 1 && steps <= 96) return launch_down_few<STREAM, T, 1, H_TERMS>(g, Y, ldy, st);
+    if (g.T > 1 && steps <= 48) return launch_down_few<STREAM, T, 4, H_TERMS>(g, Y, ldy, st);
   }
   constexpr int NS = 3;
   typedef DownShape<XR, H_TERMS, NS> Shape;
   static_assert(Shape::RING + kMostTokens * 512 <= 150 * 1024, "a CU's, less what is declared in the kernel");
-  hipLaunchKernelGGL((moe_down_kernel<T, XR, H_TERMS, NS>), dim3((unsigned)g.row_groups, (unsigned)g.splits), dim3(kDownWaves * 64),
+  hipLaunchKernelGGL((moe_down_kernel<T, XR, H_TERMS, NS, STREAM>), dim3((unsigned)g.row_groups, (unsigned)g.splits), dim3(kDownWaves * 64),
                      (unsigned)(Shape::RING + g.T * 512), st, g, static_cast<typename T::Elem *>(Y), ldy);
   if (g.splits > 1)
     hipLaunchKernelGGL((moe_join_kernel<T>), dim3((unsigned)g.row_groups, (unsigned)((g.T + 7) / 8)), dim3(256), 0, st, g,
@@ -819,12 +819,23 @@ int32_t launch_moe(const MoeArgs &g, const void *X, int64_t ldx, const void *rou
   int32_t rc = xorenc_internal_check_launch();
   if (rc != XORENC_OK) return rc;
   constexpr int MOST = pass_of(TERMS > 1);
-  if (g.T <= 4)
-    launch_products<T, 4, TERMS, H_TERMS>(g, Y, ldy, st);
-  else if (g.T <= 16)
-    launch_products<T, 16, TERMS, H_TERMS>(g, Y, ldy, st);
+  // From 96 MB of weights on they are read past the caches, which would not hold them until the next call (us: 8 tokens, four of
+  // 16 experts of 4096 x 4096 148 and 161, one token 56 and 60, 32 tokens, two of eight of 4096 x 9216 188 and 201, eight tokens, four of
+  // 64 of 1024 x 1024 34.9 and 36.3; one token, six of 64 of 2048 x 1024, 38 MB, 21.7 and 21.0)
+  const int64_t used = g.E < g.T * g.top ? g.E : g.T * g.top;
+  auto products = [&](auto stream) {
+    constexpr bool STREAM = decltype(stream)::value;
+    if (g.T <= 4)
+      launch_products<STREAM, T, 4, TERMS, H_TERMS>(g, Y, ldy, st);
+    else if (g.T <= 16)
+      launch_products<STREAM, T, 16, TERMS, H_TERMS>(g, Y, ldy, st);
+    else
+      launch_products<STREAM, T, MOST, TERMS, H_TERMS>(g, Y, ldy, st);
+  };
+  if (used * g.H * g.I * 3 >= (int64_t)96 << 20)
+    products(std::true_type());
   else
-    launch_products<T, MOST, TERMS, H_TERMS>(g, Y, ldy, st);
+    products(std::false_type());
   return xorenc_internal_check_launch();
 }
 

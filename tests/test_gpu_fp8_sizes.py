@@ -162,3 +162,41 @@ def test_what_is_not_finite_stays_with_its_token():
         Y = xe.moe_fp8(bad, router, W13, S13, W2, S2, 3)
         keep = torch.arange(T, device=DEV) != t
         assert torch.equal(Y[keep], clean[keep]) and torch.isnan(Y[~keep]).all()
+
+
+# 96 MB of weights and more are read another way: the same values as those of each token
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("T,H,I,E,n", [(1, 4096, 4100, 2, 2), (4, 4000, 2100, 5, 2), (9, 4096, 2048, 4, 2), (40, 2048, 2050, 9, 3)])
+def test_experts_of_many_bytes(T, H, I, E, n, dtype):
+    g = torch.Generator(device=DEV).manual_seed(T)
+
+    def weights(*shape):
+        q = (torch.randn(shape, generator=g, device=DEV) * 60).clamp(-448, 448).to(F8)
+        ld = -(-shape[-1] // 16) * 16
+        out = torch.full((*shape[:-1], ld), 0x7F, dtype=torch.uint8, device=DEV)
+        out[..., :shape[-1]] = q.view(torch.uint8)
+        blocks = (shape[0], -(-shape[1] // 128), -(-shape[2] // 128))
+        return out.view(F8)[..., :shape[-1]], torch.exp2(torch.randn(blocks, generator=g, device=DEV)) / 60 / shape[-1] ** 0.5
+
+    def dense(q, s):
+        return q.double() * s.double().repeat_interleave(128, 0)[:q.shape[0]].repeat_interleave(128, 1)[:, :q.shape[1]]
+    x = torch.randn((T, H), generator=g, device=DEV).to(dtype)
+    router = (torch.randn((E, H), generator=g, device=DEV) * 2 / H ** 0.5).to(dtype)
+    (W13, S13), (W2, S2) = weights(E, 2 * I, H), weights(E, H, I)
+    Y = xe.moe_fp8(x, router, W13, S13, W2, S2, n)
+    shares, chosen = torch.softmax(x.double() @ router.double().t(), 1).topk(n, 1)
+    shares = shares / shares.sum(1, keepdim=True)
+    want, mag = torch.zeros((2, T, H), dtype=torch.float64, device=DEV)
+    for e in range(E):
+        w13, w2 = dense(W13[e], S13[e]), dense(W2[e], S2[e])
+        gate, up = (x.double() @ w13.t()).chunk(2, 1)
+        h = gate * torch.sigmoid(gate) * up
+        f = (shares * (chosen == e)).sum(1, keepdim=True)
+        want += f * (h @ w2.t())
+        mag += f * (h.abs() @ w2.abs().t())
+    err = (Y.double() - want).abs()
+    if dtype is torch.bfloat16:
+        assert (err <= 2.0 ** -8 * 1.01 * want.abs() + 2.0 ** -15 * mag).all()
+        assert err.norm() <= (2.0 ** -8 + 2.0 ** -14) * want.norm()
+    else:
+        assert (err <= 2.0 ** -18 * mag).all() and err.norm() <= 4e-6 * want.norm()
