@@ -3,10 +3,10 @@
 //
 // Five launches: the router's logits; the picks (not for very few tokens, whose picks every workgroup finds by itself); the gated
 // activations h of the picked experts; their second product and the sum over picks; the sum of that product's parts (where it
-// has any).  The bytes of the picked experts' weights bound the two products.  Weights go from memory to a ring of stages in LDS (eight lanes fetch 128 bytes of a row; loads to
-// registers, where a lane needs 32 bytes of one row of 16, take the address units twice as long: 32 tokens and eight experts of
-// 4096 x 9216 250 us, 207 by rings alone and 201 now: 4.5 TB/s of weights over all launches), and so do the activations that multiply them.  e4m3 values become bf16 exactly
-// and multiply bf16 terms of the activations (one for bf16 activations, three for fp32, which sum to the value exactly), so
+// has any).  The bytes of the picked experts' weights bound the two products (32 tokens, two of eight experts of 4096 x 9216: 181 us,
+// 5.0 TB/s over all launches).  Weights go from memory to a ring of stages in LDS (eight lanes fetch 128 bytes of a row; loads to
+// registers, where a lane needs 32 bytes of one row of 16, take the address units twice as long: the same call 250 us, 207 by
+// rings alone), and so do the activations that multiply them.  e4m3 values become bf16 exactly and multiply bf16 terms of the activations (one for bf16 activations, three for fp32, which sum to the value exactly), so
 // that nothing is rounded to 8 bits on the way; h is kept as bf16 terms that hold 16 (24) bits.  The tokens that picked an
 // expert are the columns of its matrix instructions; rows of tokens that are not there are not loaded.
 //
