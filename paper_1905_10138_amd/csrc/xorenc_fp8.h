@@ -159,11 +159,15 @@ __device__ inline void store_piece(typename T::Elem *row, int c, int cols, const
 }
 
 // Eight values as e4m3 to row[c ..].  Rows of Q start on 16-byte boundaries and c is a multiple of eight.
+template <bool STREAM = false>
 __device__ inline void store_e4m3_piece(uint8_t *row, int c, int cols, const float *v, float inv, bool whole = false) {
   const u32x2 w = {pack_e4m3(v[0] * inv, v[1] * inv, v[2] * inv, v[3] * inv),
                    pack_e4m3(v[4] * inv, v[5] * inv, v[6] * inv, v[7] * inv)};
   if (whole || c + 8 <= cols) {
-    *reinterpret_cast<u32x2 *>(row + c) = w;
+    if constexpr (STREAM)
+      __builtin_nontemporal_store(w, reinterpret_cast<u32x2 *>(row + c));
+    else
+      *reinterpret_cast<u32x2 *>(row + c) = w;
   } else {
     uint64_t left = __builtin_bit_cast(uint64_t, w);
 #pragma unroll 1

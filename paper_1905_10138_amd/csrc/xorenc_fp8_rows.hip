@@ -6,8 +6,8 @@
 // (8192 x 1501 with a residual 22 us; value by value, where rows are not on 16-byte boundaries, 52).
 //
 // us and GB/s read and written (a copy of 1 GB: 5160): rows of 33 x 9216 fp32 5 (the call's time on the host), of 8192 x 5001 bf16
-// 26, 4840; squares of 16384 x 4096 bf16 35, 5660; the gates of 8192 x 9216 bf16 65, 5800; the norm of 8192 x 6000 bf16 with a
-// residual 66, 5250.
+// 26, 4840; squares of 16384 x 4096 bf16 36, 5600; the gates of 8192 x 9216 bf16 65, 5850; the norm of 8192 x 6000 bf16 with a
+// residual 66, 5210.
 #include <type_traits>
 
 #include "xorenc_fp8.h"
@@ -42,7 +42,7 @@ __global__ __launch_bounds__(256) void quant_rows_kernel(const typename T::Elem 
 #pragma unroll
   for (int i = 0; i < 8; ++i) a = max(a, magnitude_bits(v[i]));
   const float s = block_scale(max_of_16_lanes(a));
-  store_e4m3_piece(Q + r * ldq, c, cols, v, 1.f / s);
+  store_e4m3_piece<STREAM>(Q + r * ldq, c, cols, v, 1.f / s);
   if (l == 0) S[r * s_row + kb * s_blk] = s;
 }
 
@@ -81,7 +81,7 @@ __global__ __launch_bounds__(256) void quant_square_kernel(const typename T::Ele
   for (int p = 0; p < 8; ++p) {
     const int r = r0 + 16 * p;
     piece_of<T>(x[p], c, cols, v);
-    if (r < rows) store_e4m3_piece(Q + r * ldq, c, cols, v, inv);
+    if (r < rows) store_e4m3_piece<STREAM>(Q + r * ldq, c, cols, v, inv);
   }
   if (threadIdx.x == 0) S[blockIdx.y * s_mat + rb * s_row + kb * s_blk] = s;
 }
@@ -186,7 +186,7 @@ __global__ __launch_bounds__(THREADS *ROWS) void rmsnorm_kernel(const typename T
     }
     const float sc = block_scale(max_of_16_lanes(a));
     if (!whole && c >= cols) return;
-    store_e4m3_piece(Q + r * ldq, c, cols, v, 1.f / sc, whole);
+    store_e4m3_piece<STREAM>(Q + r * ldq, c, cols, v, 1.f / sc, whole);
     if ((t & 15) == 0) S[r * s_row + (int64_t)(c / kBlock) * s_blk] = sc;
     if (Y) {
       if (y_col == 1) {
@@ -223,11 +223,12 @@ int32_t launch_rows(const void *X, const void *up, int64_t ldx, int64_t rows, in
   return xorenc_internal_check_launch();
 }
 
-// Calls that move more than the memory-side cache holds (256 MB) would find nothing there when they run again, and read past it:
-// 8192 x 6000 with a residual 65 us and, with plain loads, 71; the gates of 8192 x 9216 65 and 69; 16384 x 9000 to squares 99
-// and 122.  Below, such loads cost (8192 x 4096 42.7 and 42.0, 2048 x 6000 21.3 and 17.3), and where two of them share a line: rows of
-// fp32, of which a lane takes 32 bytes (8192 x 9216 with a residual 202 and 185; a square's other rows hide it, 162 and 181).
-inline bool streams(int64_t values, int64_t bytes) { return values > ((int64_t)256 << 20) / bytes; }
+// Calls that move more than half of what the memory-side cache holds (256 MB) would find little there when they run again, and read
+// and write their 8 bits past it (into two outputs in turn): 8192 x 6000 with a residual 66 us and, with plain loads, 71; 2500 x 9216 34
+// and 37; the gates of 8192 x 9216 65 and 69; 16384 x 4096 to squares 36 and 39.  Below, such loads cost (4096 x 4096 with a residual
+// 23.9 and 23.1, 8192 x 4096 to squares 19.5 and 18.2), and where two of them share a line: rows of fp32, of which a lane takes 32 bytes (8192 x
+// 9216 with a residual 202 and 185; a square's other rows hide it, 162 and 181).
+inline bool streams(int64_t values, int64_t bytes) { return values > ((int64_t)128 << 20) / bytes; }
 
 // f(type, whether to stream)
 template <class F>
