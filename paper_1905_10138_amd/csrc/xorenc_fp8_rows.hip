@@ -90,11 +90,13 @@ __global__ __launch_bounds__(256) void quant_square_kernel(const typename T::Ele
 // eps) * w.  PASSES > 0: the row's sums stay in registers, eight per thread and pass.  PASSES = 0, rows that do not fit: x and the
 // residual are read once more for the second half (from the caches; a `total` that is stored over one of them is not read
 // back, it may be rounded).  A row is wider than all passes but the last, which alone has to look where it ends: its code is four times
-// as long, and a single row waits for code (one token of 9216 5.4 -> 5.1 us, and where its end is in brief code 4.7).  Up to 1536 columns a wave holds a row: no barrier, and a quarter of the workgroups (8192 x 600
-// 15.4 -> 12.0 us, 8192 x 1200 without a residual 14.9 -> 11.0; 8192 x 2000 a wave a row 32.8, four 29.4).  Beyond, 256 threads: several
-// rows a CU hide each other's loads (8192 x 9216 without a residual 54 us; 1024 threads 76).  Up to 512 rows there are no others, and
-// more threads a row are faster: 512 for 9216 columns of one token 6.6 -> 5.4 us (1024 5.5), of 64 6.6 -> 5.6, of 1000 15.3 and 15.2;
-// 1024 for 16000 columns of one token 7.8 -> 5.0, of 500 14.9 -> 12.9; 256, not a wave, for 500 x 1500 5.6 -> 4.2.
+// as long, and a single row waits for code (one token of 9216 5.4 -> 5.1 us, and where its end is in brief code 4.7).
+//
+// Up to 1536 columns a wave holds a row: no barrier, and a quarter of the workgroups (8192 x 600 15.4 -> 12.0 us, 8192 x 1200
+// without a residual 14.9 -> 11.0; 8192 x 2000 a wave a row 32.8, four 29.4).  Beyond, 256 threads: several rows a CU hide each
+// other's loads (8192 x 9216 without a residual 54 us; 1024 threads 76).  Up to 512 rows there are no others, and more threads a row
+// are faster: 512 for 9216 columns of one token 6.6 -> 5.4 us (1024 5.5), of 64 6.6 -> 5.6, of 1000 15.3 and 15.2; 1024 for 16000
+// columns of one token 7.8 -> 5.0, of 500 14.9 -> 12.9; 256, not a wave, for 500 x 1500 5.6 -> 4.2.
 template <class T, int THREADS, int PASSES, int ROWS, bool STREAM>
 __global__ __launch_bounds__(THREADS *ROWS) void rmsnorm_kernel(const typename T::Elem *X, int64_t ldx,
                                                           const typename T::Elem *R, int64_t ldr, const void *__restrict__ w,

@@ -6,9 +6,10 @@
 // has any).  The bytes of the picked experts' weights bound the two products (32 tokens, two of eight experts of 4096 x 9216: 181 us,
 // 5.0 TB/s over all launches).  Weights go from memory to a ring of stages in LDS (eight lanes fetch 128 bytes of a row; loads to
 // registers, where a lane needs 32 bytes of one row of 16, take the address units twice as long: the same call 250 us, 207 by
-// rings alone), and so do the activations that multiply them.  e4m3 values become bf16 exactly and multiply bf16 terms of the activations (one for bf16 activations, three for fp32, which sum to the value exactly), so
-// that nothing is rounded to 8 bits on the way; h is kept as bf16 terms that hold 16 (24) bits.  The tokens that picked an
-// expert are the columns of its matrix instructions; rows of tokens that are not there are not loaded.
+// rings alone), and so do the activations that multiply them.  e4m3 values become bf16 exactly and multiply bf16 terms of the
+// activations (one for bf16 activations, three for fp32, which sum to the value exactly), so that nothing is rounded to 8 bits on
+// the way; h is kept as bf16 terms that hold 16 (24) bits.  The tokens that picked an expert are the columns of its matrix
+// instructions; rows of tokens that are not there are not loaded.
 //
 // Terms of x and h lie in the workspace in the order in which they are used: a row is a run of blocks of 128 columns (zero
 // behind the last column), a block its terms one after the other, a term the columns 16 g + 64 p + 8 h + 0..7 at 64 p + 32 h + 8 g:

@@ -1,6 +1,6 @@
 // The calls on 8-bit matrices for torch tensors: checks of arguments, new tensors for the results, the current stream.  A
 // Python extension, because these calls often take less time on the GPU than their arguments take in Python (silu(gate) * up
-// of one token: 6.5 us a call through ctypes, 4.4 so, of which the launch is 3).
+// of one token: 6.5 us a call through ctypes, 3.8 so, of which the launch is 3).
 #define PY_SSIZE_T_CLEAN
 #include <Python.h>
 
@@ -44,8 +44,8 @@ struct Place {
 };
 
 // The new tensors of a call.  Where they are small they share one allocation, at 256-byte boundaries: a tensor in it takes 0.15 us,
-// one of its own 0.5 (the norm of one token with a residual and normed values 6.0 -> 4.3 us of host time).  Large ones, whose memory one may want back
-// before the others', have their own.
+// one of its own 0.5 (the norm of one token with a residual and normed values 6.0 -> 4.3 us of host time).  Large ones, whose
+// memory one may want back before the others', have their own.
 class Fresh {
   static constexpr int64_t kShared = 1 << 20;
   const Place &place;
