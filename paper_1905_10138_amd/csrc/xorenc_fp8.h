@@ -215,7 +215,8 @@ __device__ inline u32x4 first_bytes(u32x4 v, int left) {
 }
 
 // Loads from memory to LDS: lane l's 16 (4) bytes at descriptor + off + more go to to + 16 l (4 l).  The compiler does not know
-// of them: who reads the LDS waits for them with s_waitcnt vmcnt, as many later ones left out as it knows of.
+// of them: who reads the LDS waits for them with s_waitcnt vmcnt, as many later ones left out as it knows of.  Nor does it look
+// after the wait state that such a load needs behind the instruction that writes m0.
 constexpr uint32_t kRawBuffer = 0x00020000u;    // descriptor word 3: untyped data
 constexpr uint32_t kBeyond = 0x80000000u;       // an offset past every descriptor's extent: reads as zero, from nowhere
 constexpr int64_t kMostTileBytes = 0x7fffff00;  // extent of the descriptors
@@ -227,18 +228,18 @@ __device__ inline u32x4 descriptor(const void *p) {
 template <bool STREAM = false>
 __device__ inline void fetch_16(uint32_t to, uint32_t off, const u32x4 &desc, uint32_t more) {
   if constexpr (STREAM)  // not kept in caches
-    asm volatile("s_mov_b32 m0, %0\n\tbuffer_load_dwordx4 %1, %2, %3 offen nt lds" ::"s"(__builtin_amdgcn_readfirstlane(to)), "v"(off),
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, %3 offen nt lds" ::"s"(__builtin_amdgcn_readfirstlane(to)), "v"(off),
                  "s"(desc), "s"(__builtin_amdgcn_readfirstlane(more))
-                 : "memory");
+                 : "memory", "m0");
   else
-    asm volatile("s_mov_b32 m0, %0\n\tbuffer_load_dwordx4 %1, %2, %3 offen lds" ::"s"(__builtin_amdgcn_readfirstlane(to)), "v"(off),
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, %3 offen lds" ::"s"(__builtin_amdgcn_readfirstlane(to)), "v"(off),
                  "s"(desc), "s"(__builtin_amdgcn_readfirstlane(more))
-                 : "memory");
+                 : "memory", "m0");
 }
 __device__ inline void fetch_4(uint32_t to, uint32_t off, const u32x4 &desc, uint32_t more) {
-  asm volatile("s_mov_b32 m0, %0\n\tbuffer_load_dword %1, %2, %3 offen lds" ::"s"(__builtin_amdgcn_readfirstlane(to)), "v"(off),
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dword %1, %2, %3 offen lds" ::"s"(__builtin_amdgcn_readfirstlane(to)), "v"(off),
                "s"(desc), "s"(__builtin_amdgcn_readfirstlane(more))
-               : "memory");
+               : "memory", "m0");
 }
 __device__ inline uint32_t lds_address(const void *p) {
   return __builtin_amdgcn_readfirstlane((uint32_t)(size_t)(__attribute__((address_space(3))) const uint8_t *)p);
