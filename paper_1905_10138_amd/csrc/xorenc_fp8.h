@@ -216,7 +216,9 @@ __device__ inline u32x4 first_bytes(u32x4 v, int left) {
 
 // Loads from memory to LDS: lane l's 16 (4) bytes at descriptor + off + more go to to + 16 l (4 l).  The compiler does not know
 // of them: who reads the LDS waits for them with s_waitcnt vmcnt, as many later ones left out as it knows of.  Nor does it look
-// after the wait state that such a load needs behind the instruction that writes m0.
+// after the wait states that such a load needs: one behind the instruction that writes m0, and five behind a vector instruction
+// that writes a scalar register it reads (the descriptor, `more`: v_readfirstlane, or one that the compiler restores from a vector
+// register).  s_mov and s_nop 3 are five (64 x 16384 x 4096 14.5 us; with s_nop 0, for m0 alone, 14.3).
 constexpr uint32_t kRawBuffer = 0x00020000u;    // descriptor word 3: untyped data
 constexpr uint32_t kBeyond = 0x80000000u;       // an offset past every descriptor's extent: reads as zero, from nowhere
 constexpr int64_t kMostTileBytes = 0x7fffff00;  // extent of the descriptors
@@ -228,16 +230,16 @@ __device__ inline u32x4 descriptor(const void *p) {
 template <bool STREAM = false>
 __device__ inline void fetch_16(uint32_t to, uint32_t off, const u32x4 &desc, uint32_t more) {
   if constexpr (STREAM)  // not kept in caches
-    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, %3 offen nt lds" ::"s"(__builtin_amdgcn_readfirstlane(to)), "v"(off),
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 3\n\tbuffer_load_dwordx4 %1, %2, %3 offen nt lds" ::"s"(__builtin_amdgcn_readfirstlane(to)), "v"(off),
                  "s"(desc), "s"(__builtin_amdgcn_readfirstlane(more))
                  : "memory", "m0");
   else
-    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, %3 offen lds" ::"s"(__builtin_amdgcn_readfirstlane(to)), "v"(off),
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 3\n\tbuffer_load_dwordx4 %1, %2, %3 offen lds" ::"s"(__builtin_amdgcn_readfirstlane(to)), "v"(off),
                  "s"(desc), "s"(__builtin_amdgcn_readfirstlane(more))
                  : "memory", "m0");
 }
 __device__ inline void fetch_4(uint32_t to, uint32_t off, const u32x4 &desc, uint32_t more) {
-  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dword %1, %2, %3 offen lds" ::"s"(__builtin_amdgcn_readfirstlane(to)), "v"(off),
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 3\n\tbuffer_load_dword %1, %2, %3 offen lds" ::"s"(__builtin_amdgcn_readfirstlane(to)), "v"(off),
                "s"(desc), "s"(__builtin_amdgcn_readfirstlane(more))
                : "memory", "m0");
 }

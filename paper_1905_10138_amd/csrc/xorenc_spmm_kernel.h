@@ -290,7 +290,8 @@ __global__ __launch_bounds__(NW * 64, (NW == 4 && XFAST && !XF32) ? 2 : 1) void 
   const uint32_t x_lane_off = (uint32_t)(xrow * row_bytes) + ((col0 + xch * EPC < B) ? xch * 16 : 0);
   const uint32_t x_lds_off = XFAST ? (uint32_t)(xrow * RSB + xch * 16) : (uint32_t)(lane * RSB);
   // direct global -> LDS copy of slice s into this wave's slice buffer (XDIR)
-  // (a load to LDS needs a wait state behind the instruction that writes m0; the compiler does not look into assembly)
+  // (A load to LDS needs a wait state behind the instruction that writes m0, and five behind a vector instruction that writes a scalar
+  // register it reads, such as one restored from a vector register: s_mov and s_nop 3.  The compiler does not look into assembly.)
   const uint64_t x_base = reinterpret_cast<uint64_t>(static_cast<const uint8_t *>(Xv) + (int64_t)col0 * ESZ);
   const u32x4 xdesc = {(uint32_t)x_base, (uint32_t)(x_base >> 32) & 0xffffu, x_extent, kRsrcFlags};
   const uint32_t xbuf_lds = __builtin_amdgcn_readfirstlane(
@@ -301,7 +302,7 @@ __global__ __launch_bounds__(NW * 64, (NW == 4 && XFAST && !XF32) ? 2 : 1) void 
     for (int i = 0; i < NCH; ++i) {
       const uint32_t so = __builtin_amdgcn_readfirstlane(sbase + (uint32_t)(row_of_pos(i << LB) * row_bytes));
       const uint32_t dst = __builtin_amdgcn_readfirstlane(xbuf_lds + (uint32_t)(i * 1024));
-      asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, %3 offen lds" ::"s"(dst), "v"(x_lane_off),
+      asm volatile("s_mov_b32 m0, %0\n\ts_nop 3\n\tbuffer_load_dwordx4 %1, %2, %3 offen lds" ::"s"(dst), "v"(x_lane_off),
                    "s"(xdesc), "s"(so)
                    : "memory", "m0");
     }
@@ -422,7 +423,7 @@ __global__ __launch_bounds__(NW * 64, (NW == 4 && XFAST && !XF32) ? 2 : 1) void 
   const uint32_t cbuf_lds = __builtin_amdgcn_readfirstlane(
       (uint32_t)(size_t)(__attribute__((address_space(3))) uint32_t *)(cbuf));
   auto dma_dword = [&](uint32_t lds_addr, uint32_t lane_off, const u32x4 &desc, uint32_t so) {
-    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dword %1, %2, %3 offen lds" ::"s"(
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 3\n\tbuffer_load_dword %1, %2, %3 offen lds" ::"s"(
                      __builtin_amdgcn_readfirstlane(lds_addr)),
                  "v"(lane_off), "s"(desc), "s"(__builtin_amdgcn_readfirstlane(so))
                  : "memory", "m0");

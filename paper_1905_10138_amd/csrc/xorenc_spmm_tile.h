@@ -111,11 +111,12 @@ __global__ __launch_bounds__(WR *KG * 64, 2) void spmm_tile_kernel(DevLayer L, c
   const uint32_t x_dst = __builtin_amdgcn_readfirstlane(xbufs_lds + (uint32_t)(first_load * 1024));
   uint32_t x_next = __builtin_amdgcn_readfirstlane((uint32_t)(k0 * 64 * row_bytes));  // the slice to be fetched next
   const uint32_t x_step = __builtin_amdgcn_readfirstlane((uint32_t)(64 * row_bytes));
-  // (a load to LDS needs a wait state behind the instruction that writes m0; the compiler does not look into assembly)
+  // (A load to LDS needs a wait state behind the instruction that writes m0, and five behind a vector instruction that writes a scalar
+  // register it reads, such as one restored from a vector register: s_mov and s_nop 3.  The compiler does not look into assembly.)
   auto dma_x = [&](uint32_t buf_off) {  // the next slice of X, this wave's part
 #pragma unroll
     for (int i = 0; i < PERX; ++i)
-      asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, %3 offen lds" ::"s"(x_dst + buf_off + i * 1024),
+      asm volatile("s_mov_b32 m0, %0\n\ts_nop 3\n\tbuffer_load_dwordx4 %1, %2, %3 offen lds" ::"s"(x_dst + buf_off + i * 1024),
                    "v"(x_lane_off), "s"(xdesc), "s"(x_next + x_row[i])
                    : "memory", "m0");
     x_next += x_step;
@@ -129,7 +130,7 @@ __global__ __launch_bounds__(WR *KG * 64, 2) void spmm_tile_kernel(DevLayer L, c
   const uint32_t comp_lds = __builtin_amdgcn_readfirstlane(
       (uint32_t)(size_t)(__attribute__((address_space(3))) uint32_t *)(comp));
   auto dma_dword = [&](uint32_t lds_addr, const u32x4 &desc, uint32_t so) {  // 64 consecutive dwords
-    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dword %1, %2, %3 offen lds" ::"s"(
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 3\n\tbuffer_load_dword %1, %2, %3 offen lds" ::"s"(
                      __builtin_amdgcn_readfirstlane(lds_addr)),
                  "v"(lane * 4), "s"(desc), "s"(__builtin_amdgcn_readfirstlane(so))
                  : "memory", "m0");
@@ -143,7 +144,7 @@ __global__ __launch_bounds__(WR *KG * 64, 2) void spmm_tile_kernel(DevLayer L, c
     const uint32_t dst = comp_lds + (gi & 1) * Lds::COMP;
 #pragma unroll
     for (int rb = 0; rb < RB; ++rb) {
-      asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, %3 offen lds" ::"s"(
+      asm volatile("s_mov_b32 m0, %0\n\ts_nop 3\n\tbuffer_load_dwordx4 %1, %2, %3 offen lds" ::"s"(
                        __builtin_amdgcn_readfirstlane(dst + rb * 1024)),
                    "v"(lane * 16), "s"(mdesc),
                    "s"(__builtin_amdgcn_readfirstlane((uint32_t)((rb0 + rb) * l_spr + s) * 256u))

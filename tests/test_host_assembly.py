@@ -50,3 +50,37 @@ def test_loads_to_lds_wait_for_m0(loads_to_lds):
     short = {kernel for kernel, before, _ in loads if re.match(r"s_\w+ m0,", before[-1])}
     assert not short
     assert not others  # and nothing else has a value of its own there
+
+
+def wait_states(text):
+    m = re.match(r"s_nop (\d+)", text)
+    return 1 + int(m[1]) if m else 1
+
+
+def registers(operand):
+    m = re.match(r"s\[(\d+):(\d+)\]$|s(\d+)$", operand)
+    return set() if not m else set(range(int(m[1]), int(m[2]) + 1)) if m[1] else {int(m[3])}
+
+
+def test_loads_to_lds_wait_for_their_scalar_operands(loads_to_lds):
+    # five wait states between a vector instruction that writes a scalar register and a load that reads it: what stands before a load
+    # in those five is its own two instructions, or nothing that writes them (a jump ends what can be seen, and counts as a write)
+    loads, _ = loads_to_lds
+    short = set()
+    for kernel, before, load in loads:
+        needed = set().union(*(registers(operand.split()[0]) for operand in load.split(None, 1)[1].split(",")[1:]))
+        assert len(needed) >= 4
+        left = 5
+        for text in reversed(before):
+            if left <= 0:
+                break
+            operands = text.split(None, 1)[1].split(",") if " " in text else []
+            writes = set().union(*(registers(o.strip()) for o in operands[:2])) if text.startswith("v_") else set()
+            if writes & needed or "branch" in text:
+                short.add((kernel, text, load))
+                break
+            left -= wait_states(text)
+        else:
+            if left > 0:
+                short.add((kernel, "", load))
+    assert not short
