@@ -1,6 +1,6 @@
 // The calls on 8-bit matrices for torch tensors: checks of arguments, new tensors for the results, the current stream.  A
 // Python extension, because these calls often take less time on the GPU than their arguments take in Python (silu(gate) * up
-// of one token: 6.5 us a call through ctypes, 3.8 so, of which the launch is 3).
+// of one token: 6.5 us a call through ctypes, 4.8 so, of which the launch is 3).
 #define PY_SSIZE_T_CLEAN
 #include <Python.h>
 
@@ -38,32 +38,10 @@ struct Place {
   c10::DeviceIndex gpu = c10::hip::current_device();
   void *stream() const { return c10::hip::getCurrentHIPStream(gpu).stream(); }
   bool has(const TensorBase &t) const { return t.is_cuda() && t.get_device() == gpu; }
+  // Each with memory of its own: results are saved, freed and handed to other streams one by one.  (Several in one allocation would take
+  // 0.4 us less each, but torch saves no two types of one storage.)
   TensorBase fresh(at::IntArrayRef sizes, at::IntArrayRef strides, ScalarType type) const {
     return at::detail::empty_strided_cuda(sizes, strides, type, c10::Device(c10::kCUDA, gpu));
-  }
-};
-
-// The new tensors of a call.  Where they are small they share one allocation, at 256-byte boundaries: a tensor in it takes 0.15 us,
-// one of its own 0.5 (the norm of one token with a residual and normed values 6.0 -> 4.3 us of host time).  Large ones, whose
-// memory one may want back before the others', have their own.
-class Fresh {
-  static constexpr int64_t kShared = 1 << 20;
-  const Place &place;
-  TensorBase shared;
-  int64_t used = 0;
-
- public:
-  Fresh(const Place &here, int64_t bytes) : place(here) {  // bytes: of all of them, each rounded up to 256
-    if (bytes <= kShared) shared = here.fresh({bytes}, {1}, ScalarType::Byte);
-  }
-  static int64_t room(int64_t bytes) { return round_up(bytes, 256); }
-  TensorBase take(int64_t bytes, at::IntArrayRef sizes, at::IntArrayRef strides, ScalarType type) {
-    if (!shared.defined()) return place.fresh(sizes, strides, type);
-    TensorBase t = at::detail::make_tensor<c10::TensorImpl>(c10::Storage(shared.storage()), shared.key_set(), c10::scalarTypeToTypeMeta(type));
-    t.unsafeGetTensorImpl()->set_storage_offset(used / (int64_t)c10::elementSize(type));
-    t.unsafeGetTensorImpl()->set_sizes_and_strides(sizes, strides);
-    used += room(bytes);
-    return t;
   }
 };
 
@@ -123,10 +101,9 @@ const uint8_t *bytes(const TensorBase &t) { return static_cast<const uint8_t *>(
 struct NewRows {
   int64_t ld, rows;
   TensorBase Q, S;
-  NewRows(int64_t rows_, int64_t cols, Fresh &fresh)
-      : ld(round_up(cols, 16)), rows(rows_), Q(fresh.take(rows * ld, {rows, cols}, {ld, 1}, ScalarType::Float8_e4m3fn)),
-        S(fresh.take(4 * rows * blocks_of(cols), {rows, blocks_of(cols)}, {1, step()}, ScalarType::Float)) {}
-  static int64_t bytes(int64_t rows, int64_t cols) { return Fresh::room(rows * round_up(cols, 16)) + Fresh::room(4 * rows * blocks_of(cols)); }
+  NewRows(int64_t rows_, int64_t cols, const Place &here)
+      : ld(round_up(cols, 16)), rows(rows_), Q(here.fresh({rows, cols}, {ld, 1}, ScalarType::Float8_e4m3fn)),
+        S(here.fresh({rows, blocks_of(cols)}, {1, step()}, ScalarType::Float)) {}
   int64_t step() const { return rows ? rows : 1; }
   uint8_t *q() const { return static_cast<uint8_t *>(Q.data_ptr()); }
   float *s() const { return static_cast<float *>(S.data_ptr()); }
@@ -178,8 +155,7 @@ PyObject *quant(PyObject *const *args) {
   const int64_t ldx = rows_of(X, dims, "X", here), rows = X.size(dims - 2), cols = X.size(dims - 1), blocks = blocks_of(cols);
   const int32_t type = x_type(X, "X");
   if (dims == 2 && block_rows == 1) {
-    Fresh fresh(here, NewRows::bytes(rows, cols));
-    const NewRows out(rows, cols, fresh);
+    const NewRows out(rows, cols, here);
     call("xorenc_quant_fp8", [&] {
       return xorenc_quant_fp8(X.data_ptr(), type, ldx, 0, 1, rows, (int32_t)cols, 1, out.q(), out.ld, 0, out.s(), 1, out.step(), 0, here.stream());
     });
@@ -239,12 +215,9 @@ PyObject *norm(PyObject *const *args) {
     y_row = t.stride(0);
     y_col = cols == 1 ? 1 : t.stride(1);
   }
-  const bool new_total = residual && !total.defined(), new_y = args[5] == Py_True;
-  const int64_t of_x = rows * cols * (type == XORENC_X_BF16 ? 2 : 4);
-  Fresh fresh(here, NewRows::bytes(rows, cols) + ((int)new_total + (int)new_y) * Fresh::room(of_x));
-  const NewRows out(rows, cols, fresh);
-  if (new_total) total = fresh.take(of_x, {rows, cols}, {cols, 1}, X.scalar_type());
-  if (new_y) y = fresh.take(of_x, {rows, cols}, {cols, 1}, X.scalar_type());
+  const NewRows out(rows, cols, here);
+  if (residual && !total.defined()) total = here.fresh({rows, cols}, {cols, 1}, X.scalar_type());
+  if (args[5] == Py_True) y = here.fresh({rows, cols}, {cols, 1}, X.scalar_type());
   call("xorenc_add_rmsnorm_fp8", [&] {
     return xorenc_add_rmsnorm_fp8(X.data_ptr(), type, ldx, residual, ldr, weight.data_ptr(), w_type, rows, (int32_t)cols, (float)eps,
                                   total.defined() ? total.data_ptr() : nullptr, ldt, y.defined() ? y.data_ptr() : nullptr, y_row, y_col, out.q(),
@@ -260,8 +233,7 @@ PyObject *gate(PyObject *const *args) {
   const int64_t ldx = rows_of(X, 2, "X", here), rows = X.size(0), cols = X.size(1) / 2;
   const int32_t type = x_type(X, "X");
   if (X.size(1) % 2) throw Refused{"X must have as many gates as ups"};
-  Fresh fresh(here, NewRows::bytes(rows, cols));
-  const NewRows out(rows, cols, fresh);
+  const NewRows out(rows, cols, here);
   const uint8_t *const gates = bytes(X);
   call("xorenc_silu_mul_fp8", [&] {
     return xorenc_silu_mul_fp8(gates, gates + cols * (type == XORENC_X_BF16 ? 2 : 4), type, ldx, rows, (int32_t)cols, out.q(), out.ld, out.s(), 1,

@@ -1,0 +1,30 @@
+"""What the calls on 8-bit matrices return, as tensors."""
+import io
+
+import pytest
+import torch
+
+import paper_1905_10138_amd as xe
+from test_gpu_fp8 import DEV, gen, normal
+
+pytestmark = pytest.mark.gpu
+
+
+# few rows and many: results are tensors of their own, that are saved together, and without what else the call returned
+@pytest.mark.parametrize("rows", [1, 40, 3000])
+def test_results_can_be_saved(rows):
+    g = gen(rows)
+    x, r, w = normal(g, rows, 600, dtype=torch.bfloat16).to(DEV), normal(g, rows, 600, dtype=torch.bfloat16).to(DEV), normal(g, 600).to(DEV)
+    for got in (xe.quant_fp8(x), xe.quant_fp8(x, block_rows=128), xe.quant_fp8(x[None], block_rows=128), xe.silu_mul_fp8(x),
+                xe.add_rmsnorm_fp8(x, w, r, normed=True)):
+        file = io.BytesIO()
+        torch.save(got, file)
+        file.seek(0)
+        back = torch.load(file, weights_only=True)
+        assert all(torch.equal(a.float(), b.float()) for a, b in zip(got, back))
+        assert len({t.untyped_storage().data_ptr() for t in got}) == len(got)
+        for t in got:
+            assert t.untyped_storage().nbytes() < t.element_size() * (t.numel() + 16 * rows)
+            file = io.BytesIO()
+            torch.save(t, file)
+            assert len(file.getvalue()) < t.untyped_storage().nbytes() + 4096
