@@ -1,4 +1,4 @@
-"""Builds libxorenc.so (HIP, gfx950) and _fp8.so (the calls for torch tensors) in-tree with hipcc.  `python -m paper_1905_10138_amd.build`."""
+"""Builds libxorenc.so (HIP, gfx950) and, where torch is installed, _fp8.so (the calls for torch tensors) in-tree with hipcc.  `python -m paper_1905_10138_amd.build`."""
 import os
 import shutil
 import subprocess
@@ -54,19 +54,25 @@ def _run(cmd):
 
 
 def build_library(verbose: bool = False, jobs: int = 8) -> str:
-    """Compile every source (objects in parallel; HIP for gfx950) and link the shared library and the extension."""
+    """Compile every source (objects in parallel; HIP for gfx950), link the shared library, and then the extension.  The library
+    needs hipcc alone: it is there before an extension that does not build raises, and without torch there is none."""
     hipcc = hipcc_path()
     os.makedirs(OBJ_DIR, exist_ok=True)
     objs = [os.path.join(OBJ_DIR, os.path.splitext(s)[0] + ".o") for s in SOURCES]
     cmds = [[hipcc] + FLAGS + ["-x", "hip", "-c", os.path.join(CSRC, s), "-o", o] for s, o in zip(SOURCES, objs)]
-    compile_extension, link_extension = extension_commands(hipcc)
-    cmds.insert(0, compile_extension)
-    with ThreadPoolExecutor(max_workers=max(1, min(jobs, len(cmds)))) as ex:
+    try:
+        compile_extension, link_extension = extension_commands(hipcc)
+    except ImportError:
+        compile_extension = None
+        print(f"no torch here: {EXT_PATH} (the calls on 8-bit matrices from Python) is not built")
+    with ThreadPoolExecutor(max_workers=max(1, min(jobs, len(cmds) + 1))) as ex:
+        extension = ex.submit(_run, compile_extension) if compile_extension else None
         outs = list(ex.map(_run, cmds))
     outs.append(_run([hipcc, "--offload-arch=gfx950", "-shared", "-fPIC"] + objs + ["-o", LIB_PATH + ".tmp"]))
     os.replace(LIB_PATH + ".tmp", LIB_PATH)
-    outs.append(_run(link_extension))
-    os.replace(EXT_PATH + ".tmp", EXT_PATH)
+    if extension:
+        outs += [extension.result(), _run(link_extension)]
+        os.replace(EXT_PATH + ".tmp", EXT_PATH)
     if verbose:
         for o in outs:
             if o.strip():
