@@ -351,7 +351,8 @@ XORENC_API int32_t xorenc_spmm_ws(const xorenc_layer *layer, const void *X, int3
  *   - S has two strides where it belongs to activations: element (r, b) is S[r * s_row + b * s_blk].  s_row = 1 (block column
  *     by block column) is what the kernels write and read fastest;
  *   - calls with no rows (tokens) succeed and enqueue nothing;
- *   - outputs do not overlap inputs, except where an entry point says so.
+ *   - outputs do not overlap inputs, except where an entry point says so, nor do an output's elements overlap each other (strides
+ *     that make two elements of S or Y one, or the matrices of a stack one, are XORENC_EINVAL).
  */
 #define XORENC_FP8_BLOCK 128
 

@@ -8,6 +8,7 @@
 // us and GB/s read and written (a copy of 1 GB: 5160): rows of 33 x 9216 fp32 5 (the call's time on the host), of 8192 x 5001 bf16
 // 26, 4840; squares of 16384 x 4096 bf16 36, 5600; the gates of 8192 x 9216 bf16 65, 5850; the norm of 8192 x 6000 bf16 with a
 // residual 66, 5210.
+#include <numeric>
 #include <type_traits>
 
 #include "xorenc_fp8.h"
@@ -243,6 +244,14 @@ constexpr bool kStreamsRows = STREAM && sizeof(typename T::Elem) == 2;
 
 constexpr int64_t kMostBlocks = ((int64_t)1 << 28) - 16;  // a launch has fewer than 2^32 threads
 
+// Whether two elements of rows x cols, at r * row + c * col, are one: r * row = c * col for differences r and c below rows and cols,
+// the least of which are col / g and row / g with g the strides' greatest common divisor.
+bool overlaps(int64_t rows, int64_t cols, int64_t row, int64_t col) {
+  if (rows <= 1 || cols <= 1) return (rows > 1 && row == 0) || (cols > 1 && col == 0);
+  const int64_t g = std::gcd(row, col);
+  return g == 0 || (col / g < rows && row / g < cols);
+}
+
 // Checks that the entry points share: an 8-bit result of rows x cols with its scales.
 int32_t check_result(int64_t rows, int32_t cols, const uint8_t *Q, int64_t ldq, const float *S, int64_t s_row, int64_t s_blk) {
   if (rows < 0 || cols <= 0 || ldq < cols || s_row < 0 || s_blk < 0) return XORENC_EINVAL;
@@ -273,6 +282,10 @@ extern "C" int32_t xorenc_quant_fp8(const void *X, int32_t x_dtype, int64_t ldx,
   if (!aligned_to(X, esz) || (matrices > 1 && q_stride % 16)) return XORENC_EALIGN;
   hipStream_t st = static_cast<hipStream_t>(hip_stream);
   const int per_row = (cols + kBlock - 1) / kBlock;
+  const int64_t squares = (rows + kBlock - 1) / kBlock * per_row;
+  if (block_rows == kBlock && (rows > (1 << 30) || squares >= (1 << 24))) return XORENC_ELIMIT;
+  if (overlaps(block_rows == 1 ? rows : (rows + kBlock - 1) / kBlock, per_row, s_row, s_blk) || (matrices > 1 && (q_stride == 0 || s_stride == 0)))
+    return XORENC_EINVAL;
   xorenc_internal_begin_call();
   if (block_rows == 1) {
     for (int32_t i = 0; i < matrices; ++i) {
@@ -285,8 +298,6 @@ extern "C" int32_t xorenc_quant_fp8(const void *X, int32_t x_dtype, int64_t ldx,
     }
     return XORENC_OK;
   }
-  const int64_t squares = (rows + kBlock - 1) / kBlock * per_row;
-  if (rows > (1 << 30) || squares >= (1 << 24)) return XORENC_ELIMIT;
   for (int64_t at = 0; at < matrices; at += 65535) {  // the grid's second size is limited
     const dim3 grid((unsigned)squares, (unsigned)min(matrices - at, (int64_t)65535));
     const int32_t rl = for_type(x_dtype, streams(rows * cols, (int64_t)(esz + 1) * matrices), [&](auto type, auto stream) {
@@ -311,6 +322,7 @@ extern "C" int32_t xorenc_silu_mul_fp8(const void *gate, const void *up, int32_t
   if (!gate || !up) return XORENC_EINVAL;
   const int esz = dtype_bytes(x_dtype);
   if (!aligned_to(gate, esz) || !aligned_to(up, esz)) return XORENC_EALIGN;
+  if (overlaps(rows, (cols + kBlock - 1) / kBlock, s_row, s_blk)) return XORENC_EINVAL;
   hipStream_t st = static_cast<hipStream_t>(hip_stream);
   xorenc_internal_begin_call();
   return for_type(x_dtype, streams(rows * cols, 2 * esz + 1), [&](auto type, auto stream) {
@@ -386,6 +398,7 @@ extern "C" int32_t xorenc_add_rmsnorm_fp8(const void *X, int32_t x_dtype, int64_
   if (!aligned_to(X, esz) || !aligned_to(residual, esz) || !aligned_to(total, esz) || !aligned_to(Y, esz) ||
       !aligned_to(weight, dtype_bytes(w_dtype)))
     return XORENC_EALIGN;
+  if (overlaps(rows, (cols + kBlock - 1) / kBlock, s_row, s_blk) || (Y && overlaps(rows, cols, y_row, y_col))) return XORENC_EINVAL;
   hipStream_t st = static_cast<hipStream_t>(hip_stream);
   xorenc_internal_begin_call();
   const int moved = 1 + esz * (1 + (residual != nullptr) + (total != nullptr) + (Y != nullptr));

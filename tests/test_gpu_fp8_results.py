@@ -28,3 +28,14 @@ def test_results_can_be_saved(rows):
             file = io.BytesIO()
             torch.save(t, file)
             assert len(file.getvalue()) < t.untyped_storage().nbytes() + 4096
+
+
+def test_normed_rows_that_overlap_are_refused():
+    x, w = torch.ones((4, 600), device=DEV), torch.ones(600, device=DEV)
+    one = torch.zeros(600 * 4, device=DEV)
+    for normed in (one[:600].expand(4, 600), one.as_strided((4, 600), (1, 1)), one.as_strided((4, 600), (599, 1))):
+        with pytest.raises(xe.XorencError):
+            xe.add_rmsnorm_fp8(x, w, normed=normed)
+    assert not one.any()
+    for normed in (one[:600].expand(1, 600), one.as_strided((4, 600), (600, 1)), one.as_strided((4, 600), (1, 4))):
+        assert torch.equal(xe.add_rmsnorm_fp8(x[:normed.shape[0]], w, normed=normed)[3], xe.add_rmsnorm_fp8(x[:normed.shape[0]], w, normed=True)[3])

@@ -1,0 +1,28 @@
+"""What else the C ABI of the operators in 8 bits refuses, and what it does not (see test_host_fp8.py): no GPU is needed, and no pointer is
+followed.  A call whose sizes are accepted is stopped by a later check, of an address that is not aligned, before any launch."""
+import ctypes  # noqa: F401
+
+import pytest
+
+from paper_1905_10138_amd import fp8
+from test_host_fp8 import BF16, EALIGN, EINVAL, ELIMIT, F32, P, with_changes
+
+QUANT = dict(X=P, dt=BF16, ldx=256, xs=0, n=1, rows=4, cols=256, br=1, Q=P, ldq=256, qs=0, S=P, sr=1, sb=4, ss=0, st=None)
+NORM = dict(X=P, dt=BF16, ldx=256, R=P, ldr=256, w=P, wdt=F32, rows=4, cols=256, eps=1e-6, t=P, ldt=256, Y=P, yr=256, yc=1, Q=P, ldq=256,
+            S=P, sr=1, sb=4, st=None)
+GATE = dict(g=P, u=P, dt=F32, ldx=512, rows=4, cols=256, Q=P, ldq=256, S=P, sr=1, sb=4, st=None)
+
+
+@pytest.fixture(scope="module")
+def lib():
+    return fp8._library()
+
+
+def test_results_whose_elements_are_one(lib):
+    stack = dict(n=2, rows=130, br=128, qs=65536, ss=8, sb=2)
+    with_changes(lib.xorenc_quant_fp8, QUANT, [
+        ({"sr": 0}, EINVAL), ({"sb": 0}, EINVAL), ({"sr": 1, "sb": 3}, EINVAL), ({"sr": 2, "sb": 6}, EINVAL),
+        ({**stack, "qs": 0}, EINVAL), ({**stack, "ss": 0}, EINVAL), ({**stack, "sb": 1}, EINVAL)])
+    with_changes(lib.xorenc_silu_mul_fp8, GATE, [({"sr": 0}, EINVAL), ({"sb": 0}, EINVAL), ({"sr": 1, "sb": 1}, EINVAL)])
+    with_changes(lib.xorenc_add_rmsnorm_fp8, NORM, [
+        ({"sr": 0}, EINVAL), ({"yr": 0}, EINVAL), ({"yr": 255}, EINVAL), ({"yr": 1, "yc": 3}, EINVAL), ({"yr": 2, "yc": 4}, EINVAL)])
