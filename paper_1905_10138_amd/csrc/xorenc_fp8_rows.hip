@@ -258,7 +258,7 @@ int32_t check_result(int64_t rows, int32_t cols, const uint8_t *Q, int64_t ldq, 
   if (rows == 0) return XORENC_OK;
   if (!Q || !S) return XORENC_EINVAL;
   if (!aligned_to(Q, 16) || (rows > 1 && ldq % 16) || !aligned_to(S, 4)) return XORENC_EALIGN;
-  if (rows * ((cols + (int64_t)kBlock - 1) / kBlock) > kMostBlocks || cols > (1 << 30)) return XORENC_ELIMIT;
+  if (rows > kMostBlocks / ((cols + (int64_t)kBlock - 1) / kBlock) || cols > (1 << 30)) return XORENC_ELIMIT;  // (a division: the product may not fit)
   return XORENC_OK;
 }
 

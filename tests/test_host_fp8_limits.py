@@ -26,3 +26,11 @@ def test_results_whose_elements_are_one(lib):
     with_changes(lib.xorenc_silu_mul_fp8, GATE, [({"sr": 0}, EINVAL), ({"sb": 0}, EINVAL), ({"sr": 1, "sb": 1}, EINVAL)])
     with_changes(lib.xorenc_add_rmsnorm_fp8, NORM, [
         ({"sr": 0}, EINVAL), ({"yr": 0}, EINVAL), ({"yr": 255}, EINVAL), ({"yr": 1, "yc": 3}, EINVAL), ({"yr": 2, "yc": 4}, EINVAL)])
+
+
+def test_rows_whose_blocks_exceed_64_bits(lib):
+    # 2^57 + 1 rows of 128 blocks are 2^64 + 128 blocks
+    wide = dict(rows=(1 << 57) + 1, cols=16384, ldx=16384, ldq=16384)
+    with_changes(lib.xorenc_quant_fp8, QUANT, [({**wide, "X": P + 1}, ELIMIT), ({**wide, "rows": (1 << 63) - 1, "br": 128, "X": P}, ELIMIT)])
+    with_changes(lib.xorenc_silu_mul_fp8, GATE, [({**wide, "u": P + 2}, ELIMIT)])
+    with_changes(lib.xorenc_add_rmsnorm_fp8, NORM, [({**wide, "ldr": 16384, "ldt": 16384, "yr": 16384, "X": P + 1}, ELIMIT)])
