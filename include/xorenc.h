@@ -359,7 +359,7 @@ XORENC_API int32_t xorenc_spmm_ws(const xorenc_layer *layer, const void *X, int3
 /*
  * `matrices` matrices of rows x cols (element (r, c) of matrix i: X[i * x_stride + r * ldx + c], and so on for Q; scale (r, b)
  * of matrix i: S[i * s_stride + r * s_row + b * s_blk]) to 8 bits, in blocks of block_rows (1 or 128) x 128.
- * XORENC_ELIMIT from 2^28 - 16 blocks of one row, or 2^24 of 128, on in one matrix.
+ * XORENC_ELIMIT beyond 2^28 - 16 blocks of one row, or 2^24 - 1 of 128 (and 2^30 rows), in one matrix, and beyond 2^30 columns.
  */
 XORENC_API int32_t xorenc_quant_fp8(const void *X, int32_t x_dtype, int64_t ldx, int64_t x_stride, int32_t matrices, int64_t rows,
                                     int32_t cols, int32_t block_rows, uint8_t *Q, int64_t ldq, int64_t q_stride, float *S,

@@ -242,7 +242,7 @@ int32_t for_type(int32_t x_dtype, bool stream, F f) {
 template <class T, bool STREAM>
 constexpr bool kStreamsRows = STREAM && sizeof(typename T::Elem) == 2;
 
-constexpr int64_t kMostBlocks = ((int64_t)1 << 28) - 16;  // a launch has fewer than 2^32 threads
+constexpr int64_t kMostBlocks = ((int64_t)1 << 28) - 16, kMostSquares = (1 << 24) - 1;  // a launch has fewer than 2^32 threads
 
 // Whether two elements of rows x cols, at r * row + c * col, are one: r * row = c * col for differences r and c below rows and cols,
 // the least of which are col / g and row / g with g the strides' greatest common divisor.
@@ -252,13 +252,15 @@ bool overlaps(int64_t rows, int64_t cols, int64_t row, int64_t col) {
   return g == 0 || (col / g < rows && row / g < cols);
 }
 
-// Checks that the entry points share: an 8-bit result of rows x cols with its scales.
-int32_t check_result(int64_t rows, int32_t cols, const uint8_t *Q, int64_t ldq, const float *S, int64_t s_row, int64_t s_blk) {
+// Checks that the entry points share: an 8-bit result of rows x cols with its scales, a launch's blocks of block_rows x 128.
+int32_t check_result(int64_t rows, int32_t cols, const uint8_t *Q, int64_t ldq, const float *S, int64_t s_row, int64_t s_blk, int32_t block_rows = 1) {
   if (rows < 0 || cols <= 0 || ldq < cols || s_row < 0 || s_blk < 0) return XORENC_EINVAL;
   if (rows == 0) return XORENC_OK;
   if (!Q || !S) return XORENC_EINVAL;
   if (!aligned_to(Q, 16) || (rows > 1 && ldq % 16) || !aligned_to(S, 4)) return XORENC_EALIGN;
-  if (rows > kMostBlocks / ((cols + (int64_t)kBlock - 1) / kBlock) || cols > (1 << 30)) return XORENC_ELIMIT;  // (a division: the product may not fit)
+  const int64_t per_row = (cols + (int64_t)kBlock - 1) / kBlock;  // (divisions: products may not fit)
+  if (cols > (1 << 30) || (block_rows == 1 ? rows > kMostBlocks / per_row : rows > (1 << 30) || (rows + kBlock - 1) / kBlock > kMostSquares / per_row))
+    return XORENC_ELIMIT;
   return XORENC_OK;
 }
 
@@ -273,7 +275,7 @@ extern "C" int32_t xorenc_quant_fp8(const void *X, int32_t x_dtype, int64_t ldx,
   if (matrices < 0 || ldx < cols) return XORENC_EINVAL;
   if (block_rows != 1 && block_rows != kBlock) return XORENC_EUNSUPPORTED;
   if (!known_dtype(x_dtype)) return XORENC_EUNSUPPORTED;
-  const int32_t rc = check_result(rows, cols, Q, ldq, S, s_row, s_blk);
+  const int32_t rc = check_result(rows, cols, Q, ldq, S, s_row, s_blk, block_rows);
   if (rc != XORENC_OK) return rc;
   if (rows == 0 || matrices == 0) return XORENC_OK;
   if (!X) return XORENC_EINVAL;
@@ -282,8 +284,6 @@ extern "C" int32_t xorenc_quant_fp8(const void *X, int32_t x_dtype, int64_t ldx,
   if (!aligned_to(X, esz) || (matrices > 1 && q_stride % 16)) return XORENC_EALIGN;
   hipStream_t st = static_cast<hipStream_t>(hip_stream);
   const int per_row = (cols + kBlock - 1) / kBlock;
-  const int64_t squares = (rows + kBlock - 1) / kBlock * per_row;
-  if (block_rows == kBlock && (rows > (1 << 30) || squares >= (1 << 24))) return XORENC_ELIMIT;
   if (overlaps(block_rows == 1 ? rows : (rows + kBlock - 1) / kBlock, per_row, s_row, s_blk) || (matrices > 1 && (q_stride == 0 || s_stride == 0)))
     return XORENC_EINVAL;
   xorenc_internal_begin_call();
@@ -299,7 +299,7 @@ extern "C" int32_t xorenc_quant_fp8(const void *X, int32_t x_dtype, int64_t ldx,
     return XORENC_OK;
   }
   for (int64_t at = 0; at < matrices; at += 65535) {  // the grid's second size is limited
-    const dim3 grid((unsigned)squares, (unsigned)min(matrices - at, (int64_t)65535));
+    const dim3 grid((unsigned)((rows + kBlock - 1) / kBlock * per_row), (unsigned)min(matrices - at, (int64_t)65535));
     const int32_t rl = for_type(x_dtype, streams(rows * cols, (int64_t)(esz + 1) * matrices), [&](auto type, auto stream) {
       typedef typename decltype(type)::Elem E;
       hipLaunchKernelGGL((quant_square_kernel<decltype(type), decltype(stream)::value>), grid, dim3(256), 0, st,

@@ -34,3 +34,11 @@ def test_rows_whose_blocks_exceed_64_bits(lib):
     with_changes(lib.xorenc_quant_fp8, QUANT, [({**wide, "X": P + 1}, ELIMIT), ({**wide, "rows": (1 << 63) - 1, "br": 128, "X": P}, ELIMIT)])
     with_changes(lib.xorenc_silu_mul_fp8, GATE, [({**wide, "u": P + 2}, ELIMIT)])
     with_changes(lib.xorenc_add_rmsnorm_fp8, NORM, [({**wide, "ldr": 16384, "ldt": 16384, "yr": 16384, "X": P + 1}, ELIMIT)])
+
+
+def test_squares_have_their_own_limit(lib):
+    # 2^21 x 2^14 is 2^28 blocks of 1 x 128, and 2^21 of 128 x 128; 2^24 of those are too many
+    tall = dict(br=128, cols=16384, ldx=16384, ldq=16384, sr=128, sb=1)
+    with_changes(lib.xorenc_quant_fp8, QUANT, [
+        ({**tall, "rows": 1 << 21, "X": P + 1}, EALIGN), ({**tall, "rows": (1 << 24) - 128, "X": P + 1}, EALIGN), ({**tall, "rows": 1 << 24}, ELIMIT),
+        ({**tall, "rows": 1 << 21, "br": 1}, ELIMIT), ({**tall, "rows": (1 << 21) - 1, "br": 1, "X": P + 1}, EALIGN)])
