@@ -113,9 +113,9 @@ __global__ __launch_bounds__(256) void router_kernel(const typename T::Elem *__r
 
 // ---------------------------------------------------------------------------------------------- picks
 
-// fp32 -> integers in the same order, any NaN above infinity
+// fp32 -> integers in the same order, any NaN above infinity, both zeros as one (-0 + 0 is 0)
 __device__ inline uint32_t ordered(float v) {
-  const uint32_t b = __float_as_uint(v);
+  const uint32_t b = __float_as_uint(v + 0.f);
   if (v != v) return 0xffffffffu;
   return b & 0x80000000u ? ~b : b | 0x80000000u;
 }

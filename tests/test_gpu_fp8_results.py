@@ -39,3 +39,21 @@ def test_normed_rows_that_overlap_are_refused():
     assert not one.any()
     for normed in (one[:600].expand(1, 600), one.as_strided((4, 600), (600, 1)), one.as_strided((4, 600), (1, 4))):
         assert torch.equal(xe.add_rmsnorm_fp8(x[:normed.shape[0]], w, normed=normed)[3], xe.add_rmsnorm_fp8(x[:normed.shape[0]], w, normed=True)[3])
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("T", [1, 3, 5])
+def test_logits_of_either_zero_are_equal(T, dtype):
+    # products of -1e-60 round to -0, and a sum of them is -0: no less than the 0 of the next expert
+    g = gen(T)
+    E, H, I = 3, 2048, 40
+    x = torch.full((T, H), 1e-30, dtype=dtype, device=DEV)
+    W13, S13 = xe.quant_fp8(normal(g, E, 2 * I, H, scale=1e29).to(DEV), block_rows=128)
+    W2, S2 = xe.quant_fp8(normal(g, E, H, I).to(DEV), block_rows=128)
+    for signs in ((-1.0, 0.0), (0.0, -1.0), (0.0, 0.0), (-1.0, -1.0)):
+        router = torch.full((E, H), -1e30, dtype=dtype, device=DEV)
+        router[0], router[1] = signs[0] * 1e-30, signs[1] * 1e-30
+        Y = xe.moe_fp8(x, router, W13, S13, W2, S2, 1)
+        router[:2] = 0.0
+        router[1] = -1e30                                                # the first alone
+        assert Y.any() and torch.equal(Y, xe.moe_fp8(x, router, W13, S13, W2, S2, 1)), signs
