@@ -5,6 +5,7 @@ import pytest
 import torch
 
 import paper_1905_10138_amd as xe
+import fp8_oracle as ref
 from test_gpu_fp8 import DEV, gen, normal
 
 pytestmark = pytest.mark.gpu
@@ -57,3 +58,13 @@ def test_logits_of_either_zero_are_equal(T, dtype):
         router[:2] = 0.0
         router[1] = -1e30                                                # the first alone
         assert Y.any() and torch.equal(Y, xe.moe_fp8(x, router, W13, S13, W2, S2, 1)), signs
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+def test_gates_whose_logistic_is_subnormal(dtype):
+    # 1 / (1 + exp(88)) is 6.1e-39, below the normal numbers of fp32, and 88 times that is none of them; up to exp(-x) = 2^128
+    x = torch.cat([-torch.linspace(84.0, 88.7, 512), torch.full((512,), 1e30)]).to(dtype).reshape(1, -1)
+    Q, S = xe.silu_mul_fp8(x.to(DEV))
+    # as test_gate of test_gpu_fp8.py has it for the exponential's argument (and 2^-26 of it for the constant), and half of a subnormal's
+    # last bit: 2^-150 of 2^-128
+    ref.check_quantised(ref.silu_mul(x), Q, S, 1, 89 * (2.0 ** -24 + 2.0 ** -26) + 8 * 2.0 ** -24 + 2.0 ** -22)
