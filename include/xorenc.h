@@ -390,8 +390,8 @@ XORENC_API int32_t xorenc_silu_mul_fp8(const void *gate, const void *up, int32_t
  * (i, b) at SW[i * ldsw + b]), Y (M x N, XORENC_X_F32 or XORENC_X_BF16).  Scaled sums of blocks are added in fp32.  bf16 results
  * come from the 8-bit matrix instruction, whose sums inside a block are 1.5e-5 of the result off (2-norm, Gaussian
  * values); fp32 results from the bf16 one, which is exact in the products and half as fast.
- * XORENC_ELIMIT beyond 4194240 rows of A, 2^22 tiles of 128 x 128 results, 2^22 columns (or such a leading dimension of A or W), sa_row = 2^20, and
- * where 256 * sa_row + sa_blk * ceil(K / 128) reaches 2^29.
+ * XORENC_ELIMIT beyond 4194240 rows of A, 2^22 tiles of 128 x 128 results, 2^22 columns (or such a leading dimension of A or W), sa_row = 2^20,
+ * sa_blk = 2^28, and where 256 * sa_row + sa_blk * ceil(K / 128) reaches 2^29.
  */
 XORENC_API int32_t xorenc_matmul_fp8(const uint8_t *A, int64_t lda, const float *SA, int64_t sa_row, int64_t sa_blk, const uint8_t *W,
                                      int64_t ldw, const float *SW, int64_t ldsw, int32_t M, int32_t N, int32_t K, void *Y,
@@ -428,7 +428,8 @@ typedef struct xorenc_moe {
  *   y = sum over the picks of share * W2_e (silu(G_e x) * (U_e x)).
  * Activations are not rounded to 8 bits; the inner ones keep 16 bits of mantissa (24 for fp32 X).  Weights of experts that no
  * token picks are not read.  The same bits on every call.  workspace: DEV, 16-byte aligned, xorenc_moe_workspace bytes, contents
- * undefined before and after.  XORENC_ELIMIT beyond the limits above, and for hidden or inner > 2^17.
+ * undefined before and after.  XORENC_ELIMIT beyond the limits above, for hidden or inner > 2^17, and for leading dimensions of W13
+ * or W2 > 2^24 or of S13 or S2 > 2^16.
  */
 XORENC_API int32_t xorenc_moe_workspace(int32_t tokens, int32_t hidden, int32_t inner, int32_t experts, int32_t picks, int32_t x_dtype,
                                         int64_t *bytes /*HOST*/);

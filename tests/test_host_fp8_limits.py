@@ -1,11 +1,9 @@
 """What else the C ABI of the operators in 8 bits refuses, and what it does not (see test_host_fp8.py): no GPU is needed, and no pointer is
 followed.  A call whose sizes are accepted is stopped by a later check, of an address that is not aligned, before any launch."""
-import ctypes  # noqa: F401
-
 import pytest
 
 from paper_1905_10138_amd import fp8
-from test_host_fp8 import BF16, EALIGN, EINVAL, ELIMIT, F32, P, with_changes
+from test_host_fp8 import BF16, EALIGN, EINVAL, ELIMIT, F32, P, layer, with_changes
 
 QUANT = dict(X=P, dt=BF16, ldx=256, xs=0, n=1, rows=4, cols=256, br=1, Q=P, ldq=256, qs=0, S=P, sr=1, sb=4, ss=0, st=None)
 NORM = dict(X=P, dt=BF16, ldx=256, R=P, ldr=256, w=P, wdt=F32, rows=4, cols=256, eps=1e-6, t=P, ldt=256, Y=P, yr=256, yc=1, Q=P, ldq=256,
@@ -42,3 +40,17 @@ def test_squares_have_their_own_limit(lib):
     with_changes(lib.xorenc_quant_fp8, QUANT, [
         ({**tall, "rows": 1 << 21, "X": P + 1}, EALIGN), ({**tall, "rows": (1 << 24) - 128, "X": P + 1}, EALIGN), ({**tall, "rows": 1 << 24}, ELIMIT),
         ({**tall, "rows": 1 << 21, "br": 1}, ELIMIT), ({**tall, "rows": (1 << 21) - 1, "br": 1, "X": P + 1}, EALIGN)])
+
+
+def test_strides_of_products(lib):
+    good = dict(A=P, lda=256, SA=P, sar=1, sab=4, W=P, ldw=256, SW=P, ldsw=2, M=4, N=128, K=256, Y=P, dt=BF16, ldy=128, st=None)
+    with_changes(lib.xorenc_matmul_fp8, good, [
+        ({"lda": (1 << 22) + 16}, ELIMIT), ({"ldw": (1 << 22) + 16}, ELIMIT), ({"sar": (1 << 20) + 1}, ELIMIT), ({"sab": (1 << 28) + 1, "K": 128}, ELIMIT),
+        ({"sar": 1 << 20, "sab": 1 << 27}, ELIMIT), ({"M": 1 << 20, "N": 1 << 20, "lda": 256, "ldy": 1 << 20}, ELIMIT)])
+
+
+def test_strides_of_experts(lib):
+    good = dict(L=layer(), X=P, dt=BF16, ldx=256, T=4, n=2, re=1, Y=P, ldy=256, ws=P, wsb=1 << 30, st=None)
+    with_changes(lib.xorenc_moe_fp8, good, [
+        ({"L": layer(ld13=(1 << 24) + 16)}, ELIMIT), ({"L": layer(ld2=(1 << 24) + 16)}, ELIMIT), ({"L": layer(lds13=(1 << 16) + 1)}, ELIMIT),
+        ({"L": layer(lds2=(1 << 16) + 1)}, ELIMIT), ({"L": layer(ld13=1 << 24, ld2=1 << 24, lds13=1 << 16, lds2=1 << 16), "ws": P + 4}, EALIGN)])
