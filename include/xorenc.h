@@ -388,8 +388,9 @@ XORENC_API int32_t xorenc_silu_mul_fp8(const void *gate, const void *up, int32_t
 /*
  * Y = A W^T: A (M x K, blocks of 1 x 128, scale (m, b) at SA[m * sa_row + b * sa_blk]), W (N x K, blocks of 128 x 128, scale
  * (i, b) at SW[i * ldsw + b]), Y (M x N, XORENC_X_F32 or XORENC_X_BF16).  Scaled sums of blocks are added in fp32.  bf16 results
- * come from the 8-bit matrix instruction, whose sums inside a block are 1.5e-5 of the result off (2-norm, Gaussian
- * values); fp32 results from the bf16 one, which is exact in the products and half as fast.
+ * come from the 8-bit matrix instruction, which cuts a block's products some 14 bits below the largest of them (1.5e-5 of the result
+ * in the 2-norm for Gaussian values; more of results that cancel to far less than their terms); fp32 results from the bf16 one,
+ * which is exact in the products and half as fast.
  * XORENC_ELIMIT beyond 4194240 rows of A, 2^22 tiles of 128 x 128 results, 2^22 columns (or such a leading dimension of A or W), sa_row = 2^20,
  * sa_blk = 2^28, and where 256 * sa_row + sa_blk * ceil(K / 128) reaches 2^29.
  */

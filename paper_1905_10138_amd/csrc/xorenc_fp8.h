@@ -112,8 +112,7 @@ struct BF16 {
 
 // Eight values of a row from column c on; columns from `cols` on are zero.  The load comes first, without a branch (so that
 // several are on their way together), and takes the row's last eight elements where fewer are left behind c; the values
-// come from it.  STREAM: they are not kept in caches.  whole (a constant): c + 8 <= cols is known;
-// brief (a constant): in short code, which takes longer at a row's end.
+// come from it (piece_of).  STREAM: they are not kept in caches.  whole (a constant): c + 8 <= cols is known.
 template <class T, bool STREAM = false>
 __device__ inline typename T::Raw load_piece(const typename T::Elem *row, int c, int cols, bool whole = false) {
   if (whole) return T::template load8<STREAM>(row + c);
@@ -127,6 +126,7 @@ __device__ inline void shift_down(float *v) {
   v[7] = 0.f;
 }
 
+// The values of such a load.  brief (a constant): in short code, which takes longer at a row's end.
 template <class T>
 __device__ inline void piece_of(const typename T::Raw &raw, int c, int cols, float *v, bool whole = false, bool brief = false) {
   T::widen(raw, v);
@@ -204,10 +204,6 @@ __device__ inline float sum_of_wave(float v) {
   return v + __shfl_xor(v, 32);
 }
 
-// Operands of the matrix instructions for 128 columns of 16 rows.  Lane l holds 32 values of row l % 16: columns
-// 16 (l / 16) + 0..15 of the first 64 columns (piece 0), then of the second 64 (piece 1).  Which of the instruction's k a column
-// becomes does not matter as long as both operands agree.
-
 // What a row's last 16-byte piece holds behind its last column, `left` bytes from its start (1 .. 15): zero.
 __device__ inline u32x4 first_bytes(u32x4 v, int left) {
 #pragma unroll
@@ -258,6 +254,9 @@ __device__ inline uint32_t e4m3_operand_offset(int lane) {  // of the first piec
   return (uint32_t)((lane & 15) * 128 + (((lane >> 4) ^ (((lane & 15) >> 1) & 7)) * 16));
 }
 
+// Operands of the matrix instructions for 128 columns of 16 rows.  Lane l holds 32 values of row l % 16: columns
+// 16 (l / 16) + 0..15 of the first 64 columns (piece 0), then of the second 64 (piece 1).  Which of the instruction's k a column
+// becomes does not matter as long as both operands agree.
 struct E4m3Operand {
   u32x4 piece[2];
 };
@@ -283,9 +282,9 @@ __device__ inline bf16x8 quarter_as_bf16(const E4m3Operand &o, int q) {
 }
 
 // The product of 16 rows of A and 16 of B over 128 columns.  Lane l gets column l % 16 (a row of B), rows 4 (l / 16) .. + 3
-// (of A).  The 8-bit instruction adds products aligned to the largest of them: 1.5e-5 of the result for Gaussian
-// values (2-norm), which results of 16 bits do not show.  Results of 32 bits come from the bf16 instruction, which
-// multiplies e4m3 values exactly and adds in fp32, at half the rate.
+// (of A).  The 8-bit instruction adds products aligned to the largest of them, some 14 bits below it: 1.5e-5 of the result for
+// Gaussian values (2-norm), less than results of 16 bits are rounded by, unless a block's products cancel to far less than the largest of them.
+// Results of 32 bits come from the bf16 instruction, which multiplies e4m3 values exactly and adds in fp32, at half the rate.
 template <bool EXACT>
 __device__ inline f32x4 product_128(const E4m3Operand &a, const E4m3Operand &b) {
   f32x4 d = {0.f, 0.f, 0.f, 0.f};
@@ -303,7 +302,6 @@ __device__ inline f32x4 product_128(const E4m3Operand &a, const E4m3Operand &b) 
 inline bool known_dtype(int32_t t) { return t == XORENC_X_F32 || t == XORENC_X_BF16; }
 inline int dtype_bytes(int32_t t) { return t == XORENC_X_F32 ? 4 : 2; }
 inline bool aligned_to(const void *p, size_t n) { return ((uintptr_t)p & (n - 1)) == 0; }
-// pieces of eight values of every row on 16-byte boundaries
 
 }  // namespace xorenc_fp8_detail
 

@@ -39,7 +39,8 @@ constexpr Cost kCosts[2][kKernels] = {
      {64, 64, 256, 2, 1.88f, 2.25f, 0.50f, 0.13f},     // 8: of 64 x 64, two groups of four waves
      {256, 192, 256, 1, 2.00f, 5.75f, 1.27f, 0.19f},   // 9: as 0, of 256 x 192
      {128, 128, 256, 1, 1.77f, 2.85f, 0.67f, 0.08f}},  // 10: as 8, of 128 x 128, one group of eight waves
-    // fp32 results (those of 0 and 9 do not fit in LDS, nor the operands of 0 in registers; 8 and 10 would be taken for no size)
+    // fp32 results (those of 0 and 9 do not fit in LDS, nor the operands of 0 in registers; 8 and 10 would be taken for no size; of 3
+    // two workgroups fit on a CU, but 256 slots are nearer to its times)
     {{},
      {128, 128, 512, 1, 0.81f, 5.84f, 1.23f, 0.45f},
      {128, 64, 768, 1, 1.45f, 3.22f, 0.88f, 0.63f},

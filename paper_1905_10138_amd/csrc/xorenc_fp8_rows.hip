@@ -19,13 +19,13 @@ namespace {
 // Y = x (or silu(x) * up) by blocks of one row x 128.  Sixteen lanes per block, blocks numbered row by row.
 template <class T, bool GATED, bool STREAM>
 __global__ __launch_bounds__(256) void quant_rows_kernel(const typename T::Elem *__restrict__ X,
-                                                         const typename T::Elem *__restrict__ up, int64_t ldx, int64_t blocks,
-                                                         int cols, int per_row, uint8_t *__restrict__ Q, int64_t ldq,
+                                                         const typename T::Elem *__restrict__ up, int64_t ldx, uint32_t blocks,
+                                                         int cols, uint32_t per_row, uint8_t *__restrict__ Q, int64_t ldq,
                                                          float *__restrict__ S, int64_t s_row, int64_t s_blk) {
-  const int64_t b = (int64_t)blockIdx.x * 16 + (threadIdx.x >> 4);
+  const uint32_t b = blockIdx.x * 16 + (threadIdx.x >> 4);  // (a launch's blocks are fewer than 2^28)
   if (b >= blocks) return;
-  const int64_t r = blocks <= 0x7fffffff ? (int64_t)((uint32_t)b / (uint32_t)per_row) : b / per_row;
-  const int kb = (int)(b - r * per_row), l = threadIdx.x & 15;
+  const int64_t r = b / per_row;
+  const int kb = (int)(b % per_row), l = threadIdx.x & 15;
   const int c = kb * kBlock + l * 8;
   float v[8];
   const typename T::Raw x = load_piece<T, STREAM>(X + r * ldx, c, cols);
@@ -218,8 +218,7 @@ __global__ __launch_bounds__(THREADS *ROWS) void rmsnorm_kernel(const typename T
 template <class T, bool GATED, bool STREAM>
 int32_t launch_rows(const void *X, const void *up, int64_t ldx, int64_t rows, int32_t cols, uint8_t *Q, int64_t ldq,
                     float *S, int64_t s_row, int64_t s_blk, hipStream_t st) {
-  const int per_row = (cols + kBlock - 1) / kBlock;
-  const int64_t blocks = rows * per_row;
+  const uint32_t per_row = (uint32_t)((cols + kBlock - 1) / kBlock), blocks = (uint32_t)(rows * per_row);
   hipLaunchKernelGGL((quant_rows_kernel<T, GATED, STREAM>), dim3((unsigned)((blocks + 15) / 16)), dim3(256), 0, st,
                      static_cast<const typename T::Elem *>(X), static_cast<const typename T::Elem *>(up), ldx, blocks, cols,
                      per_row, Q, ldq, S, s_row, s_blk);

@@ -3,7 +3,7 @@
 //
 // Five launches: the router's logits; the picks (not for very few tokens, whose picks every workgroup finds by itself); the gated
 // activations h of the picked experts; their second product and the sum over picks; the sum of that product's parts (where it
-// has any).  The bytes of the picked experts' weights bound the two products (32 tokens, two of eight experts of 4096 x 9216: 181 us,
+// has any).  The bytes of the picked experts' weights bound the two products (32 tokens, two of eight experts of 4096 x 9216: 183 us,
 // 5.0 TB/s over all launches).  Weights go from memory to a ring of stages in LDS (eight lanes fetch 128 bytes of a row; loads to
 // registers, where a lane needs 32 bytes of one row of 16, take the address units twice as long: the same call 250 us, 207 by
 // rings alone), and so do the activations that multiply them.  e4m3 values become bf16 exactly and multiply bf16 terms of the
@@ -743,8 +743,8 @@ MoePlan plan_of(int T, int H, int I, int E, int top, int32_t dtype) {
   p.x_row = (H + kBlock - 1) / kBlock * terms * (2 * kBlock);
   p.h_row = (I + kBlock - 1) / kBlock * h_terms * (2 * kBlock);
   p.row_groups = (H + 127) / 128;
-  // workgroups of the second product: one for each CU (two: 205 against 201 us for 32 tokens and eight experts of 4096 x 9216, 33.6
-  // against 32.1 for one token and four of 2048 x 4096), a block of the reduction each at least, 32 parts at most (64: 29 against 26
+  // workgroups of the second product: one for each CU (two: 190 against 184 us for 32 tokens and eight experts of 4096 x 9216, 152
+  // against 147 for eight tokens and 16 of 4096 x 4096), a block of the reduction each at least, 32 parts at most (64: 29 against 26
   // for 64 tokens and 16 of 512 x 512)
   const int64_t steps = (int64_t)used * ((I + kBlock - 1) / kBlock);
   p.splits = (256 + p.row_groups - 1) / p.row_groups;
@@ -783,8 +783,8 @@ void launch_down_few(const MoeArgs &g, void *Y, int64_t ldy, hipStream_t st) {
 template <bool STREAM, class T, int XR, int TERMS, int H_TERMS>
 void launch_products(const MoeArgs &g, void *Y, int64_t ldy, hipStream_t st) {
   // Four waves: side by side where x is wide and they share it, in pairs otherwise, and all on the same 16 rows where there
-  // are few of them (us, in this order: 32 tokens, two of eight experts of 4096 x 9216 201, 208, 244; 16 tokens 194, 183,
-  // 190; eight tokens, four of 16 experts of 4096 x 4096 173, 161, 165; one token, six of 2048 x 1024 25, 22, 21)
+  // are few of them (us, in this order: 32 tokens, two of eight experts of 4096 x 9216 184, 189, 246; 16 tokens 177, 163,
+  // 175; eight tokens, four of 16 experts of 4096 x 4096 156, 147, 159; one token, six of 64 of 2048 x 1024 24, 21, 20)
   const int64_t tiles = (int64_t)((g.I + 15) / 16) * g.most_uses;
   if (tiles < 2048)
     launch_up<STREAM, XR, TERMS, H_TERMS, 1, 4>(g, st);

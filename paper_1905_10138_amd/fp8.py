@@ -56,7 +56,8 @@ def silu_mul_fp8(X):
 
 def matmul_fp8(A, SA, W, SW, out_dtype=None, Y=None):
     """xorenc_matmul_fp8: Y = A W^T with A (tokens, inputs) in blocks of 1 x 128 and W (outputs, inputs) in blocks of
-    128 x 128.  Y is float32 or bfloat16 (out_dtype, bfloat16 unless given)."""
+    128 x 128.  Y is float32 or bfloat16 (out_dtype, bfloat16 unless given); float32 adds exact products in fp32, bfloat16
+    products that are aligned to a block's largest (include/xorenc.h), which results that cancel to far less than their terms show."""
     return (_native or _load()).matmul(A, SA, W, SW, out_dtype, Y)
 
 
