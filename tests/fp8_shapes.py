@@ -1,5 +1,5 @@
 """Sizes at which the kernels of the products in 8 bits reach their steady state: stages that are filled again while others are
-multiplied, and scales of W of a second run of 64 blocks.  (M, N, K); test_host_plans.py's rule says which kernel each takes."""
+multiplied, and scales of W of a second run of 64 blocks.  (M, N, K); test_host_fp8_plan.py asks which kernel each takes."""
 
 # more than 64 blocks of 128
 LONG = [(9, 64, 8459), (250, 513, 8449), (500, 513, 8303), (700, 1500, 8459), (777, 700, 8303), (1500, 1500, 8303), (1300, 3001, 8449),
