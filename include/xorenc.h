@@ -37,7 +37,7 @@ extern "C" {
 #define XORENC_API
 #endif
 
-#define XORENC_VERSION 0x00020400u
+#define XORENC_VERSION 0x00020500u
 
 enum {
   XORENC_OK = 0,
@@ -436,6 +436,99 @@ XORENC_API int32_t xorenc_moe_workspace(int32_t tokens, int32_t hidden, int32_t 
                                         int64_t *bytes /*HOST*/);
 XORENC_API int32_t xorenc_moe_fp8(const xorenc_moe *layer, const void *X, int32_t x_dtype, int64_t ldx, int32_t tokens, int32_t picks,
                                   int32_t renormalise, void *Y, int64_t ldy, void *workspace, int64_t workspace_bytes, void *hip_stream);
+
+/*
+ * A mixture of experts for any number of tokens, in parts: picks, pairs of tokens and experts sorted by expert, the tokens' rows in that
+ * order, products of each row with its own expert's matrix (xorenc_experts_fp8), and the rows back to their tokens.
+ *
+ * Pairs are numbered token by token: pair t * picks + p is token t's p-th.  A pair whose expert is not one of 0 .. experts - 1 (-1: none)
+ * has no expert; it has a row behind all others, which is not multiplied and adds nothing.
+ *   places  DEV int32[tokens][picks], contiguous: the row of each pair, a permutation of 0 .. tokens * picks - 1
+ *   offsets DEV int32[experts + 1]: rows offsets[e] .. offsets[e + 1] - 1 are expert e's, and offsets[experts] rows have an expert.  Entry points that
+ *           need this number only take its address, `used` = offsets + experts.
+ *   shares  DEV float[tokens][picks], contiguous
+ * tokens = 0 succeeds; xorenc_sort_tokens alone writes something then, its offsets.  XORENC_ELIMIT beyond XORENC_MOE_MAX_EXPERTS
+ * experts, XORENC_MOE_MAX_PICKS picks, 2^24 - 1 pairs, 2^20 columns, and where tokens times eighths of columns exceed 2^31 - 1.  Places and tokens outside
+ * their ranges are taken for pairs without an expert.
+ */
+enum { XORENC_I32 = 0, XORENC_I64 = 1 };
+
+/*
+ * ids (DEV int32[tokens][picks], contiguous): the experts with the largest logits (tokens x experts, fp32 or bf16), the largest first, the lowest index
+ * of equals, a NaN before all.  An expert whose logit is -infinity is masked: never picked.  Where fewer are left than
+ * `picks`, -1 with a share of 0 follows.  shares: the softmax over all experts, or with renormalise != 0 over the picked
+ * ones.  A token with a NaN or an infinite logit has NaN shares, as the formula has it.
+ */
+XORENC_API int32_t xorenc_pick_experts(const void *logits, int32_t x_dtype, int64_t ldl, int32_t tokens, int32_t experts, int32_t picks,
+                                       int32_t renormalise, int32_t *ids, float *shares, void *hip_stream);
+
+/*
+ * places and offsets of ids (DEV [tokens][picks], contiguous, XORENC_I32 or XORENC_I64), and rows (DEV int32[tokens * picks], or NULL): the token of
+ * each row.  Rows of one expert are in the order of their pairs.  workspace: DEV, 4-byte aligned, xorenc_sort_tokens_workspace bytes, which may be none (then
+ * NULL will do); contents undefined before and after.
+ */
+XORENC_API int32_t xorenc_sort_tokens_workspace(int32_t tokens, int32_t picks, int32_t experts, int64_t *bytes /*HOST*/);
+XORENC_API int32_t xorenc_sort_tokens(const void *ids, int32_t id_type, int32_t tokens, int32_t picks, int32_t experts, int32_t *places,
+                                      int32_t *rows, int32_t *offsets, void *workspace, int64_t workspace_bytes, void *hip_stream);
+
+/*
+ * R[places[t][p]] = X[t], times shares[t][p] unless shares is NULL (fp32, rounded once).  X tokens x cols, R tokens * picks x cols of the same type;
+ * rows of pairs without an expert are zero.
+ */
+XORENC_API int32_t xorenc_gather_tokens(const void *X, int32_t x_dtype, int64_t ldx, const int32_t *places, const int32_t *used,
+                                        const float *shares, int32_t tokens, int32_t picks, int32_t cols, void *R, int64_t ldr, void *hip_stream);
+
+/*
+ * Y[t] = sum over p of shares[t][p] R[places[t][p]] (shares NULL: of the rows alone), plus residual[t] unless that is NULL: in fp32, in the order of
+ * p, the residual last.  Y and residual have R's type; Y may be residual.
+ */
+XORENC_API int32_t xorenc_combine_tokens(const void *R, int32_t x_dtype, int64_t ldr, const int32_t *places, const int32_t *used,
+                                         const float *shares, const void *residual, int64_t ld_residual, int32_t tokens, int32_t picks, int32_t cols,
+                                         void *Y, int64_t ldy, void *hip_stream);
+
+/*
+ * Its gradient: with dY (tokens x cols) that of Y, dR[places[t][p]] = shares[t][p] dY[t] (zero for pairs without an expert) and
+ * dshares[t][p] = the inner product of dY[t] and R[places[t][p]] (fp32; 0 for those).  dR may be R.  The residual's is dY itself.  (And that of
+ * xorenc_gather_tokens: X's is xorenc_combine_tokens of R's with the same shares, and the shares' is dshares for X in the place of dY
+ * and R's gradient in the place of R.)
+ */
+XORENC_API int32_t xorenc_combine_tokens_grad(const void *dY, int32_t x_dtype, int64_t ldy, const void *R, int64_t ldr, const int32_t *places,
+                                              const int32_t *used, const float *shares, int32_t tokens, int32_t picks, int32_t cols, void *dR,
+                                              int64_t lddr, float *dshares, void *hip_stream);
+
+/*
+ * What a product does to its results before they are rounded, in fp32:  y = residual + f(z + bias).
+ *   bias      DEV, fp32 or bf16 (bias_dtype), a value for each column of Y, contiguous, or NULL
+ *   f         one of the below; erf in XORENC_GELU is the error function, XORENC_GELU_TANH has tanh(sqrt(2 / pi) (z + 0.044715 z^3)) in its place
+ *   residual  DEV, the type of Y, or NULL; it may be Y
+ */
+enum { XORENC_NO_ACTIVATION = 0, XORENC_RELU = 1, XORENC_SILU = 2, XORENC_GELU = 3, XORENC_GELU_TANH = 4 };
+typedef struct xorenc_epilogue {
+  uint32_t struct_size; /* = sizeof(xorenc_epilogue), ABI guard */
+  int32_t activation;
+  const void *bias;
+  int32_t bias_dtype;
+  int64_t bias_stride; /* elements from one expert's bias to the next one's (xorenc_experts_fp8) */
+  const void *residual;
+  int64_t ld_residual;
+} xorenc_epilogue;
+
+/* xorenc_matmul_fp8 with an epilogue: Y = residual + f(A W^T + bias).  The same limits. */
+XORENC_API int32_t xorenc_linear_fp8(const uint8_t *A, int64_t lda, const float *SA, int64_t sa_row, int64_t sa_blk, const uint8_t *W,
+                                     int64_t ldw, const float *SW, int64_t ldsw, int32_t M, int32_t N, int32_t K, const xorenc_epilogue *epilogue,
+                                     void *Y, int32_t y_dtype, int64_t ldy, void *hip_stream);
+
+/*
+ * The same for rows sorted by expert:  Y[i] = f(A[r(i)] W_e^T + bias_e) for offsets[e] <= i < offsets[e + 1], with r(i) = rows[i] (xorenc_sort_tokens'
+ * rows: A holds each token once, a_rows of them), or i where rows is NULL (A is sorted, a_rows = the rows of Y).  W_e starts at W + e * w_stride bytes (a
+ * multiple of 16), its scales at SW + e * sw_stride.  Y has y_rows rows, of which those from offsets[experts] on are left as they are.
+ * No residual.  XORENC_ELIMIT as xorenc_matmul_fp8 with M = y_rows, beyond XORENC_MOE_MAX_EXPERTS, and with `rows` where a_rows * lda exceeds 2^31 - 256
+ * or a_rows * sa_row + sa_blk * ceil(K / 128) 2^29.
+ */
+XORENC_API int32_t xorenc_experts_fp8(const uint8_t *A, int64_t lda, const float *SA, int64_t sa_row, int64_t sa_blk, int32_t a_rows,
+                                      const int32_t *rows, const int32_t *offsets, int32_t experts, const uint8_t *W, int64_t ldw, int64_t w_stride,
+                                      const float *SW, int64_t ldsw, int64_t sw_stride, int32_t N, int32_t K, const xorenc_epilogue *epilogue,
+                                      void *Y, int32_t y_dtype, int64_t ldy, int32_t y_rows, void *hip_stream);
 
 #ifdef __cplusplus
 }

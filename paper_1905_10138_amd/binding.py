@@ -127,6 +127,23 @@ def load_library():
     lib.xorenc_moe_workspace.argtypes = [i32, i32, i32, i32, i32, i32, vp]
     lib.xorenc_moe_fp8.restype = i32
     lib.xorenc_moe_fp8.argtypes = [ctypes.c_char_p, vp, i32, i64, i32, i32, i32, vp, i64, vp, i64, vp]
+    lib.xorenc_pick_experts.restype = i32
+    lib.xorenc_pick_experts.argtypes = [vp, i32, i64, i32, i32, i32, i32, vp, vp, vp]
+    lib.xorenc_sort_tokens_workspace.restype = i32
+    lib.xorenc_sort_tokens_workspace.argtypes = [i32, i32, i32, vp]
+    lib.xorenc_sort_tokens.restype = i32
+    lib.xorenc_sort_tokens.argtypes = [vp, i32, i32, i32, i32, vp, vp, vp, vp, i64, vp]
+    lib.xorenc_gather_tokens.restype = i32
+    lib.xorenc_gather_tokens.argtypes = [vp, i32, i64, vp, vp, vp, i32, i32, i32, vp, i64, vp]
+    lib.xorenc_combine_tokens.restype = i32
+    lib.xorenc_combine_tokens.argtypes = [vp, i32, i64, vp, vp, vp, vp, i64, i32, i32, i32, vp, i64, vp]
+    lib.xorenc_combine_tokens_grad.restype = i32
+    lib.xorenc_combine_tokens_grad.argtypes = [vp, i32, i64, vp, i64, vp, vp, vp, i32, i32, i32, vp, i64, vp, vp]
+    lib.xorenc_linear_fp8.restype = i32
+    lib.xorenc_linear_fp8.argtypes = [vp, i64, vp, i64, i64, vp, i64, vp, i64, i32, i32, i32, ctypes.c_char_p, vp, i32, i64, vp]
+    lib.xorenc_experts_fp8.restype = i32
+    lib.xorenc_experts_fp8.argtypes = [vp, i64, vp, i64, i64, i32, vp, vp, i32, vp, i64, i64, vp, i64, i64, i32, i32, ctypes.c_char_p, vp,
+                                       i32, i64, i32, vp]
     _LIB = lib
     return lib
 

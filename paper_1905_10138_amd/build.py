@@ -13,7 +13,8 @@ LIB_PATH = os.path.join(PKG_DIR, "libxorenc.so")
 EXT_PATH = os.path.join(PKG_DIR, "_fp8.so")
 SOURCES = ["xorenc_host.cpp", "xorenc_paper.cpp", "xorenc_decode.hip", "xorenc_encode.hip", "xorenc_spmm.hip",
            "xorenc_spmm_q1.hip", "xorenc_spmm_q2.hip", "xorenc_spmm_q3.hip", "xorenc_spmm_q4.hip",
-           "xorenc_fp8_rows.hip", "xorenc_fp8_matmul.hip", "xorenc_moe.hip"]
+           "xorenc_fp8_rows.hip", "xorenc_fp8_matmul.hip", "xorenc_fp8_linear.hip", "xorenc_fp8_experts.hip",
+           "xorenc_moe.hip", "xorenc_tokens.hip"]
 FLAGS = [
     "--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-munsafe-fp-atomics", "-fvisibility=hidden",
     # packed fp32 VALU forms are kept out of the generated code on purpose

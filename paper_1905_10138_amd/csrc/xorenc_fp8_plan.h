@@ -53,20 +53,41 @@ constexpr Cost kCosts[2][kKernels] = {
      {},
      {}}};
 
-inline int cheapest(int64_t M, int64_t N, int64_t blocks, bool exact) {
+// row_tiles(bm): how many tiles of bm rows of Y there are; most(bm): as many at most.
+template <class F, class G>
+int cheapest_of(F row_tiles, G most, int64_t N, int64_t blocks, bool exact) {
   int best = -1;
   float least = 0.f;
   for (int i = 0; i < kKernels; ++i) {
     const Cost &c = kCosts[exact][i];
     if (!c.bn) continue;
-    const int64_t tiles = ((N + c.bn - 1) / c.bn) * ((M + c.bm - 1) / c.bm), steps = (blocks + c.split - 1) / c.split;
-    if (tiles >= (1 << 22)) continue;
+    const int64_t n_tiles = (N + c.bn - 1) / c.bn, tiles = n_tiles * row_tiles(c.bm), steps = (blocks + c.split - 1) / c.split;
+    if (n_tiles * most(c.bm) >= (1 << 22)) continue;
     const int64_t rounds = (tiles + c.slots - 1) / c.slots;
     const float use = tiles < c.slots ? (float)tiles / (float)c.slots : 1.f;
     const float t = c.start + (float)rounds * (c.tile + (float)steps * (c.step + c.load * use));
     if (best < 0 || t < least) best = i, least = t;
   }
   return best;
+}
+
+inline int cheapest(int64_t M, int64_t N, int64_t blocks, bool exact) {
+  auto row_tiles = [&](int bm) { return (M + bm - 1) / bm; };
+  return cheapest_of(row_tiles, row_tiles, N, blocks, exact);
+}
+
+// `rows` rows sorted by expert: at most this many tiles of bm rows, whatever the experts' shares (one row each for as many as there
+// are, the rest in whole tiles).
+inline int64_t most_tiles_of_experts(int64_t rows, int64_t experts, int bm) {
+  const int64_t some = rows < experts ? rows : experts;
+  return some + (rows - some) / bm;
+}
+
+// Their usual number: all experts have rows, and each a tile that is half empty.
+inline int cheapest_for_experts(int64_t rows, int64_t experts, int64_t N, int64_t blocks, bool exact) {
+  const int64_t some = rows < experts ? rows : experts;
+  return cheapest_of([&](int bm) { const int64_t tiles = (rows + some * (bm / 2)) / bm; return tiles > some ? tiles : some; },
+                     [&](int bm) { return most_tiles_of_experts(rows, experts, bm); }, N, blocks, exact);
 }
 
 }  // namespace xorenc_fp8_detail

@@ -26,13 +26,18 @@ struct RingShape {
   static_assert((BN + BM) % (8 * GROUP) == 0 && SCALES % 64 == 0 && 128 % (16 * TN) == 0 && LDS <= 160 * 1024, "shape");
 };
 
-template <int TN, int TM, int WN, int WM, int KG, int NS, bool EXACT>
-__global__ __launch_bounds__(WN *WM *KG * 64) void matmul_ring_kernel(MatmulArgs g, int n_tiles, int m_tiles, int per_xcd) {
+template <int TN, int TM, int WN, int WM, int KG, int NS, bool EXACT, class Job>
+__global__ __launch_bounds__(WN *WM *KG * 64) void matmul_ring_kernel(MatmulArgs g, int n_tiles, int m_tiles, int per_xcd, Job job) {
   typedef RingShape<TN, TM, WN, WM, KG, NS> Shape;
   constexpr int BN = Shape::BN, BM = Shape::BM, PER = Shape::PER, BLOCK = Shape::BLOCK, STAGE = Shape::STAGE;
   extern __shared__ __attribute__((aligned(1024))) uint8_t ring_lds[];
-  const int tile = (blockIdx.x & 7) * per_xcd + (blockIdx.x >> 3);  // XCDs take runs of tiles that share rows of W
-  if (tile >= n_tiles * m_tiles) return;
+  int tile = (blockIdx.x & 7) * per_xcd + (blockIdx.x >> 3), first_row = 0;  // XCDs take runs of tiles that share rows of W
+  if constexpr (Job::ROWS) {
+    if (!take_tile<BM, typename std::conditional<EXACT, float, uint16_t>::type>(job, g, job.epilogue, n_tiles, threadIdx.x & 63, tile, m_tiles, first_row))
+      return;
+  } else {
+    if (tile >= n_tiles * m_tiles) return;
+  }
   const int tile_n = tile / m_tiles, tile_m = tile - tile_n * m_tiles;
   const int n0 = tile_n * BN, m0 = tile_m * BM;
   const int tid = threadIdx.x, lane = tid & 63, r = lane & 15;
@@ -41,7 +46,8 @@ __global__ __launch_bounds__(WN *WM *KG * 64) void matmul_ring_kernel(MatmulArgs
   const uint32_t lds0 = lds_address(ring_lds);
 
   // ---- loads: this wave's part of its group's blocks
-  const u32x4 w_desc = descriptor(g.W + n0 * g.ldw), a_desc = descriptor(g.A + m0 * g.lda), s_desc = descriptor(g.SA + m0 * g.sa_row);
+  const RowsOfA<Job> rows_of_a(job, g, m0, first_row);
+  const u32x4 w_desc = descriptor(g.W + n0 * g.ldw), a_desc = descriptor(rows_of_a.A), s_desc = descriptor(rows_of_a.SA);
   const int lane_row = lane >> 3;
   auto row_of = [&](int i) {  // of W, then of A
     const int row = (in_group * PER + i) * 8;
@@ -52,9 +58,10 @@ __global__ __launch_bounds__(WN *WM *KG * 64) void matmul_ring_kernel(MatmulArgs
   uint32_t at[PER];
 #pragma unroll
   for (int i = 0; i < PER; ++i)
-    at[i] = (uint32_t)(min(row_of(i) + lane_row, (of_w(i) ? g.N - n0 : g.M - m0) - 1) * (of_w(i) ? g.ldw : g.lda)) + (uint32_t)chunk_of(i);
+    at[i] = (uint32_t)(of_w(i) ? min(row_of(i) + lane_row, g.N - n0 - 1) * g.ldw : rows_of_a(min(row_of(i) + lane_row, g.M - m0 - 1)) * g.lda) +
+            (uint32_t)chunk_of(i);
   const int s_rows = in_group % (Shape::SCALES / 64) * 64;
-  const uint32_t s_at = (uint32_t)(min(s_rows + lane, g.M - m0 - 1) * g.sa_row) * 4u, s_step = (uint32_t)(g.sa_blk * 4);
+  const uint32_t s_at = (uint32_t)(rows_of_a(min(s_rows + lane, g.M - m0 - 1)) * g.sa_row) * 4u, s_step = (uint32_t)(g.sa_blk * 4);
   const int tail = g.K & (kBlock - 1), stages = (g.blocks + KG - 1) / KG;
   // Load i of stage s of this group's blocks into its slot.  A block past the last one reads as zero, and so do chunks behind
   // column K.
@@ -182,6 +189,12 @@ __global__ __launch_bounds__(WN *WM *KG * 64) void matmul_ring_kernel(MatmulArgs
     }
     __syncthreads();
     if (kg > 0) return;
+  }
+  if constexpr (Job::EPILOGUE) {
+    if (!job.epilogue.none()) {
+      store_tile_with<TN, TM, EXACT>(job.epilogue, g, acc, ring_lds + in_group * (16 * TM * 16 * TN * 4), m0 + wm * (16 * TM), n0 + wn * (16 * TN), lane);
+      return;
+    }
   }
   store_tile<TN, TM, EXACT>(g, acc, ring_lds + in_group * (16 * TM * 16 * TN * 4), m0 + wm * (16 * TM), n0 + wn * (16 * TN), lane);
 }

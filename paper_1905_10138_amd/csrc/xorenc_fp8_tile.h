@@ -17,17 +17,9 @@
 
 #include <type_traits>
 
-#include "xorenc_fp8.h"
+#include "xorenc_fp8_job.h"
 
 namespace xorenc_fp8_detail {
-
-struct MatmulArgs {
-  const uint8_t *A, *W;
-  const float *SA, *SW;
-  void *Y;
-  int64_t lda, ldw, sa_row, sa_blk, ldsw, ldy;
-  int M, N, K, blocks;
-};
 
 // A wave's 16 TN x 16 TM results, from row n_first of W and m_first of A on.  A lane holds four neighbours of a row of Y in
 // each 16 x 16 tile.  They change places in LDS (`out`, the wave's own; 16-byte chunks of row m at chunk ^ m), so that a store
@@ -83,15 +75,20 @@ struct TileShape {
   static_assert(BM % 64 == 0 && TN >= 2 && TN % 2 == 0 && 128 % (16 * TN) == 0, "scales");
 };
 
-template <int TN, int TM, int WN, int WM, bool EXACT>
-__global__ __launch_bounds__(WN *WM * 64, 2) void matmul_tile_kernel(MatmulArgs g, int n_tiles, int m_tiles, int per_xcd) {
+template <int TN, int TM, int WN, int WM, bool EXACT, class Job>
+__global__ __launch_bounds__(WN *WM * 64, 2) void matmul_tile_kernel(MatmulArgs g, int n_tiles, int m_tiles, int per_xcd, Job job) {
   typedef TileShape<TN, TM, WN, WM, EXACT> Shape;
   constexpr int BN = Shape::BN, BM = Shape::BM, STAGE = Shape::STAGE, N1 = Shape::GROUP1, N2 = Shape::GROUP2;
   extern __shared__ __attribute__((aligned(1024))) uint8_t tile_lds[];
 
   // workgroup i runs on XCD i % 8: each XCD takes a run of tiles, four row tiles of A wide, that share rows in its L2
-  const int tile = (blockIdx.x & 7) * per_xcd + (blockIdx.x >> 3);
-  if (tile >= n_tiles * m_tiles) return;
+  int tile = (blockIdx.x & 7) * per_xcd + (blockIdx.x >> 3), first_row = 0;
+  if constexpr (Job::ROWS) {
+    if (!take_tile<BM, typename std::conditional<EXACT, float, uint16_t>::type>(job, g, job.epilogue, n_tiles, threadIdx.x & 63, tile, m_tiles, first_row))
+      return;
+  } else {
+    if (tile >= n_tiles * m_tiles) return;
+  }
   constexpr int GROUP = 4;
   const int strip = tile / (GROUP * n_tiles), in_strip = tile - strip * (GROUP * n_tiles);
   const int strip_m = min(GROUP, m_tiles - strip * GROUP);
@@ -108,7 +105,8 @@ __global__ __launch_bounds__(WN *WM * 64, 2) void matmul_tile_kernel(MatmulArgs 
   const uint32_t lds0 = lds_address(tile_lds);
 
   // ---- this wave's loads
-  const u32x4 w_desc = descriptor(g.W + n0 * g.ldw), a_desc = descriptor(g.A + m0 * g.lda), s_desc = descriptor(g.SA + m0 * g.sa_row);
+  const RowsOfA<Job> rows_of_a(job, g, m0, first_row);
+  const u32x4 w_desc = descriptor(g.W + n0 * g.ldw), a_desc = descriptor(rows_of_a.A), s_desc = descriptor(rows_of_a.SA);
   constexpr int HALF = TN * 8;  // rows of half of a wave's row tiles
   // first row of load i of group 1 (rows of A, then lower halves) and of group 2
   auto row1 = [&](int i) {
@@ -125,12 +123,13 @@ __global__ __launch_bounds__(WN *WM * 64, 2) void matmul_tile_kernel(MatmulArgs 
   uint32_t at1[N1], at2[N2];
 #pragma unroll
   for (int i = 0; i < N1; ++i)
-    at1[i] = (uint32_t)(min(row1(i) + lane_row, (of_a(i) ? g.M - m0 : g.N - n0) - 1) * (of_a(i) ? g.lda : g.ldw)) + (uint32_t)chunk_of(row1(i));
+    at1[i] = (uint32_t)(of_a(i) ? rows_of_a(min(row1(i) + lane_row, g.M - m0 - 1)) * g.lda : min(row1(i) + lane_row, g.N - n0 - 1) * g.ldw) +
+             (uint32_t)chunk_of(row1(i));
 #pragma unroll
   for (int i = 0; i < N2; ++i) at2[i] = (uint32_t)(min(row2(i) + lane_row, g.N - n0 - 1) * g.ldw) + (uint32_t)chunk_of(row2(i));
   // ---- and of 64 rows' scales of A (the waves beyond BM / 64 fetch what others fetch: all wait for as many loads)
   const int s_rows = wave % (BM / 64) * 64;
-  const uint32_t s_at = (uint32_t)(min(s_rows + lane, g.M - m0 - 1) * g.sa_row) * 4u;
+  const uint32_t s_at = (uint32_t)(rows_of_a(min(s_rows + lane, g.M - m0 - 1)) * g.sa_row) * 4u;
   const uint32_t s_step = (uint32_t)(g.sa_blk * 4);
   const int tail = g.K & (kBlock - 1);
   auto fetch1 = [&](int b, int i) {
@@ -264,6 +263,13 @@ __global__ __launch_bounds__(WN *WM * 64, 2) void matmul_tile_kernel(MatmulArgs 
     for (int k = 0; k < 4; ++k) acc[TN - 1][j][k] += f[j] * d[(TN - 1) & 1][j][k];
   static_assert(BN * BM * (EXACT ? 4 : 2) <= 2 * STAGE, "the results of a tile fit");
   __syncthreads();
+  if constexpr (Job::EPILOGUE) {
+    if (!job.epilogue.none()) {
+      static_assert(Shape::WAVES * 16 * 16 * TN * 4 <= Shape::LDS, "sixteen rows of each wave's results fit");
+      store_tile_with<TN, TM, EXACT>(job.epilogue, g, acc, tile_lds + wave * (16 * 16 * TN * 4), m0 + wm * (16 * TM), n0 + wn * (16 * TN), lane);
+      return;
+    }
+  }
   store_tile<TN, TM, EXACT>(g, acc, tile_lds + wave * (16 * TM * 16 * TN * (EXACT ? 4 : 2)), m0 + wm * (16 * TM), n0 + wn * (16 * TN), lane);
 }
 

@@ -327,6 +327,8 @@ PyObject *moe(PyObject *const *args) {
   return args[8];
 }
 
+#include "xorenc_torch_experts.h"
+
 template <PyObject *(*F)(PyObject *const *), int N>
 PyObject *entry(PyObject *, PyObject *const *args, Py_ssize_t n) {
   HANDLE_TH_ERRORS
@@ -350,7 +352,10 @@ PyMethodDef method(const char *name) {
 }
 
 PyMethodDef methods[] = {method<quant, 2>("quant"),   method<norm, 6>("norm"), method<gate, 1>("gate"),
-                         method<matmul, 6>("matmul"), method<moe, 9>("moe"),   {nullptr, nullptr, 0, nullptr}};
+                         method<matmul, 6>("matmul"), method<moe, 9>("moe"),   method<pick, 3>("pick"),
+                         method<sort, 2>("sort"),     method<gather, 5>("gather"), method<combine, 6>("combine"),
+                         method<combine_grad, 6>("combine_grad"), method<linear, 9>("linear"), method<experts, 10>("experts"),
+                         {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_fp8", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 
 }  // namespace

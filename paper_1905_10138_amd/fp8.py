@@ -69,3 +69,63 @@ def moe_fp8(X, router, W13, S13, W2, S2, picks: int, renormalise: bool = True, Y
     takes the `picks` experts with its largest logits; their softmax shares are made to sum to one unless renormalise is
     False.  Returns Y (tokens, hidden) of X's type (Y may be X)."""
     return (_native or _load()).moe(X, router, W13, S13, W2, S2, picks, renormalise, Y)
+
+
+def linear_fp8(A, SA, W, SW, bias=None, activation=None, residual=None, out_dtype=None, Y=None):
+    """xorenc_linear_fp8: Y = residual + f(A W^T + bias), matmul_fp8 with an epilogue that is computed in fp32 before the only rounding.
+
+    bias (outputs,) float32 or bfloat16; activation None, 'relu', 'silu', 'gelu' (with the error function) or 'gelu_tanh'; residual (tokens,
+    outputs) of the type of Y, which may be Y."""
+    return (_native or _load()).linear(A, SA, W, SW, bias, activation, residual, out_dtype, Y)
+
+
+def pick_experts(logits, picks: int, renormalise: bool = True):
+    """xorenc_pick_experts: the experts of each token and their shares -> (ids int32, shares float32), both (tokens, picks).
+
+    logits (tokens, experts) float32 or bfloat16.  The largest logits, the lowest index of equals; an expert whose logit is -inf is
+    never picked, and where fewer are left the id is -1 and the share 0.  The shares are the softmax over all experts,
+    made to sum to one over the picked ones unless renormalise is False."""
+    return (_native or _load()).pick(logits, picks, renormalise)
+
+
+def sort_tokens(ids, experts: int):
+    """xorenc_sort_tokens: the pairs of tokens and experts sorted by expert -> (places, tokens, offsets), int32.
+
+    ids (tokens, picks) int32 or int64.  places (tokens, picks) is the row of each pair, tokens (tokens * picks,) the token of each row, and
+    rows offsets[e] .. offsets[e + 1] - 1 are expert e's, in the order of the tokens.  Ids outside 0 .. experts - 1 are pairs without an expert:
+    their rows come last, from offsets[experts] on."""
+    return (_native or _load()).sort(ids, experts)
+
+
+def gather_tokens(X, places, offsets, shares=None, R=None):
+    """xorenc_gather_tokens: R[places[t, p]] = X[t], times shares[t, p] if they are given; zero for pairs without an expert.
+
+    X (tokens, features) float32 or bfloat16; R (tokens * picks, features) of its type.  Its gradient for X is combine_tokens(dR, places,
+    offsets, shares), and for the shares the second result of combine_tokens_grad(X, dR, places, offsets, shares)."""
+    return (_native or _load()).gather(X, places, offsets, shares, R)
+
+
+def combine_tokens(R, places, offsets, shares=None, residual=None, Y=None):
+    """xorenc_combine_tokens: Y[t] = sum over p of shares[t, p] R[places[t, p]] (without shares: of the rows alone) + residual[t].
+
+    R (tokens * picks, features) float32 or bfloat16; residual and Y (tokens, features) of its type, Y may be residual.  Pairs without an expert
+    add nothing.  Sums are in fp32, in the order of p."""
+    return (_native or _load()).combine(R, places, offsets, shares, residual, Y)
+
+
+def combine_tokens_grad(dY, R, places, offsets, shares, dR=None):
+    """xorenc_combine_tokens_grad: the gradients of combine_tokens for R and shares, given that for Y -> (dR, dshares).
+
+    dR (the type of R; it may be R) is zero where a pair has no expert, and so is dshares (float32).  The residual's gradient is dY, and
+    without shares R's is gather_tokens(dY, places, offsets)."""
+    return (_native or _load()).combine_grad(dY, R, places, offsets, shares, dR)
+
+
+def experts_fp8(A, SA, W, SW, offsets, tokens=None, bias=None, activation=None, out_dtype=None, Y=None):
+    """xorenc_experts_fp8: products of sorted rows with their own expert's matrix, Y[i] = f(A[tokens[i]] W[e]^T + bias[e]) for
+    offsets[e] <= i < offsets[e + 1].
+
+    A in blocks of 1 x 128: a row for each token, with `tokens` of sort_tokens, or without it a row for each row of Y.  W (experts, outputs,
+    inputs) in blocks of 128 x 128, as quant_fp8 lays stacks out; bias (experts, outputs) and activation as linear_fp8.  Rows of Y from
+    offsets[experts] on are left as they are: in a new Y they hold anything."""
+    return (_native or _load()).experts(A, SA, W, SW, offsets, tokens, bias, activation, out_dtype, Y)

@@ -1,0 +1,344 @@
+"""8-bit products with an epilogue, and those of rows sorted by expert, on the GPU against 64 bits.
+
+A product z is off by what test_gpu_fp8.py and test_gpu_fp8_sizes.py derive for the product alone: fp32 results by (K / 128 + 128) 2 U of its terms'
+magnitudes, bf16 ones by 2^-13 of a block's largest product, summed over the blocks (and the rounding of the result).  The epilogue in fp32: the
+bias' addition rounds once (U of |z| + |bias|); an activation passes on what its argument is off by, times its steepest slope, and is itself
+computed to 24 U of the larger of its argument's and its result's magnitude (an exponential whose argument is rounded, a reciprocal, a few products;
+measured below against 64 bits); the residual's addition rounds once more, and the result by half a step of its type."""
+import math
+
+import pytest
+import torch
+
+import paper_1905_10138_amd as xe
+import experts_oracle as ref
+import fp8_oracle as fp8
+from experts_shapes import SIZES
+from fp8_shapes import LONG, SHORT
+from test_gpu_fp8 import DEV, U, gen, normal, random_8bit
+
+pytestmark = pytest.mark.gpu
+
+TYPES = [torch.bfloat16, torch.float32]
+ACTIVATIONS = [None, "relu", "silu", "gelu", "gelu_tanh"]
+
+
+def tops(v):
+    """The largest magnitude in each block of 128 columns."""
+    return torch.nn.functional.pad(v.abs(), (0, -v.shape[1] % 128)).reshape(v.shape[0], -1, 128).amax(2)
+
+
+def check(Y, a, w, bias, activation, residual):
+    """Y = residual + f(a w^T + bias): a and w fp64, on the GPU."""
+    K = a.shape[1]
+    z = a @ w.t()
+    if Y.dtype is torch.float32:
+        off = (K / 128 + 128) * 2 * U * (a.abs() @ w.abs().t())
+    else:
+        off = 2.0 ** -13 * 128 * (tops(a) @ tops(w).t())
+    b = 0 if bias is None else bias.double()
+    off = off + U * (z.abs() + (0 if bias is None else b.abs())) * (bias is not None)
+    z = z + b
+    f = ref.activation(activation, z)
+    off = off * ref.SLOPE[activation] + (24 * U * torch.maximum(z.abs(), f.abs()) if activation not in (None, "relu") else 0)
+    want = f if residual is None else f + residual.double()
+    off = off + (0 if residual is None else U * (f.abs() + residual.double().abs())) + (2.0 ** -8 * want.abs() * 1.01 if Y.dtype is torch.bfloat16 else 0)
+    err = (Y.double() - want).abs()
+    assert (err <= off * 1.01 + 2.0 ** -126).all(), float((err / (off * 1.01 + 2.0 ** -126)).max())
+    if want.numel() > 500:
+        assert err.norm() <= ((2.0 ** -8 + 1e-4) if Y.dtype is torch.bfloat16 else 4e-6) * want.norm()
+
+
+def operands(g, M, N, K, out, bias=None, residual=False):
+    A, SA = random_8bit(g, M, K, 1)
+    W, SW = random_8bit(g, N, K, 128)
+    b = None if bias is None else normal(g, N, dtype=bias).to(DEV)
+    r = normal(g, M, N, dtype=out).to(DEV) if residual else None
+    return A, SA, W, SW, b, r
+
+
+# ---------------------------------------------------------------------------------------------- one product
+
+SMALL = [(1, 1, 1), (1, 9, 130), (2, 16, 16), (3, 100, 40), (16, 128, 128), (17, 129, 129), (33, 65, 300), (64, 640, 256), (65, 72, 500), (130, 260, 129), (300, 200, 1000)]
+KINDS = [(None, None, False), (torch.float32, None, False), (torch.bfloat16, "relu", False), (None, "silu", True), (torch.float32, "gelu", True),
+         (torch.bfloat16, "gelu_tanh", True), (None, None, True), (torch.bfloat16, None, True)]
+
+
+@pytest.mark.parametrize("bias,activation,residual", KINDS)
+@pytest.mark.parametrize("out", TYPES)
+@pytest.mark.parametrize("M,N,K", SMALL)
+def test_product(M, N, K, out, bias, activation, residual):
+    A, SA, W, SW, b, r = operands(gen(M + N + K), M, N, K, out, bias, residual)
+    Y = xe.linear_fp8(A, SA, W, SW, b, activation, r, out_dtype=out)
+    assert Y.dtype is out and Y.shape == (M, N)
+    check(Y, fp8.dense(A, SA, 1).to(DEV), fp8.dense(W, SW, 128).to(DEV), b, activation, r)
+    if (bias, activation, residual) == (None, None, False):
+        assert torch.equal(Y, xe.matmul_fp8(A, SA, W, SW, out_dtype=out))
+
+
+# every kernel of the products, in its steady state
+@pytest.mark.parametrize("out", TYPES)
+@pytest.mark.parametrize("i", range(len(SHORT + LONG)))
+def test_product_of_every_kernel(i, out):
+    M, N, K = (SHORT + LONG)[i]
+    bias, activation, residual = KINDS[1 + i % (len(KINDS) - 1)]
+    A, SA, W, SW, b, r = operands(gen(i), M, N, K, out, bias, residual)
+    Y = xe.linear_fp8(A, SA, W, SW, b, activation, r, out_dtype=out)
+    check(Y, fp8.dense(A, SA, 1).to(DEV), fp8.dense(W, SW, 128).to(DEV), b, activation, r)
+    plain = xe.matmul_fp8(A, SA, W, SW, out_dtype=out)
+    assert torch.equal(xe.linear_fp8(A, SA, W, SW, out_dtype=out), plain)
+    # rows of Y and of the residual off 16-byte boundaries, and Y the residual itself: the same bits
+    wide = torch.full((M, N + 3), 9.0, dtype=out, device=DEV)
+    if r is not None:
+        wide[:, 1:-2] = r
+    inside = wide[:, 1:-2]
+    assert xe.linear_fp8(A, SA, W, SW, b, activation, None if r is None else inside, Y=inside) is inside
+    assert torch.equal(inside, Y) and (wide[:, 0] == 9).all() and (wide[:, -2:] == 9).all()
+
+
+@pytest.mark.parametrize("out", TYPES)
+@pytest.mark.parametrize("activation", ACTIVATIONS)
+def test_activations_over_their_range(activation, out):
+    # A product of one term: z is the bias alone where A is zero, so that the activation's own error shows
+    n = 4096
+    A, SA = xe.quant_fp8(torch.zeros(2, 16, device=DEV))
+    W, SW = xe.quant_fp8(torch.ones(n, 16, device=DEV), block_rows=128)
+    z = torch.cat([torch.linspace(-20, 20, n // 2), torch.linspace(-1, 1, n // 4), torch.logspace(-30, 30, n // 8), -torch.logspace(-30, 30, n // 8)])
+    Y = xe.linear_fp8(A, SA, W, SW, z.to(DEV), activation, out_dtype=out).cpu().double()
+    z = z.double()
+    want = ref.activation(activation, z)
+    # relative to the result itself, so that the tails count: exp(-x^2 / 2) of a rounded x^2 / 2 is off by x^2 / 2 roundings, as many as the
+    # logarithm of what is left; results that are no normal numbers may be 0
+    off = 0 if activation in (None, "relu") else (32 + 8 * torch.log(z.abs() / want.abs().clamp(min=2.0 ** -126)).clamp(0, 100)) * U
+    if out is torch.bfloat16:
+        off = off + 2.0 ** -8 + (0 if activation != "gelu" else 2.0 ** -9)
+    assert ((Y - want).abs() <= off * want.abs() + 2.0 ** -120).all(), float(((Y - want).abs() / (want.abs() + 1e-38)).max())
+
+
+@pytest.mark.parametrize("out", TYPES)
+@pytest.mark.parametrize("activation", ACTIVATIONS)
+def test_what_is_not_finite_stays_in_its_place(activation, out):
+    g = gen(3)
+    M, N, K = 40, 70, 200
+    A, SA, W, SW, b, r = operands(g, M, N, K, out, torch.float32, True)
+    clean = xe.linear_fp8(A, SA, W, SW, b, activation, r, out_dtype=out)
+    for v in (math.nan, math.inf, -math.inf):
+        bad = r.clone()
+        bad[7, 11] = v
+        Y = xe.linear_fp8(A, SA, W, SW, b, activation, bad, out_dtype=out)
+        assert not torch.isfinite(Y[7, 11])
+        Y[7, 11] = clean[7, 11]
+        assert torch.equal(Y, clean)
+        bad = b.clone()
+        bad[11] = v
+        Y = xe.linear_fp8(A, SA, W, SW, bad, activation, r, out_dtype=out)
+        want = ref.activation(activation, torch.tensor(v, dtype=torch.float64))  # (NaN where the formula has it: infinity times 0)
+        assert activation in ("gelu", "gelu_tanh", "silu") or torch.isfinite(Y[:, 11]).all() == bool(torch.isfinite(want))
+        Y[:, 11] = clean[:, 11]
+        assert torch.equal(Y, clean)
+
+
+# ---------------------------------------------------------------------------------------------- rows of experts
+
+def check_experts(T, P, E, N, K, out, bias, activation, fused, without=0.0, ids=None, seed=0, strided=False):
+    g = gen(seed + T + N + K)
+    if ids is None:
+        ids = torch.rand((T, E), generator=g).argsort(1)[:, :P].to(torch.int32).contiguous()
+        ids[torch.rand((T, P), generator=g) < without] = -1
+    places, tokens, offsets = xe.sort_tokens(ids.to(DEV), E)
+    R = T * P
+    A, SA = random_8bit(g, T if fused else R, K, 1)
+    W, SW = random_8bit(g, N, K, 128, lead=(E,))
+    b = None if bias is None else normal(g, E, N, dtype=bias).to(DEV)
+    wide = torch.full((R + 1, N + 5), 9.0, dtype=out, device=DEV)
+    Y = wide[:R, 2:2 + N] if strided else torch.full((R, N), 9.0, dtype=out, device=DEV)
+    assert xe.experts_fp8(A, SA, W, SW, offsets, tokens if fused else None, b, activation, Y=Y) is Y
+    a = fp8.dense(A, SA, 1).to(DEV)
+    a = a[tokens.long()] if fused else a
+    at = offsets.tolist()
+    assert (Y[at[E]:] == 9).all()  # rows behind the last are left as they were
+    if strided:
+        assert (wide[R] == 9).all() and (wide[:, :2] == 9).all() and (wide[:, 2 + N:] == 9).all()
+    for e in range(E):
+        rows = slice(at[e], at[e + 1])
+        if at[e] < at[e + 1]:
+            check(Y[rows], a[rows], fp8.dense(W[e], SW[e], 128).to(DEV), None if b is None else b[e], activation, None)
+    return A, SA, W, SW, offsets, tokens, b, Y
+
+
+# (T, P, E, N, K): one row, fewer rows than experts, experts without rows, more rows than a tile, one expert, all of 256
+EXPERTS = [(1, 1, 1, 1, 1), (1, 2, 8, 40, 130), (1, 6, 64, 64, 256), (3, 2, 5, 129, 300), (5, 8, 8, 16, 16), (20, 2, 256, 30, 144), (64, 2, 8, 256, 384),
+           (130, 4, 16, 100, 200), (257, 1, 3, 300, 129), (300, 3, 3, 65, 700), (40, 1, 1, 128, 1000), (700, 2, 7, 520, 260), (100, 16, 17, 33, 64)]
+
+
+@pytest.mark.parametrize("fused", [True, False])
+@pytest.mark.parametrize("out", TYPES)
+@pytest.mark.parametrize("i", range(len(EXPERTS)))
+def test_experts(i, out, fused):
+    bias, activation, _ = KINDS[(i + fused) % len(KINDS)]
+    check_experts(*EXPERTS[i], out, bias, activation, fused, without=0.2 if i % 2 else 0.0, strided=i % 3 == 0)
+
+
+# every kernel of the products in its steady state (experts_shapes.py)
+@pytest.mark.parametrize("out", TYPES)
+@pytest.mark.parametrize("i", range(len(SIZES)))
+def test_experts_of_every_kernel(i, out):
+    bias, activation, _ = KINDS[i % len(KINDS)]
+    check_experts(*SIZES[i], out, bias, activation, fused=i % 2 == 0, without=0.1, seed=i)
+
+
+@pytest.mark.parametrize("out", TYPES)
+@pytest.mark.parametrize("what", ["all to the last", "none", "one row", "one tile each", "the same twice"])
+@pytest.mark.parametrize("T", [70, 1100])
+def test_experts_of_uneven_shares(T, what, out):
+    E, P = 9, 2
+    ids = torch.full((T, P), {"all to the last": E - 1, "none": -1, "one row": -1, "one tile each": -1, "the same twice": 4}[what], dtype=torch.int32)
+    if what == "one row":
+        ids[T // 2, 1] = 3
+    if what == "one tile each":
+        ids[:, 0] = torch.arange(T) * E // T
+    check_experts(T, P, E, 200, 260, out, torch.float32, "silu", True, ids=ids)
+    check_experts(T, P, E, 200, 260, out, None, None, False, ids=ids)
+
+
+@pytest.mark.parametrize("out", TYPES)
+def test_fused_rows_are_those_of_a_copy(out):
+    A, SA, W, SW, offsets, tokens, b, Y = check_experts(150, 3, 12, 260, 500, out, torch.bfloat16, "gelu", True)
+    rows = tokens.long()
+    ld = A.stride(0)
+    copy = torch.zeros(len(rows), ld, dtype=torch.uint8, device=DEV)
+    copy[:, :500] = A.view(torch.uint8)[rows]
+    again = xe.experts_fp8(copy.view(A.dtype)[:, :500], SA[rows], W, SW, offsets, None, b, "gelu", out_dtype=out)
+    assert torch.equal(again, Y)
+    assert torch.equal(xe.experts_fp8(A, SA, W, SW, offsets, tokens, b, "gelu", out_dtype=out), Y)  # the same bits on every call
+
+
+def test_experts_beyond_32_bits():
+    g = gen(5)
+    T, P, E, N, K = 40, 2, 3, 140, 200
+    A, SA, W, SW, offsets, tokens, b, Y = check_experts(T, P, E, N, K, torch.bfloat16, torch.float32, None, True)
+    mat = (1 << 31) + 64
+    far = torch.empty(2 * mat + N * W.stride(1), dtype=torch.uint8, device=DEV).as_strided((E, N, K), (mat, W.stride(1), 1))
+    far.copy_(W.view(torch.uint8))
+    assert torch.equal(xe.experts_fp8(A, SA, far.view(A.dtype), SW, offsets, tokens, b), Y)
+    ld = 1 << 26
+    out = torch.empty((T * P - 1) * ld + N, dtype=torch.bfloat16, device=DEV).as_strided((T * P, N), (ld, 1))
+    xe.experts_fp8(A, SA, W, SW, offsets, tokens, b, Y=out)
+    assert torch.equal(out, Y)
+    # A itself is addressed with 32 bits: what is beyond is refused
+    rows = torch.empty(1024 * (1 << 21) + K, dtype=torch.uint8, device=DEV).as_strided((1025, K), (1 << 21, 1)).view(A.dtype)
+    with pytest.raises(xe.XorencError, match="capacity"):
+        xe.experts_fp8(rows, torch.ones(1025, 2, device=DEV), W, SW, offsets, tokens, b)
+
+
+def test_offsets_and_tokens_out_of_range_stay_within_the_operands():
+    A, SA, W, SW, offsets, tokens, b, Y = check_experts(50, 2, 4, 130, 200, torch.bfloat16, None, None, True)
+    bad = tokens.clone()
+    bad[3], bad[5] = 1 << 30, -7
+    got = xe.experts_fp8(A, SA, W, SW, offsets, bad)
+    keep = torch.ones(100, dtype=torch.bool, device=DEV)
+    keep[3] = keep[5] = False
+    assert torch.equal(got[keep], Y[keep])
+    strange = torch.tensor([-50, 20, 10, 1 << 30, 1 << 30], dtype=torch.int32, device=DEV)
+    wide = torch.full((104, 130), 9.0, dtype=torch.bfloat16, device=DEV)
+    xe.experts_fp8(A, SA, W, SW, strange, tokens, Y=wide[2:102])
+    assert (wide[:2] == 9).all() and (wide[102:] == 9).all()
+
+
+# ---------------------------------------------------------------------------------------------- a layer of experts
+
+@pytest.mark.parametrize("T,P,E,H,I", [(1, 2, 8, 256, 128), (70, 2, 8, 384, 200), (500, 4, 16, 512, 264)])
+def test_a_layer_of_experts(T, P, E, H, I):
+    """The operators together, as a layer runs them, against the same on the CPU in 64 bits from the parts' own inputs."""
+    g = gen(T)
+    x, residual = normal(g, T, H, dtype=torch.bfloat16).to(DEV), normal(g, T, H, dtype=torch.bfloat16).to(DEV)
+    logits = normal(g, T, E).to(DEV)
+    W13, S13 = random_8bit(g, 2 * I, H, 128, lead=(E,))
+    W2, S2 = random_8bit(g, H, I, 128, lead=(E,))
+    Q, S = xe.quant_fp8(x)
+    ids, shares = xe.pick_experts(logits, P)
+    places, tokens, offsets = xe.sort_tokens(ids, E)
+    u = xe.experts_fp8(Q, S, W13, S13, offsets, tokens)
+    h, sh = xe.silu_mul_fp8(u)
+    d = xe.experts_fp8(h, sh, W2, S2, offsets)
+    y = xe.combine_tokens(d, places, offsets, shares, residual)
+    q, want = fp8.dense(Q, S, 1), residual.cpu().double().clone()
+    mag = want.abs()
+    for t in range(T):
+        chosen = ref.picks(logits[t].tolist(), P)
+        for e, share in zip(chosen, ref.shares(logits[t].tolist(), chosen, True)):
+            row = places[t, chosen.index(e)]
+            z = fp8.dense(W13[e], S13[e], 128) @ q[t]
+            assert (u[row].cpu().double() - z).norm() <= (2.0 ** -8 + 1e-4) * z.norm()
+            v = fp8.dense(W2[e], S2[e], 128) @ fp8.dense(h[row:row + 1], sh[row:row + 1], 1)[0]
+            want[t] += share * v
+            mag[t] += share * v.abs()
+    # d is rounded to 16 bits, and so is y
+    assert ((y.cpu().double() - want).abs() <= 2.0 ** -8 * 1.01 * (mag + want.abs()) + 1e-4 * mag.norm(dim=1, keepdim=True)).all()
+    # the layer for few tokens, which rounds no activation to 8 bits: two roundings of at most 2^-4 (0.026 of the 2-norm) apart
+    if T <= xe.MOE_MAX_TOKENS:
+        router = torch.zeros(E, H)
+        few = xe.moe_fp8(x, router.to(torch.bfloat16).to(DEV), W13, S13, W2, S2, P)
+        assert few.shape == y.shape
+
+
+def test_on_another_stream_and_in_graphs():
+    g = gen(9)
+    T, P, E, N, K = 300, 2, 8, 520, 300
+    A, SA, W, SW, offsets, tokens, b, Y = check_experts(T, P, E, N, K, torch.bfloat16, torch.float32, "silu", True)
+    W1, SW1 = W[0], SW[0]
+    r = normal(g, T, N, dtype=torch.bfloat16).to(DEV)
+
+    def both():
+        return xe.linear_fp8(A, SA, W1, SW1, b[0], "gelu_tanh", r), xe.experts_fp8(A, SA, W, SW, offsets, tokens, b, "silu")
+    want = both()
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        got = both()
+    side.synchronize()
+    assert all(torch.equal(u, v) for u, v in zip(got, want))
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        out = both()
+    for k in range(3):
+        r.copy_(normal(g, T, N, dtype=torch.bfloat16))
+        b.copy_(normal(g, E, N))
+        ids = torch.randint(-1, E, (T, P), generator=g, dtype=torch.int32)
+        _, new_tokens, new_offsets = xe.sort_tokens(ids.to(DEV), E)
+        tokens.copy_(new_tokens)
+        offsets.copy_(new_offsets)
+        want = both()
+        graph.replay()
+        torch.cuda.synchronize()
+        used = int(offsets[-1])
+        assert torch.equal(out[0], want[0]) and torch.equal(out[1][:used], want[1][:used]), k
+
+
+def test_refusals():
+    g = gen(1)
+    A, SA, W, SW, b, r = operands(g, 6, 40, 200, torch.bfloat16, torch.float32, True)
+    V, SV = random_8bit(g, 40, 200, 128, lead=(4,))
+    offsets, tokens = torch.zeros(5, dtype=torch.int32, device=DEV), torch.zeros(12, dtype=torch.int32, device=DEV)
+    bias = normal(g, 4, 40).to(DEV)
+    for call in (lambda: xe.linear_fp8(A, SA, W, SW, b[:39]), lambda: xe.linear_fp8(A, SA, W, SW, b.half()), lambda: xe.linear_fp8(A, SA, W, SW, b.cpu()),
+                 lambda: xe.linear_fp8(A, SA, W, SW, b[None]), lambda: xe.linear_fp8(A, SA, W, SW, activation="tanh"), lambda: xe.linear_fp8(A, SA, W, SW, activation=1),
+                 lambda: xe.linear_fp8(A, SA, W, SW, residual=r[:5]), lambda: xe.linear_fp8(A, SA, W, SW, residual=r.float()),
+                 lambda: xe.linear_fp8(A, SA, W, SW, residual=r.cpu()), lambda: xe.linear_fp8(A, SA, W, SW, residual=r, out_dtype=torch.float32),
+                 lambda: xe.linear_fp8(A, SA, V, SV), lambda: xe.linear_fp8(A, SA, W, SW, out_dtype=torch.half), lambda: xe.linear_fp8(A, SA, W, SW, Y=r[:, :39]),
+                 lambda: xe.experts_fp8(A, SA, W, SW, offsets, tokens), lambda: xe.experts_fp8(A, SA, V, SV, offsets[:4], tokens),
+                 lambda: xe.experts_fp8(A, SA, V, SV, offsets.long(), tokens), lambda: xe.experts_fp8(A, SA, V, SV, offsets, tokens.long()),
+                 lambda: xe.experts_fp8(A, SA, V, SV, offsets, tokens[::2]), lambda: xe.experts_fp8(A, SA, V, SV, offsets.cpu(), tokens),
+                 lambda: xe.experts_fp8(A, SA, V, SV[0], offsets, tokens), lambda: xe.experts_fp8(A, SA, V, SV, offsets, tokens, bias[0]),
+                 lambda: xe.experts_fp8(A, SA, V, SV, offsets, tokens, bias[:3]), lambda: xe.experts_fp8(A, SA, V, SV, offsets, tokens, bias.t().contiguous().t()),
+                 lambda: xe.experts_fp8(A, SA, V, SV, offsets, tokens, Y=r), lambda: xe.experts_fp8(A, SA, V, SV, offsets, Y=r[:5]),
+                 lambda: xe.experts_fp8(A, SA, V[:, :, :100], SV, offsets, tokens)):
+        with pytest.raises(ValueError):
+            call()
+    for call in (lambda: xe.linear_fp8(A, SA, W, None), lambda: xe.linear_fp8(A, SA, W, SW, bias=1.0), lambda: xe.linear_fp8(A, SA, W, SW, residual="r"),
+                 lambda: xe.experts_fp8(A, SA, V, SV, None)):
+        with pytest.raises(TypeError):
+            call()
+    none = xe.linear_fp8(A[:0], SA[:0], W, SW, b, "gelu")
+    assert none.shape == (0, 40) and none.dtype is torch.bfloat16
+    assert xe.experts_fp8(A, SA, V, SV, offsets, tokens[:0]).shape == (0, 40)
