@@ -83,8 +83,9 @@ __global__ __launch_bounds__(WN *WM * 64, 2) void matmul_tile_kernel(MatmulArgs 
 
   // workgroup i runs on XCD i % 8: each XCD takes a run of tiles, four row tiles of A wide, that share rows in its L2
   int tile = (blockIdx.x & 7) * per_xcd + (blockIdx.x >> 3), first_row = 0;
+  Epilogue epilogue = epilogue_of(job);
   if constexpr (Job::ROWS) {
-    if (!take_tile<BM, typename std::conditional<EXACT, float, uint16_t>::type>(job, g, job.epilogue, n_tiles, threadIdx.x & 63, tile, m_tiles, first_row))
+    if (!take_tile<BM, typename std::conditional<EXACT, float, uint16_t>::type>(job, g, epilogue, n_tiles, threadIdx.x & 63, tile, m_tiles, first_row))
       return;
   } else {
     if (tile >= n_tiles * m_tiles) return;
@@ -264,9 +265,12 @@ __global__ __launch_bounds__(WN *WM * 64, 2) void matmul_tile_kernel(MatmulArgs 
   static_assert(BN * BM * (EXACT ? 4 : 2) <= 2 * STAGE, "the results of a tile fit");
   __syncthreads();
   if constexpr (Job::EPILOGUE) {
-    if (!job.epilogue.none()) {
-      static_assert(Shape::WAVES * 16 * 16 * TN * 4 <= Shape::LDS, "sixteen rows of each wave's results fit");
-      store_tile_with<TN, TM, EXACT>(job.epilogue, g, acc, tile_lds + wave * (16 * 16 * TN * 4), m0 + wm * (16 * TM), n0 + wn * (16 * TN), lane);
+    if (!epilogue.none()) {
+      typedef EpilogueTile<TN, TM, EXACT> Results;
+      static_assert(Shape::WAVES * Results::LDS <= Shape::LDS, "sixteen rows of each wave's results fit");
+      Results results(g, m0 + wm * (16 * TM), n0 + wn * (16 * TN), lane);
+      results.load(epilogue);
+      results.store(epilogue, acc, tile_lds + wave * Results::LDS);
       return;
     }
   }
