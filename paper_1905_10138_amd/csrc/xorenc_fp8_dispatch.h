@@ -26,12 +26,16 @@ void launch_tile(const MatmulArgs &g, const Job &job, hipStream_t st) {
                      n_tiles, m_tiles, per_xcd, job);
 }
 
-template <int TN, int TM, int WN, int WM, int KG, int NS, bool EXACT, class Job>
+// STREAMS: it may be that experts' weights are read past the caches.
+template <int TN, int TM, int WN, int WM, int KG, int NS, bool EXACT, bool STREAMS = false, bool STREAM = false, class Job>
 void launch_ring(const MatmulArgs &g, const Job &job, hipStream_t st) {
   typedef RingShape<TN, TM, WN, WM, KG, NS> Shape;
+  if constexpr (STREAMS && !STREAM) {
+    if (streams_weights(job.y_rows, job.experts, g.ldw * g.N, Shape::BM)) return launch_ring<TN, TM, WN, WM, KG, NS, EXACT, STREAMS, true>(g, job, st);
+  }
   const int n_tiles = (g.N + Shape::BN - 1) / Shape::BN, m_tiles = (int)most_row_tiles(job, g, Shape::BM);
   const int per_xcd = (n_tiles * m_tiles + 7) / 8;
-  hipLaunchKernelGGL((matmul_ring_kernel<TN, TM, WN, WM, KG, NS, EXACT, Job>), dim3((unsigned)(per_xcd * 8)), dim3(Shape::WAVES * 64), Shape::LDS, st,
+  hipLaunchKernelGGL((matmul_ring_kernel<TN, TM, WN, WM, KG, NS, EXACT, Job, STREAM>), dim3((unsigned)(per_xcd * 8)), dim3(Shape::WAVES * 64), Shape::LDS, st,
                      g, n_tiles, m_tiles, per_xcd, job);
 }
 
@@ -43,11 +47,15 @@ int32_t dispatch_matmul(int kernel, const MatmulArgs &g, const Job &job, hipStre
       break;
     case 1: launch_tile<4, 4, 2, 2, EXACT>(g, job, st); break;
     case 2: launch_tile<4, 2, 2, 2, EXACT>(g, job, st); break;
-    case 3: launch_ring<2, 2, 2, 2, 2, 2, EXACT>(g, job, st); break;
+    case 3: launch_ring<2, 2, 2, 2, 2, 2, EXACT, Job::ROWS>(g, job, st); break;
     case 4: launch_ring<2, 2, 2, 2, 1, 2, EXACT>(g, job, st); break;
     case 5: launch_ring<1, 1, 1, 1, 8, 2, EXACT>(g, job, st); break;
-    case 6: launch_ring<2, 2, 1, 1, 8, 2, EXACT>(g, job, st); break;
-    case 7: launch_ring<2, 2, 2, 1, 4, 3, EXACT>(g, job, st); break;
+    case 6:
+      if constexpr (!Job::ROWS) launch_ring<2, 2, 1, 1, 8, 2, EXACT>(g, job, st);
+      break;
+    case 7:
+      if constexpr (!Job::ROWS) launch_ring<2, 2, 2, 1, 4, 3, EXACT>(g, job, st);
+      break;
     case 8:
       if constexpr (!EXACT) launch_ring<2, 2, 2, 2, 2, 3, EXACT>(g, job, st);
       break;
@@ -55,7 +63,13 @@ int32_t dispatch_matmul(int kernel, const MatmulArgs &g, const Job &job, hipStre
       if constexpr (!EXACT) launch_tile<8, 3, 2, 4, EXACT>(g, job, st);
       break;
     case 10:
-      if constexpr (!EXACT) launch_ring<4, 2, 2, 4, 1, 3, EXACT>(g, job, st);
+      if constexpr (!EXACT && !Job::ROWS) launch_ring<4, 2, 2, 4, 1, 3, EXACT>(g, job, st);
+      break;
+    case 11:
+      if constexpr (Job::ROWS) launch_ring<2, 1, 1, 1, 4, 2, EXACT, true>(g, job, st);
+      break;
+    case 12:
+      if constexpr (Job::ROWS) launch_ring<2, 2, 2, 1, 1, 3, EXACT, true>(g, job, st);
       break;
     default: return XORENC_ELIMIT;
   }

@@ -2,6 +2,7 @@
 #ifndef XORENC_FP8_PLAN_H
 #define XORENC_FP8_PLAN_H
 
+#include <cmath>
 #include <cstdint>
 
 namespace xorenc_fp8_detail {
@@ -53,16 +54,14 @@ constexpr Cost kCosts[2][kKernels] = {
      {},
      {}}};
 
-// row_tiles(bm): how many tiles of bm rows of Y there are; most(bm): as many at most.
-template <class F, class G>
-int cheapest_of(F row_tiles, G most, int64_t N, int64_t blocks, bool exact) {
+inline int cheapest(int64_t M, int64_t N, int64_t blocks, bool exact) {
   int best = -1;
   float least = 0.f;
   for (int i = 0; i < kKernels; ++i) {
     const Cost &c = kCosts[exact][i];
     if (!c.bn) continue;
-    const int64_t n_tiles = (N + c.bn - 1) / c.bn, tiles = n_tiles * row_tiles(c.bm), steps = (blocks + c.split - 1) / c.split;
-    if (n_tiles * most(c.bm) >= (1 << 22)) continue;
+    const int64_t tiles = ((N + c.bn - 1) / c.bn) * ((M + c.bm - 1) / c.bm), steps = (blocks + c.split - 1) / c.split;
+    if (tiles >= (1 << 22)) continue;
     const int64_t rounds = (tiles + c.slots - 1) / c.slots;
     const float use = tiles < c.slots ? (float)tiles / (float)c.slots : 1.f;
     const float t = c.start + (float)rounds * (c.tile + (float)steps * (c.step + c.load * use));
@@ -71,10 +70,51 @@ int cheapest_of(F row_tiles, G most, int64_t N, int64_t blocks, bool exact) {
   return best;
 }
 
-inline int cheapest(int64_t M, int64_t N, int64_t blocks, bool exact) {
-  auto row_tiles = [&](int bm) { return (M + bm - 1) / bm; };
-  return cheapest_of(row_tiles, row_tiles, N, blocks, exact);
-}
+// The products of rows sorted by expert.  Their tiles come in all degrees of emptiness, and their weights from memory: the kernels take
+//   start + (rounds + `tail`) * (`tile` + steps * (`step` + `load` * share of the chip in use)) + `byte` * (MB of the weights of experts that have rows),
+// with rounds not rounded, and no tail up to one.  Fitted to 1057 shapes of 1 .. 8192 tokens, 1 .. 8 picks of 2 .. 128 experts of 128 .. 8192 x
+// 128 .. 8192, with experts that differ in their shares by a factor of four; taking the one that this says is the fastest costs 1.6 % (fp32 1.0 %)
+// over taking the one that was.  Some of the times it goes by (us, bf16, in the order of the list; tokens x picks x experts x outputs x inputs):
+//   4096x2x8x8192x4096     346  414  485  763  630 3150 1030  367 1950 1190
+//   2048x8x64x1024x2048     80   85   88  133  108  599  186   73  300  181
+//   512x2x8x4096x4096       73   59   58   75    -    -    -   67  135  110
+//   256x8x64x1024x2048      41   34   34   46   44  109   58   38   57   47
+//   64x2x8x4096x4096        70   48   44   33   42   50   42   63   37   39
+//   64x6x64x2048x1024        -    -   35   43    -   76   65    -   36   31
+//   4x2x8x4096x4096          -    -   38   25    -   25   35    -   20   36
+//   1x6x64x2048x1024         -    -   11  8.2    -  9.4  8.3    -  6.6   11
+struct ExpertsCost {
+  int bn, bm, slots, split;
+  float start, tile, step, load, byte, tail;
+};
+constexpr int kExpertsKernels = 13;  // 0 .. 10 as above, of which 6, 7 and 10 would be the fastest for hardly any size
+constexpr ExpertsCost kExpertsCosts[2][kExpertsKernels] = {
+    {{256, 256, 256, 1, 3.69f, 4.02f, 1.46f, 1.11f, 0.000f, 0.90f},
+     {128, 128, 512, 1, 0.96f, 4.73f, 1.21f, 0.42f, 0.043f, 0.63f},
+     {128, 64, 768, 1, 2.51f, 1.88f, 0.95f, 0.47f, 0.040f, 0.39f},
+     {64, 64, 512, 2, 2.52f, 5.94f, 0.58f, 0.59f, 0.048f, 0.53f},
+     {64, 64, 1024, 1, 0.73f, 2.60f, 0.62f, 0.78f, 0.111f, 0.44f},
+     {16, 16, 512, 8, 1.20f, 3.10f, 0.14f, 0.91f, 0.029f, 0.53f},
+     {},
+     {},
+     {64, 64, 256, 2, 1.39f, 4.00f, 0.57f, 0.17f, 0.043f, 0.76f},
+     {256, 192, 256, 1, 1.58f, 5.01f, 1.54f, 0.31f, 0.008f, 0.61f},
+     {},
+     {32, 16, 768, 4, 1.40f, 1.66f, 0.54f, 0.66f, 0.052f, 0.67f},    // 11: rings of two stages: of 32 x 16, four waves that split the reduction
+     {64, 32, 1024, 1, 1.01f, 2.53f, 0.58f, 0.51f, 0.046f, 0.68f}},  // 12: of three: of 64 x 32, one group of two waves
+    {{},
+     {128, 128, 512, 1, 4.84f, 5.73f, 1.52f, 0.55f, 0.000f, 0.47f},
+     {128, 64, 768, 1, 2.45f, 2.74f, 1.26f, 0.67f, 0.027f, 0.20f},
+     {64, 64, 512, 2, 1.52f, 3.66f, 0.44f, 1.58f, 0.053f, 0.43f},
+     {64, 64, 768, 1, 0.88f, 2.59f, 0.80f, 0.86f, 0.096f, 0.47f},
+     {16, 16, 512, 8, 1.15f, 3.33f, 0.19f, 0.99f, 0.030f, 0.55f},
+     {},
+     {},
+     {},
+     {},
+     {},
+     {32, 16, 768, 4, 1.31f, 1.95f, 0.57f, 0.70f, 0.054f, 0.63f},
+     {64, 32, 1024, 1, 1.02f, 2.79f, 0.88f, 0.47f, 0.046f, 0.60f}}};
 
 // `rows` rows sorted by expert: at most this many tiles of bm rows, whatever the experts' shares (one row each for as many as there
 // are, the rest in whole tiles).
@@ -83,11 +123,30 @@ inline int64_t most_tiles_of_experts(int64_t rows, int64_t experts, int bm) {
   return some + (rows - some) / bm;
 }
 
-// Their usual number: all experts have rows, and each a tile that is half empty.
+// Experts' weights of 96 MB and more, which a last cache of 256 MB would not keep until the next call, are read past the caches where one tile of bm rows
+// takes an expert's (us: 64 tokens, two of eight experts of 4096 x 4096 36.5 and 33.4, 128 tokens 37.1 and 34.1, 30 tokens of 9216 x 4096 71 and 57; 512
+// tokens, two tiles, 74.8 and 77.3).
+inline bool streams_weights(int64_t rows, int64_t experts, int64_t bytes_of_one, int bm) {
+  return bytes_of_one >= ((int64_t)96 << 20) / (rows < experts ? rows : experts) && rows <= experts * bm;
+}
+
 inline int cheapest_for_experts(int64_t rows, int64_t experts, int64_t N, int64_t blocks, bool exact) {
-  const int64_t some = rows < experts ? rows : experts;
-  return cheapest_of([&](int bm) { const int64_t tiles = (rows + some * (bm / 2)) / bm; return tiles > some ? tiles : some; },
-                     [&](int bm) { return most_tiles_of_experts(rows, experts, bm); }, N, blocks, exact);
+  const float all = (float)rows, used = (float)experts * (1.f - expf(-all / (float)experts));  // (experts that have rows)
+  const float weights = used * (float)N * (float)blocks * 128e-6f;
+  int best = -1;
+  float least = 0.f;
+  for (int i = 0; i < kExpertsKernels; ++i) {
+    const ExpertsCost &c = kExpertsCosts[exact][i];
+    if (!c.bn) continue;
+    const int64_t n_tiles = (N + c.bn - 1) / c.bn, steps = (blocks + c.split - 1) / c.split;
+    if (n_tiles * most_tiles_of_experts(rows, experts, c.bm) >= (1 << 22)) continue;
+    const float more = all - used * 0.5f * (float)c.bm;  // an expert's last tile is half empty
+    const float rounds = (float)n_tiles * (used + (more > 0.f ? more / (float)c.bm : 0.f)) / (float)c.slots;
+    const float use = rounds < 1.f ? rounds : 1.f, in_turn = rounds > 1.f ? rounds + c.tail : 1.f;
+    const float t = c.start + in_turn * (c.tile + (float)steps * (c.step + c.load * use)) + c.byte * weights;
+    if (best < 0 || t < least) best = i, least = t;
+  }
+  return best;
 }
 
 }  // namespace xorenc_fp8_detail

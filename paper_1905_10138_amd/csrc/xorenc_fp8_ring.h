@@ -26,7 +26,7 @@ struct RingShape {
   static_assert((BN + BM) % (8 * GROUP) == 0 && SCALES % 64 == 0 && 128 % (16 * TN) == 0 && LDS <= 160 * 1024, "shape");
 };
 
-template <int TN, int TM, int WN, int WM, int KG, int NS, bool EXACT, class Job>
+template <int TN, int TM, int WN, int WM, int KG, int NS, bool EXACT, class Job, bool STREAM>
 __global__ __launch_bounds__(WN *WM *KG * 64) void matmul_ring_kernel(MatmulArgs g, int n_tiles, int m_tiles, int per_xcd, Job job) {
   typedef RingShape<TN, TM, WN, WM, KG, NS> Shape;
   constexpr int BN = Shape::BN, BM = Shape::BM, PER = Shape::PER, BLOCK = Shape::BLOCK, STAGE = Shape::STAGE;
@@ -61,6 +61,11 @@ __global__ __launch_bounds__(WN *WM *KG * 64) void matmul_ring_kernel(MatmulArgs
   for (int i = 0; i < PER; ++i)
     at[i] = (uint32_t)(of_w(i) ? min(row_of(i) + lane_row, g.N - n0 - 1) * g.ldw : rows_of_a(min(row_of(i) + lane_row, g.M - m0 - 1)) * g.lda) +
             (uint32_t)chunk_of(i);
+  if constexpr (Job::ROWS) {  // rows past the expert's last read as zero, from nowhere
+#pragma unroll
+    for (int i = 0; i < PER; ++i)
+      if (!of_w(i) && row_of(i) + lane_row >= g.M - m0) at[i] = kBeyond;
+  }
   const int s_rows = in_group % (Shape::SCALES / 64) * 64;
   const uint32_t s_at = (uint32_t)(rows_of_a(min(s_rows + lane, g.M - m0 - 1)) * g.sa_row) * 4u, s_step = (uint32_t)(g.sa_blk * 4);
   const int tail = g.K & (kBlock - 1), stages = (g.blocks + KG - 1) / KG;
@@ -70,7 +75,9 @@ __global__ __launch_bounds__(WN *WM *KG * 64) void matmul_ring_kernel(MatmulArgs
     const int b = s * KG + kg;
     const uint32_t to = lds0 + (uint32_t)(s % NS) * STAGE + kg * BLOCK;
     const int most = b >= g.blocks ? 0 : tail && b == g.blocks - 1 ? tail : kBlock;  // columns of the block
-    if (i < PER)
+    if (i < PER && STREAM && of_w(i))
+      fetch_16<true>(to + (in_group * PER + i) * 1024, chunk_of(i) >= most ? kBeyond : at[i], w_desc, most ? (uint32_t)b * kBlock : 0u);
+    else if (i < PER)
       fetch_16(to + (in_group * PER + i) * 1024, chunk_of(i) >= most ? kBeyond : at[i], of_w(i) ? w_desc : a_desc, most ? (uint32_t)b * kBlock : 0u);
     else
       fetch_4(to + (BN + BM) * 128 + s_rows * 4, most ? s_at : kBeyond, s_desc, most ? (uint32_t)b * s_step : 0u);

@@ -91,12 +91,15 @@ __global__ __launch_bounds__(WN *WM * 64, 2) void matmul_tile_kernel(MatmulArgs 
     if (tile >= n_tiles * m_tiles) return;
   }
   constexpr int GROUP = 4;
-  const int strip = tile / (GROUP * n_tiles), in_strip = tile - strip * (GROUP * n_tiles);
-  const int strip_m = min(GROUP, m_tiles - strip * GROUP);
+  int group = GROUP;
+  // (an expert's strips are as high as each other, up to six row tiles: a last one alone would read W again for a few rows)
+  if constexpr (Job::ROWS) group = m_tiles <= 6 ? m_tiles : (m_tiles + (m_tiles + 3) / 4 - 1) / ((m_tiles + 3) / 4);
+  const int strip = tile / (group * n_tiles), in_strip = tile - strip * (group * n_tiles);
+  const int strip_m = min(group, m_tiles - strip * group);
   // ... and each strip begins where an XCD's 32 CUs end that began with the strip before: rows of W that come from memory, not from
   // the cache behind the L2s, are then waited for by one XCD, and in the first round (8192 x 16384 x 4096, three sets of operands in turn
   // 553 -> 527 us, 4096 x 9216 x 8192 368 -> 344; one set, which that cache holds, 514 and 521)
-  const int at_n = in_strip / strip_m, tile_m = strip * GROUP + in_strip - at_n * strip_m;
+  const int at_n = in_strip / strip_m, tile_m = strip * group + in_strip - at_n * strip_m;
   const int tile_n = (at_n + strip * (32 / GROUP)) % n_tiles;
   const int n0 = tile_n * BN, m0 = tile_m * BM;
 
@@ -126,6 +129,11 @@ __global__ __launch_bounds__(WN *WM * 64, 2) void matmul_tile_kernel(MatmulArgs 
   for (int i = 0; i < N1; ++i)
     at1[i] = (uint32_t)(of_a(i) ? rows_of_a(min(row1(i) + lane_row, g.M - m0 - 1)) * g.lda : min(row1(i) + lane_row, g.N - n0 - 1) * g.ldw) +
              (uint32_t)chunk_of(row1(i));
+  if constexpr (Job::ROWS) {  // rows past the expert's last read as zero, from nowhere
+#pragma unroll
+    for (int i = 0; i < N1; ++i)
+      if (of_a(i) && row1(i) + lane_row >= g.M - m0) at1[i] = kBeyond;
+  }
 #pragma unroll
   for (int i = 0; i < N2; ++i) at2[i] = (uint32_t)(min(row2(i) + lane_row, g.N - n0 - 1) * g.ldw) + (uint32_t)chunk_of(row2(i));
   // ---- and of 64 rows' scales of A (the waves beyond BM / 64 fetch what others fetch: all wait for as many loads)

@@ -140,6 +140,30 @@ def test_what_is_not_finite_stays_in_its_place(activation, out):
 
 # ---------------------------------------------------------------------------------------------- rows of experts
 
+def random_on_gpu(seed, *shape, block_rows):
+    """Finite e4m3 values of all kinds, on the GPU; scales around 2^-8."""
+    g = torch.Generator(device=DEV).manual_seed(seed)
+    rows, K = shape[-2:]
+    q = torch.randint(0, 256, (*shape[:-1], -(-K // 16) * 16), generator=g, device=DEV, dtype=torch.uint8)
+    q[(q & 0x7f) == 0x7f] = 3                      # (NaN)
+    q[..., K:] = 0x7f                              # what is behind a row's end never reaches a result
+    s = torch.rand((*shape[:-2], -(-rows // block_rows), -(-K // 128)), generator=g, device=DEV) * 2.0 ** -8 + 2.0 ** -9
+    return q.view(torch.float8_e4m3fn)[..., :K], s
+
+
+TABLE = {}
+
+
+def dense_on_gpu(Q, S, block_rows):
+    """fp8.dense on the GPU: every code's value comes from there."""
+    if not TABLE:
+        codes = torch.arange(256, dtype=torch.uint8).view(torch.float8_e4m3fn)[None]
+        TABLE["e4m3"] = fp8.dense(codes, torch.ones(1, 2), 1)[0].to(DEV)
+    r = torch.arange(Q.shape[0], device=DEV) // block_rows
+    c = torch.arange(Q.shape[1], device=DEV) // 128
+    return TABLE["e4m3"][Q.view(torch.uint8).long()] * S.double()[r][:, c]
+
+
 def check_experts(T, P, E, N, K, out, bias, activation, fused, without=0.0, ids=None, seed=0, strided=False):
     g = gen(seed + T + N + K)
     if ids is None:
@@ -147,13 +171,13 @@ def check_experts(T, P, E, N, K, out, bias, activation, fused, without=0.0, ids=
         ids[torch.rand((T, P), generator=g) < without] = -1
     places, tokens, offsets = xe.sort_tokens(ids.to(DEV), E)
     R = T * P
-    A, SA = random_8bit(g, T if fused else R, K, 1)
-    W, SW = random_8bit(g, N, K, 128, lead=(E,))
+    A, SA = random_on_gpu(seed + 1, T if fused else R, K, block_rows=1)
+    W, SW = random_on_gpu(seed + 2, E, N, K, block_rows=128)
     b = None if bias is None else normal(g, E, N, dtype=bias).to(DEV)
     wide = torch.full((R + 1, N + 5), 9.0, dtype=out, device=DEV)
     Y = wide[:R, 2:2 + N] if strided else torch.full((R, N), 9.0, dtype=out, device=DEV)
     assert xe.experts_fp8(A, SA, W, SW, offsets, tokens if fused else None, b, activation, Y=Y) is Y
-    a = fp8.dense(A, SA, 1).to(DEV)
+    a = dense_on_gpu(A, SA, 1)
     a = a[tokens.long()] if fused else a
     at = offsets.tolist()
     assert (Y[at[E]:] == 9).all()  # rows behind the last are left as they were
@@ -162,7 +186,7 @@ def check_experts(T, P, E, N, K, out, bias, activation, fused, without=0.0, ids=
     for e in range(E):
         rows = slice(at[e], at[e + 1])
         if at[e] < at[e + 1]:
-            check(Y[rows], a[rows], fp8.dense(W[e], SW[e], 128).to(DEV), None if b is None else b[e], activation, None)
+            check(Y[rows], a[rows], dense_on_gpu(W[e], SW[e], 128), None if b is None else b[e], activation, None)
     return A, SA, W, SW, offsets, tokens, b, Y
 
 
