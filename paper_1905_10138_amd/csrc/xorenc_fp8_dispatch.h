@@ -66,7 +66,7 @@ int32_t dispatch_matmul(int kernel, const MatmulArgs &g, const Job &job, hipStre
       if constexpr (!EXACT && !Job::ROWS) launch_ring<4, 2, 2, 4, 1, 3, EXACT>(g, job, st);
       break;
     case 11:
-      if constexpr (Job::ROWS) launch_ring<2, 1, 1, 1, 4, 2, EXACT, true>(g, job, st);
+      if constexpr (Job::EPILOGUE) launch_ring<2, 1, 1, 1, 4, 2, EXACT, Job::ROWS>(g, job, st);
       break;
     case 12:
       if constexpr (Job::ROWS) launch_ring<2, 2, 2, 1, 1, 3, EXACT, true>(g, job, st);

@@ -19,7 +19,7 @@ struct Epilogue {
   const void *bias, *residual;
   int64_t ld_residual;
   int bias_bf16, activation;
-  __device__ __forceinline__ bool none() const { return !bias && !residual && activation == XORENC_NO_ACTIVATION; }
+  __host__ __device__ __forceinline__ bool none() const { return !bias && !residual && activation == XORENC_NO_ACTIVATION; }
 };
 
 // The jobs.  ROWS: rows of A and Y belong to experts.
@@ -27,7 +27,7 @@ struct Plain {
   static constexpr bool EPILOGUE = false, ROWS = false;
 };
 struct Linear {
-  static constexpr bool EPILOGUE = true, ROWS = false;
+  static constexpr bool EPILOGUE = true, ROWS = false;  // (there is something to do)
   Epilogue epilogue;
 };
 struct Experts {

@@ -54,20 +54,35 @@ constexpr Cost kCosts[2][kKernels] = {
      {},
      {}}};
 
+inline bool takes(const Cost &c, int64_t M, int64_t N, int64_t blocks, float *us) {
+  if (!c.bn) return false;
+  const int64_t tiles = ((N + c.bn - 1) / c.bn) * ((M + c.bm - 1) / c.bm), steps = (blocks + c.split - 1) / c.split;
+  if (tiles >= (1 << 22)) return false;
+  const int64_t rounds = (tiles + c.slots - 1) / c.slots;
+  const float use = tiles < c.slots ? (float)tiles / (float)c.slots : 1.f;
+  *us = c.start + (float)rounds * (c.tile + (float)steps * (c.step + c.load * use));
+  return true;
+}
+
 inline int cheapest(int64_t M, int64_t N, int64_t blocks, bool exact) {
   int best = -1;
-  float least = 0.f;
-  for (int i = 0; i < kKernels; ++i) {
-    const Cost &c = kCosts[exact][i];
-    if (!c.bn) continue;
-    const int64_t tiles = ((N + c.bn - 1) / c.bn) * ((M + c.bm - 1) / c.bm), steps = (blocks + c.split - 1) / c.split;
-    if (tiles >= (1 << 22)) continue;
-    const int64_t rounds = (tiles + c.slots - 1) / c.slots;
-    const float use = tiles < c.slots ? (float)tiles / (float)c.slots : 1.f;
-    const float t = c.start + (float)rounds * (c.tile + (float)steps * (c.step + c.load * use));
-    if (best < 0 || t < least) best = i, least = t;
-  }
+  float least = 0.f, t;
+  for (int i = 0; i < kKernels; ++i)
+    if (takes(kCosts[exact][i], M, N, blocks, &t) && (best < 0 || t < least)) best = i, least = t;
   return best;
+}
+
+// The products with an epilogue have one kernel more: rings of two stages, of 32 x 16, four waves that split the reduction (11).  Of 1363 shapes of 1 .. 64 x
+// 128 .. 16384 x 128 .. 9216 it is the fastest of 560 (fp32 530); the choice costs 1.9 % (0.6 %) over the fastest kernel's times, without it 3.4 %
+// (3.1 %).  (us, with a bias, this and the fastest of the others: 1 x 9216 x 4096 9.3 and 10.2, 1 x 16384 x 4096 12.0 and 13.4, 32 x 9216 x 4096 10.1 and 10.7, 16 x 4096 x
+// 4096 8.2 and 5.8.)
+constexpr Cost kFewRows[2] = {{32, 16, 768, 4, 3.52f, 0.33f, 0.35f, 0.75f}, {32, 16, 768, 4, 3.41f, 0.39f, 0.40f, 0.78f}};
+constexpr int kFewRowsKernel = 11;
+inline int cheapest_for_linear(int64_t M, int64_t N, int64_t blocks, bool exact) {
+  const int best = cheapest(M, N, blocks, exact);
+  float few, least;
+  return M <= 64 && best >= 0 && takes(kFewRows[exact], M, N, blocks, &few) && takes(kCosts[exact][best], M, N, blocks, &least) && few < least
+             ? kFewRowsKernel : best;
 }
 
 // The products of rows sorted by expert.  Their tiles come in all degrees of emptiness, and their weights from memory: the kernels take

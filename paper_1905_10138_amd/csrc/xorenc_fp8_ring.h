@@ -89,7 +89,7 @@ __global__ __launch_bounds__(WN *WM *KG * 64) void matmul_ring_kernel(MatmulArgs
   EpilogueTile<TN, TM, EXACT> results(g, m0 + wm * (16 * TM), n0 + wn * (16 * TN), lane);
   // Before the loop, so that nothing waits for it at the end (1 x 9216 x 4096 with a bias 11.0 -> 10.3 us, onto a residual 11.7 -> 10.3), but not where the
   // registers that this takes cost a workgroup of the CU (128 rows, eight experts of 4096 x 4096 36 -> 47).
-  constexpr bool EARLY = Shape::LDS > 80 * 1024 || TN * TM == 1;
+  constexpr bool EARLY = Shape::LDS > 80 * 1024 || TN * TM <= 2;
   if constexpr (Job::EPILOGUE && EARLY) {
     if (kg == 0) results.load(epilogue);
   }
@@ -206,7 +206,7 @@ __global__ __launch_bounds__(WN *WM *KG * 64) void matmul_ring_kernel(MatmulArgs
     if (kg > 0) return;
   }
   if constexpr (Job::EPILOGUE) {
-    if (!epilogue.none()) {
+    if (!Job::ROWS || !epilogue.none()) {
       if constexpr (!EARLY) results.load(epilogue);
       results.store(epilogue, acc, ring_lds + in_group * (16 * TM * 16 * TN * 4));
       return;

@@ -13,7 +13,7 @@ import torch
 import paper_1905_10138_amd as xe
 import experts_oracle as ref
 import fp8_oracle as fp8
-from experts_shapes import SIZES
+from experts_shapes import FEW, SIZES
 from fp8_shapes import LONG, SHORT
 from test_gpu_fp8 import DEV, U, gen, normal, random_8bit
 
@@ -78,9 +78,9 @@ def test_product(M, N, K, out, bias, activation, residual):
 
 # every kernel of the products, in its steady state
 @pytest.mark.parametrize("out", TYPES)
-@pytest.mark.parametrize("i", range(len(SHORT + LONG)))
+@pytest.mark.parametrize("i", range(len(SHORT + LONG + FEW)))
 def test_product_of_every_kernel(i, out):
-    M, N, K = (SHORT + LONG)[i]
+    M, N, K = (SHORT + LONG + FEW)[i]
     bias, activation, residual = KINDS[1 + i % (len(KINDS) - 1)]
     A, SA, W, SW, b, r = operands(gen(i), M, N, K, out, bias, residual)
     Y = xe.linear_fp8(A, SA, W, SW, b, activation, r, out_dtype=out)

@@ -1,5 +1,5 @@
 """The rule that chooses between the kernels of the experts' products, and the sizes at which the GPU tests run them."""
-from experts_shapes import SIZES
+from experts_shapes import FEW, SIZES
 from test_host_plans import run_program
 
 PROGRAM = r"""
@@ -59,6 +59,29 @@ int main() {
   return bad;
 }
 """
+
+
+LINEAR = r"""
+#include <cstdio>
+#include "xorenc_fp8_plan.h"
+using namespace xorenc_fp8_detail;
+struct Size { int64_t M, N, K; };
+static const Size sizes[] = {%s};
+int main() {
+  bool steady[2] = {}, second_run[2] = {};
+  for (int exact = 0; exact < 2; ++exact)
+    for (const Size &s : sizes)
+      if (cheapest_for_linear(s.M, s.N, (s.K + 127) / 128, exact) == kFewRowsKernel) {
+        if (s.K %% 16 && s.K > 5 * 4 * 128) steady[exact] = true;
+        if (s.K > 64 * 128) second_run[exact] = true;
+      }
+  return !(steady[0] && steady[1] && second_run[0] && second_run[1]);
+}
+"""
+
+
+def test_tests_reach_the_kernel_for_few_rows(tmp_path):
+    run_program(tmp_path, LINEAR % ", ".join("{%d, %d, %d}" % s for s in FEW))
 
 
 def text(sizes):
