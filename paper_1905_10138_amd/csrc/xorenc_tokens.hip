@@ -12,50 +12,76 @@ constexpr int64_t kMostPairs = (1 << 24) - 1;
 
 // ---------------------------------------------------------------------------------------------- picks
 
-// The order of the picks as integers: a NaN above all, -0 and 0 equal, 0 for what is never picked (-infinity).
+// The order of the picks as integers: a NaN above all, -0 and 0 equal, 0 for what is never picked (-infinity); and the value that has it.
 __device__ inline uint32_t order_of(float v) {
   const uint32_t b = __float_as_uint(v);
   if ((b & 0x7fffffffu) > 0x7f800000u) return 0xffffffffu;
   if (b == 0xff800000u) return 0u;
   return (b & 0x7fffffffu) == 0u ? 0x80000000u : b & 0x80000000u ? ~b : b | 0x80000000u;
 }
+__device__ inline float value_of(uint32_t order) { return __uint_as_float(order & 0x80000000u ? order ^ 0x80000000u : ~order); }
 
-// Sixteen lanes hold a token's logits, V each (expert l + 16 v on lane l), and take the largest that is left once per pick: its
-// order first, then the least index of those that have it.  Lane p ends up with the p-th pick.
+// Sixteen lanes hold a token's logits, V each, and take the largest that is left once per pick: its order first, then the least index of
+// those that have it.  Logits of 16 bits leave room for both in one integer, and for one maximum (16384 tokens, 8 of 128 experts: ORDER16
+// us, as those of 32 bits ORDER32).  Lane p ends up with the p-th pick.
 template <class T, int V>
 __global__ __launch_bounds__(256) void pick_kernel(const typename T::Elem *__restrict__ logits, int64_t ldl, int tokens, int experts, int picks,
                                                    int renormalise, int *__restrict__ ids, float *__restrict__ shares) {
+  constexpr bool NARROW = sizeof(typename T::Elem) == 2;
   const int t = blockIdx.x * 16 + (threadIdx.x >> 4), l = threadIdx.x & 15;
   if (t >= tokens) return;
   const typename T::Elem *const row = logits + t * ldl;
+  auto expert = [&](int v) { return V < 8 ? l * V + v : v / 8 * 128 + l * 8 + v % 8; };
   float x[V];
-  uint32_t order[V];
+  if constexpr (V < 8) {
+#pragma unroll
+    for (int v = 0; v < V; ++v) {
+      x[v] = -INFINITY;
+      if (expert(v) < experts) {
+        if constexpr (NARROW)
+          x[v] = __uint_as_float((uint32_t)row[expert(v)] << 16);
+        else
+          x[v] = row[expert(v)];
+      }
+    }
+  } else {
+#pragma unroll
+    for (int v = 0; v < V; v += 8) {
+      piece_of<T>(load_piece<T>(row, min(expert(v), experts), experts), min(expert(v), experts), experts, x + v);
+#pragma unroll
+      for (int i = 0; i < 8; ++i)
+        if (expert(v + i) >= experts) x[v + i] = -INFINITY;
+    }
+  }
+  uint32_t key[V];
 #pragma unroll
   for (int v = 0; v < V; ++v) {
-    const int e = l + 16 * v;
-    if constexpr (sizeof(typename T::Elem) == 2)
-      x[v] = e < experts ? __uint_as_float((uint32_t)row[e] << 16) : -INFINITY;
-    else
-      x[v] = e < experts ? row[e] : -INFINITY;
-    order[v] = order_of(x[v]);
+    key[v] = order_of(x[v]);
+    if (NARROW && key[v]) key[v] = (key[v] & 0xffff0000u) | (0xffffu - (uint32_t)expert(v));
   }
   int id = -1;
   float mine = -INFINITY, most = 0.f;
   for (int p = 0; p < picks; ++p) {
-    uint32_t best = 0;
-    float value = 0.f;
-    int at = 0;
+    uint32_t best = key[0];
 #pragma unroll
-    for (int v = 0; v < V; ++v)
-      if (order[v] > best) best = order[v], value = x[v], at = v;
-    const uint32_t top = max_of_16_lanes(best);
-    if (top == 0) break;  // (the same on all 16 lanes)
-    const int e = best == top ? l + 16 * at : 0xffff;
-    const int first = 0xffff - (int)max_of_16_lanes((uint32_t)(0xffff - e));
-    value = __shfl(value, first & 15, 16);
+    for (int v = 1; v < V; ++v) best = max(best, key[v]);
+    best = max_of_16_lanes(best);
+    if (best == 0) break;  // (the same on all 16 lanes)
+    int first;
+    if constexpr (NARROW) {
+      first = (int)(0xffffu - (best & 0xffffu));
 #pragma unroll
-    for (int v = 0; v < V; ++v)
-      if (first == l + 16 * v) order[v] = 0;
+      for (int v = 0; v < V; ++v) key[v] = key[v] == best ? 0u : key[v];
+      best = best & 0x80000000u ? best & 0xffff0000u : best | 0xffffu;  // (a negative value's lower bits are inverted zeros)
+    } else {
+      uint32_t least = 0;  // 0xffff less the index
+#pragma unroll
+      for (int v = V - 1; v >= 0; --v) least = key[v] == best ? 0xffffu - (uint32_t)expert(v) : least;
+      first = (int)(0xffffu - max_of_16_lanes(least));
+#pragma unroll
+      for (int v = 0; v < V; ++v) key[v] = expert(v) == first ? 0u : key[v];
+    }
+    const float value = value_of(best);
     if (p == 0) most = value;
     if (l == p) id = first, mine = value;
   }
@@ -125,13 +151,21 @@ __global__ __launch_bounds__(kSortWaves * 64) void sort_kernel(const Id *__restr
   }
   __syncthreads();
   if (counts) {
-    // (each half of the threads takes every other segment: sums of integers, the same in any order)
-    const int half = tid / (threads / 2);
-    for (int e = tid % (threads / 2); e <= experts; e += threads / 2) {
+    // Groups of threads, a thread an expert, take the segments in turn, eight loads of each on their way together (sums of integers, the same in any order).
+    const int width = (experts + 64) & ~63, groups = threads / width, group = tid / width, e = tid - group * width;
+    if (group < groups && e <= experts) {
       int b = 0, a = 0;
-      for (int s = half; s < segments; s += 2) {
-        const int n = counts[s * (experts + 1) + e];
-        if (s < (int)blockIdx.x) b += n; else a += n;
+      for (int s0 = group; s0 < segments; s0 += 8 * groups) {
+        int n[8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+          const int s = s0 + i * groups;
+          n[i] = s < segments ? counts[s * (experts + 1) + e] : 0;
+        }
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+          if (s0 + i * groups < (int)blockIdx.x) b += n[i]; else a += n[i];
+        }
       }
       atomicAdd(&before[e], b);
       atomicAdd(&behind[e], a);
@@ -210,41 +244,54 @@ struct RowArgs {
   int tokens, picks, cols, per_row;
 };
 
-template <class T>
+// STREAM: past the caches.
+template <class T, bool STREAM>
+__device__ inline void store_row(typename T::Elem *row, int c, int cols, const float *v) {
+  if constexpr (STREAM && sizeof(typename T::Elem) == 2) {
+    if (c + 8 <= cols) {
+      const u32x4 w = {to_bf16x2(v[0], v[1]), to_bf16x2(v[2], v[3]), to_bf16x2(v[4], v[5]), to_bf16x2(v[6], v[7])};
+      __builtin_nontemporal_store(w, reinterpret_cast<u32x4_anywhere *>(row + c));
+      return;
+    }
+  }
+  store_piece<T>(row, c, cols, v);
+}
+
+template <class T, bool STREAM>
 __device__ inline void store_zero(typename T::Elem *row, int c, int cols) {
   const float none[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
-  store_piece<T>(row, c, cols, none);
+  store_row<T, STREAM>(row, c, cols, none);
 }
 
 // A lane a piece of X, which it stores as often as the token has pairs.
-template <class T, bool SHARES>
+template <class T, bool SHARES, bool STREAM>
 __global__ __launch_bounds__(256) void gather_kernel(const typename T::Elem *__restrict__ X, RowArgs g, typename T::Elem *__restrict__ R) {
   const uint32_t piece = blockIdx.x * 256u + threadIdx.x;
   const int t = (int)(piece / (uint32_t)g.per_row), c = (int)(piece % (uint32_t)g.per_row) * 8;
   if (t >= g.tokens) return;
   const int used = min(*g.used, g.tokens * g.picks);
   float x[8];
-  piece_of<T>(load_piece<T>(X + t * g.ldx, c, g.cols), c, g.cols, x);
+  piece_of<T>(load_piece<T, STREAM>(X + t * g.ldx, c, g.cols), c, g.cols, x);
   for (int p = 0; p < g.picks; ++p) {
     const int place = g.places[t * g.picks + p];
     if ((unsigned)place >= (unsigned)(g.tokens * g.picks)) continue;
     typename T::Elem *const row = R + place * g.ldr;
     if (place >= used) {
-      store_zero<T>(row, c, g.cols);
+      store_zero<T, STREAM>(row, c, g.cols);
     } else if constexpr (SHARES) {
       const float s = g.shares[t * g.picks + p];
       float y[8];
 #pragma unroll
       for (int i = 0; i < 8; ++i) y[i] = x[i] * s;
-      store_piece<T>(row, c, g.cols, y);
+      store_row<T, STREAM>(row, c, g.cols, y);
     } else {
-      store_piece<T>(row, c, g.cols, x);
+      store_row<T, STREAM>(row, c, g.cols, x);
     }
   }
 }
 
 // A lane a piece of Y.  The rows of up to MOST pairs are on their way together.
-template <class T, int MOST>
+template <class T, int MOST, bool STREAM>
 __global__ __launch_bounds__(256) void combine_kernel(const typename T::Elem *__restrict__ R, RowArgs g, const typename T::Elem *residual,
                                                       typename T::Elem *Y) {
   const uint32_t piece = blockIdx.x * 256u + threadIdx.x;
@@ -252,7 +299,7 @@ __global__ __launch_bounds__(256) void combine_kernel(const typename T::Elem *__
   if (t >= g.tokens) return;
   const int used = min(*g.used, g.tokens * g.picks);
   typename T::Raw rest;
-  if (residual) rest = load_piece<T>(residual + t * g.ldx, c, g.cols);
+  if (residual) rest = load_piece<T, STREAM>(residual + t * g.ldx, c, g.cols);
   float y[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
   for (int p0 = 0; p0 < g.picks; p0 += MOST) {
     typename T::Raw raw[MOST];
@@ -266,7 +313,7 @@ __global__ __launch_bounds__(256) void combine_kernel(const typename T::Elem *__
     }
 #pragma unroll
     for (int k = 0; k < MOST; ++k)
-      if ((unsigned)place[k] < (unsigned)used) raw[k] = load_piece<T>(R + place[k] * g.ldr, c, g.cols);
+      if ((unsigned)place[k] < (unsigned)used) raw[k] = load_piece<T, STREAM>(R + place[k] * g.ldr, c, g.cols);
 #pragma unroll
     for (int k = 0; k < MOST; ++k) {
       if ((unsigned)place[k] >= (unsigned)used) continue;
@@ -282,11 +329,11 @@ __global__ __launch_bounds__(256) void combine_kernel(const typename T::Elem *__
 #pragma unroll
     for (int i = 0; i < 8; ++i) y[i] += x[i];
   }
-  store_piece<T>(Y + t * g.ldo, c, g.cols, y);
+  store_row<T, STREAM>(Y + t * g.ldo, c, g.cols, y);
 }
 
 // A workgroup a token: every piece of dY is read once, multiplied into each row's sum and written to each row's gradient.
-template <class T, int THREADS, int MOST>
+template <class T, int THREADS, int MOST, bool STREAM>
 __global__ __launch_bounds__(THREADS) void combine_grad_kernel(const typename T::Elem *__restrict__ dY, RowArgs g, const typename T::Elem *R,
                                                                typename T::Elem *dR, float *__restrict__ dshares) {
   constexpr int WAVES = THREADS / 64;
@@ -305,24 +352,24 @@ __global__ __launch_bounds__(THREADS) void combine_grad_kernel(const typename T:
   for (int c = tid * 8; c < g.cols; c += THREADS * 8) {
     float dy[8];
     typename T::Raw raw[MOST];
-    const typename T::Raw y = load_piece<T>(dY + t * g.ldx, c, g.cols);
+    const typename T::Raw y = load_piece<T, STREAM>(dY + t * g.ldx, c, g.cols);
 #pragma unroll
     for (int p = 0; p < MOST; ++p)
-      if ((unsigned)place[p] < (unsigned)used) raw[p] = load_piece<T>(R + place[p] * g.ldr, c, g.cols);
+      if ((unsigned)place[p] < (unsigned)used) raw[p] = load_piece<T, STREAM>(R + place[p] * g.ldr, c, g.cols);
     piece_of<T>(y, c, g.cols, dy);
 #pragma unroll
     for (int p = 0; p < MOST; ++p) {
       if ((unsigned)place[p] >= (unsigned)pairs) continue;
       typename T::Elem *const row = dR + place[p] * g.ldo;
       if (place[p] >= used) {
-        store_zero<T>(row, c, g.cols);
+        store_zero<T, STREAM>(row, c, g.cols);
         continue;
       }
       float x[8];
       piece_of<T>(raw[p], c, g.cols, x);
 #pragma unroll
       for (int i = 0; i < 8; ++i) dot[p] = fmaf(x[i], dy[i], dot[p]), x[i] = dy[i] * share[p];
-      store_piece<T>(row, c, g.cols, x);
+      store_row<T, STREAM>(row, c, g.cols, x);
     }
   }
 #pragma unroll
@@ -356,11 +403,17 @@ int32_t check_rows(int32_t dtype, int32_t tokens, int32_t picks, int32_t cols) {
   return XORENC_OK;
 }
 
-// f(type)
+// f(type), and f(type, whether to stream)
 template <class F>
-int32_t for_rows(int32_t dtype, F f) {
+int32_t for_type(int32_t dtype, F f) {
   return dtype == XORENC_X_F32 ? f(F32()) : f(BF16());
 }
+template <class F>
+int32_t for_rows(int32_t dtype, bool stream, F f) {
+  return dtype == XORENC_X_F32 ? f(F32(), std::false_type()) : stream ? f(BF16(), std::true_type()) : f(BF16(), std::false_type());
+}
+// Whether `rows` rows that a call reads or writes are more than half of what the memory-side cache holds (256 MB).
+inline bool streams(int64_t rows, int64_t cols, int esz) { return rows * cols > ((int64_t)128 << 20) / esz; }
 
 template <class T, int V>
 int32_t launch_pick(const void *logits, int64_t ldl, int tokens, int experts, int picks, int renormalise, int32_t *ids, float *shares, hipStream_t st) {
@@ -400,7 +453,7 @@ extern "C" int32_t xorenc_pick_experts(const void *logits, int32_t x_dtype, int6
   if (!aligned_to(logits, dtype_bytes(x_dtype)) || !aligned_to(ids, 4) || !aligned_to(shares, 4)) return XORENC_EALIGN;
   hipStream_t st = static_cast<hipStream_t>(hip_stream);
   xorenc_internal_begin_call();
-  return for_rows(x_dtype, [&](auto type) {
+  return for_type(x_dtype, [&](auto type) {
     typedef decltype(type) T;
     if (experts <= 16) return launch_pick<T, 1>(logits, ldl, tokens, experts, picks, renormalise, ids, shares, st);
     if (experts <= 32) return launch_pick<T, 2>(logits, ldl, tokens, experts, picks, renormalise, ids, shares, st);
@@ -449,13 +502,14 @@ extern "C" int32_t xorenc_gather_tokens(const void *X, int32_t x_dtype, int64_t 
   const dim3 grid((unsigned)(((int64_t)tokens * g.per_row + 255) / 256));
   hipStream_t st = static_cast<hipStream_t>(hip_stream);
   xorenc_internal_begin_call();
-  return for_rows(x_dtype, [&](auto type) {
+  return for_rows(x_dtype, streams((int64_t)tokens * (picks + 1), cols, esz), [&](auto type, auto stream) {
     typedef decltype(type) T;
     typedef typename T::Elem E;
+    constexpr bool STREAM = decltype(stream)::value;
     if (shares)
-      hipLaunchKernelGGL((gather_kernel<T, true>), grid, dim3(256), 0, st, static_cast<const E *>(X), g, static_cast<E *>(R));
+      hipLaunchKernelGGL((gather_kernel<T, true, STREAM>), grid, dim3(256), 0, st, static_cast<const E *>(X), g, static_cast<E *>(R));
     else
-      hipLaunchKernelGGL((gather_kernel<T, false>), grid, dim3(256), 0, st, static_cast<const E *>(X), g, static_cast<E *>(R));
+      hipLaunchKernelGGL((gather_kernel<T, false, STREAM>), grid, dim3(256), 0, st, static_cast<const E *>(X), g, static_cast<E *>(R));
     return xorenc_internal_check_launch();
   });
 }
@@ -476,11 +530,11 @@ extern "C" int32_t xorenc_combine_tokens(const void *R, int32_t x_dtype, int64_t
   const dim3 grid((unsigned)(((int64_t)tokens * g.per_row + 255) / 256));
   hipStream_t st = static_cast<hipStream_t>(hip_stream);
   xorenc_internal_begin_call();
-  return for_rows(x_dtype, [&](auto type) {
+  return for_rows(x_dtype, streams((int64_t)tokens * (picks + 1 + (residual != nullptr)), cols, esz), [&](auto type, auto stream) {
     typedef decltype(type) T;
     typedef typename T::Elem E;
     auto launch = [&](auto most) {
-      hipLaunchKernelGGL((combine_kernel<T, decltype(most)::value>), grid, dim3(256), 0, st, static_cast<const E *>(R), g,
+      hipLaunchKernelGGL((combine_kernel<T, decltype(most)::value, decltype(stream)::value>), grid, dim3(256), 0, st, static_cast<const E *>(R), g,
                          static_cast<const E *>(residual), static_cast<E *>(Y));
     };
     if (picks <= 2)
@@ -508,12 +562,12 @@ extern "C" int32_t xorenc_combine_tokens_grad(const void *dY, int32_t x_dtype, i
   const RowArgs g = {places, used, shares, ldy, ldr, lddr, tokens, picks, cols, 0};
   hipStream_t st = static_cast<hipStream_t>(hip_stream);
   xorenc_internal_begin_call();
-  return for_rows(x_dtype, [&](auto type) {
+  return for_rows(x_dtype, streams((int64_t)tokens * (2 * picks + 1), cols, esz), [&](auto type, auto stream) {
     typedef decltype(type) T;
     typedef typename T::Elem E;
     auto launch = [&](auto threads, auto most) {
       constexpr int THREADS = decltype(threads)::value;
-      hipLaunchKernelGGL((combine_grad_kernel<T, THREADS, decltype(most)::value>), dim3((unsigned)tokens), dim3(THREADS), 0, st,
+      hipLaunchKernelGGL((combine_grad_kernel<T, THREADS, decltype(most)::value, decltype(stream)::value>), dim3((unsigned)tokens), dim3(THREADS), 0, st,
                          static_cast<const E *>(dY), g, static_cast<const E *>(R), static_cast<E *>(dR), dshares);
     };
     auto by_picks = [&](auto threads) {
