@@ -88,8 +88,8 @@ inline int cheapest_for_linear(int64_t M, int64_t N, int64_t blocks, bool exact)
 // The products of rows sorted by expert.  Their tiles come in all degrees of emptiness, and their weights from memory: the kernels take
 //   start + (rounds + `tail`) * (`tile` + steps * (`step` + `load` * share of the chip in use)) + `byte` * (MB of the weights of experts that have rows),
 // with rounds not rounded, and no tail up to one.  Fitted to 1057 shapes of 1 .. 8192 tokens, 1 .. 8 picks of 2 .. 128 experts of 128 .. 8192 x
-// 128 .. 8192, with experts that differ in their shares by a factor of four; taking the one that this says is the fastest costs 1.6 % (fp32 1.0 %)
-// over taking the one that was.  Some of the times it goes by (us, bf16, in the order of the list; tokens x picks x experts x outputs x inputs):
+// 128 .. 8192, and for bf16 1660 more of 15 to 500 G products, with experts that differ in their shares by a factor of four; taking the one that this
+// says is the fastest costs 1.2 %, of the large shapes 2.9 %, over taking the one that was (fp32 1.0 %).  Some of the times it goes by (us, bf16, in the order of the list; tokens x picks x experts x outputs x inputs):
 //   4096x2x8x8192x4096     346  414  485  763  630 3150 1030  367 1950 1190
 //   2048x8x64x1024x2048     80   85   88  133  108  599  186   73  300  181
 //   512x2x8x4096x4096       73   59   58   75    -    -    -   67  135  110
@@ -104,19 +104,19 @@ struct ExpertsCost {
 };
 constexpr int kExpertsKernels = 13;  // 0 .. 10 as above, of which 6, 7 and 10 would be the fastest for hardly any size
 constexpr ExpertsCost kExpertsCosts[2][kExpertsKernels] = {
-    {{256, 256, 256, 1, 3.69f, 4.02f, 1.46f, 1.11f, 0.000f, 0.90f},
-     {128, 128, 512, 1, 0.96f, 4.73f, 1.21f, 0.42f, 0.043f, 0.63f},
-     {128, 64, 768, 1, 2.51f, 1.88f, 0.95f, 0.47f, 0.040f, 0.39f},
-     {64, 64, 512, 2, 2.52f, 5.94f, 0.58f, 0.59f, 0.048f, 0.53f},
-     {64, 64, 1024, 1, 0.73f, 2.60f, 0.62f, 0.78f, 0.111f, 0.44f},
-     {16, 16, 512, 8, 1.20f, 3.10f, 0.14f, 0.91f, 0.029f, 0.53f},
+    {{256, 256, 256, 1, 9.24f, 4.48f, 1.32f, 0.45f, 0.001f, 0.68f},
+     {128, 128, 512, 1, 0.39f, 6.14f, 1.05f, 0.28f, 0.028f, 0.32f},
+     {128, 64, 768, 1, 2.72f, 1.84f, 0.78f, 0.54f, 0.043f, 0.65f},
+     {64, 64, 512, 2, 1.33f, 6.49f, 0.57f, 0.52f, 0.067f, 1.35f},
+     {64, 64, 1024, 1, 0.34f, 1.94f, 0.84f, 0.77f, 0.203f, 0.89f},
+     {16, 16, 512, 8, 1.05f, 3.26f, 0.06f, 1.12f, 0.013f, 0.86f},
      {},
      {},
-     {64, 64, 256, 2, 1.39f, 4.00f, 0.57f, 0.17f, 0.043f, 0.76f},
-     {256, 192, 256, 1, 1.58f, 5.01f, 1.54f, 0.31f, 0.008f, 0.61f},
+     {64, 64, 256, 2, 1.56f, 3.90f, 0.55f, 0.07f, 0.079f, 1.21f},
+     {256, 192, 256, 1, 0.63f, 6.54f, 1.48f, 0.12f, 0.010f, 1.15f},
      {},
-     {32, 16, 768, 4, 1.40f, 1.66f, 0.54f, 0.66f, 0.052f, 0.67f},    // 11: rings of two stages: of 32 x 16, four waves that split the reduction
-     {64, 32, 1024, 1, 1.01f, 2.53f, 0.58f, 0.51f, 0.046f, 0.68f}},  // 12: of three: of 64 x 32, one group of two waves
+     {32, 16, 768, 4, 0.56f, 2.04f, 0.67f, 0.50f, 0.058f, 0.80f},    // 11: rings of two stages: of 32 x 16, four waves that split the reduction
+     {64, 32, 1024, 1, 0.94f, 2.26f, 0.74f, 0.29f, 0.039f, 1.72f}},  // 12: of three: of 64 x 32, one group of two waves
     {{},
      {128, 128, 512, 1, 4.84f, 5.73f, 1.52f, 0.55f, 0.000f, 0.47f},
      {128, 64, 768, 1, 2.45f, 2.74f, 1.26f, 0.67f, 0.027f, 0.20f},
