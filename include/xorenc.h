@@ -448,8 +448,8 @@ XORENC_API int32_t xorenc_moe_fp8(const xorenc_moe *layer, const void *X, int32_
  *           need this number only take its address, `used` = offsets + experts.
  *   shares  DEV float[tokens][picks], contiguous
  * tokens = 0 succeeds; xorenc_sort_tokens alone writes something then, its offsets.  XORENC_ELIMIT beyond XORENC_MOE_MAX_EXPERTS
- * experts, XORENC_MOE_MAX_PICKS picks, 2^24 - 1 pairs, 2^20 columns, and where tokens times eighths of columns exceed 2^31 - 1.  Places and tokens outside
- * their ranges are taken for pairs without an expert.
+ * experts, XORENC_MOE_MAX_PICKS picks, 2^24 - 1 pairs, 2^20 columns, and where tokens times eighths of columns exceed 2^31 - 1.  Places outside
+ * their range are taken for pairs without an expert, rows outside theirs for the last row of A.
  */
 enum { XORENC_I32 = 0, XORENC_I64 = 1 };
 

@@ -22,8 +22,8 @@ __device__ inline uint32_t order_of(float v) {
 __device__ inline float value_of(uint32_t order) { return __uint_as_float(order & 0x80000000u ? order ^ 0x80000000u : ~order); }
 
 // Sixteen lanes hold a token's logits, V each, and take the largest that is left once per pick: its order first, then the least index of
-// those that have it.  Logits of 16 bits leave room for both in one integer, and for one maximum (16384 tokens, 8 of 128 experts: ORDER16
-// us, as those of 32 bits ORDER32).  Lane p ends up with the p-th pick.
+// those that have it.  Logits of 16 bits leave room for both in one integer, and for one maximum (65536 tokens, 8 of 128 experts: 14.1
+// us, in 32 bits 16.9).  Lane p ends up with the p-th pick.
 template <class T, int V>
 __global__ __launch_bounds__(256) void pick_kernel(const typename T::Elem *__restrict__ logits, int64_t ldl, int tokens, int experts, int picks,
                                                    int renormalise, int *__restrict__ ids, float *__restrict__ shares) {
@@ -104,9 +104,12 @@ __global__ __launch_bounds__(256) void pick_kernel(const typename T::Elem *__res
 
 // ---------------------------------------------------------------------------------------------- sort
 
-// A stable counting sort.  A workgroup places kSegment pairs: what comes before them, and where each expert's rows begin, it
-// counts itself where there are few pairs (one launch); otherwise a launch before has counted every segment.
-constexpr int kSortWaves = 8, kSortRounds = 4, kSegment = kSortWaves * kSortRounds * 64;
+// A stable counting sort.  A workgroup places a segment of pairs, ROUNDS of 64 a wave: what comes before them, and where each expert's rows begin, it
+// counts itself where there are few pairs (one launch); otherwise a launch before has counted every segment.  Long segments where there are many: what a
+// workgroup adds up is theirs all (us, in segments of 2048 and of 8192: 2^18 pairs of 128 experts 13.5 and 19.0, 2^20 35 and 25, 8 M of 64 504 and 100; 2^14 of
+// 64 in one launch 9.1, 2^15 in two 9.2).
+constexpr int kSortWaves = 8, kFewRounds = 4, kManyRounds = 16, kManyPairs = 1 << 19;
+constexpr int segment_of(int rounds) { return kSortWaves * rounds * 64; }
 constexpr int kBuckets = kMostExperts + 1;  // the last: pairs without an expert
 constexpr int kFewPairs = 16384;
 
@@ -115,38 +118,38 @@ __device__ inline int bucket_of(Id id, int experts) {
   return id >= 0 && id < experts ? (int)id : experts;
 }
 
-template <class Id>
+template <class Id, int ROUNDS>
 __global__ __launch_bounds__(kSortWaves * 64) void count_kernel(const Id *__restrict__ ids, int pairs, int experts, int *__restrict__ counts) {
   __shared__ int count[kBuckets];
   for (int e = threadIdx.x; e <= experts; e += kSortWaves * 64) count[e] = 0;
   __syncthreads();
 #pragma unroll
-  for (int i = 0; i < kSortRounds; ++i) {
-    const int pair = blockIdx.x * kSegment + i * (kSortWaves * 64) + threadIdx.x;
+  for (int i = 0; i < ROUNDS; ++i) {
+    const int pair = blockIdx.x * segment_of(ROUNDS) + i * (kSortWaves * 64) + threadIdx.x;
     if (pair < pairs) atomicAdd(&count[bucket_of(ids[pair], experts)], 1);
   }
   __syncthreads();
   for (int e = threadIdx.x; e <= experts; e += kSortWaves * 64) counts[blockIdx.x * (experts + 1) + e] = count[e];
 }
 
-template <class Id>
+template <class Id, int ROUNDS>
 __global__ __launch_bounds__(kSortWaves * 64) void sort_kernel(const Id *__restrict__ ids, int pairs, int picks, int experts,
                                                                const int *__restrict__ counts, int segments, int *__restrict__ places,
                                                                int *__restrict__ rows, int *__restrict__ offsets) {
   __shared__ int before[kBuckets], behind[kBuckets], first[kBuckets];  // pairs of segments before this one, and of it and those behind
   __shared__ int of_wave[kSortWaves][kBuckets];
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, threads = kSortWaves * 64;
-  const int start = blockIdx.x * kSegment;
+  const int start = blockIdx.x * segment_of(ROUNDS);
   for (int e = tid; e <= experts; e += threads) {
     before[e] = behind[e] = 0;
 #pragma unroll
     for (int w = 0; w < kSortWaves; ++w) of_wave[w][e] = 0;
   }
   // this wave's pairs, in order
-  int bucket[kSortRounds], rank[kSortRounds];
+  int bucket[ROUNDS], rank[ROUNDS];
 #pragma unroll
-  for (int i = 0; i < kSortRounds; ++i) {
-    const int pair = start + (wave * kSortRounds + i) * 64 + lane;
+  for (int i = 0; i < ROUNDS; ++i) {
+    const int pair = start + (wave * ROUNDS + i) * 64 + lane;
     bucket[i] = pair < pairs ? bucket_of(ids[pair], experts) : -1;
   }
   __syncthreads();
@@ -175,7 +178,7 @@ __global__ __launch_bounds__(kSortWaves * 64) void sort_kernel(const Id *__restr
   }
   // ranks within the wave's pairs: of the same bucket, those on lower lanes and of earlier rounds
 #pragma unroll
-  for (int i = 0; i < kSortRounds; ++i) {
+  for (int i = 0; i < ROUNDS; ++i) {
     const int b = bucket[i];
     uint64_t same = __ballot(b >= 0);
 #pragma unroll
@@ -224,9 +227,9 @@ __global__ __launch_bounds__(kSortWaves * 64) void sort_kernel(const Id *__restr
   }
   __syncthreads();
 #pragma unroll
-  for (int i = 0; i < kSortRounds; ++i) {
+  for (int i = 0; i < ROUNDS; ++i) {
     if (bucket[i] < 0) continue;
-    const int pair = start + (wave * kSortRounds + i) * 64 + lane;
+    const int pair = start + (wave * ROUNDS + i) * 64 + lane;
     const int place = first[bucket[i]] + before[bucket[i]] + of_wave[wave][bucket[i]] + rank[i];
     places[pair] = place;
     if (rows) rows[place] = pair / picks;
@@ -269,7 +272,7 @@ __global__ __launch_bounds__(256) void gather_kernel(const typename T::Elem *__r
   const uint32_t piece = blockIdx.x * 256u + threadIdx.x;
   const int t = (int)(piece / (uint32_t)g.per_row), c = (int)(piece % (uint32_t)g.per_row) * 8;
   if (t >= g.tokens) return;
-  const int used = min(*g.used, g.tokens * g.picks);
+  const int used = max(min(*g.used, g.tokens * g.picks), 0);
   float x[8];
   piece_of<T>(load_piece<T, STREAM>(X + t * g.ldx, c, g.cols), c, g.cols, x);
   for (int p = 0; p < g.picks; ++p) {
@@ -297,7 +300,7 @@ __global__ __launch_bounds__(256) void combine_kernel(const typename T::Elem *__
   const uint32_t piece = blockIdx.x * 256u + threadIdx.x;
   const int t = (int)(piece / (uint32_t)g.per_row), c = (int)(piece % (uint32_t)g.per_row) * 8;
   if (t >= g.tokens) return;
-  const int used = min(*g.used, g.tokens * g.picks);
+  const int used = max(min(*g.used, g.tokens * g.picks), 0);
   typename T::Raw rest;
   if (residual) rest = load_piece<T, STREAM>(residual + t * g.ldx, c, g.cols);
   float y[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
@@ -339,7 +342,7 @@ __global__ __launch_bounds__(THREADS) void combine_grad_kernel(const typename T:
   constexpr int WAVES = THREADS / 64;
   __shared__ float sums[WAVES][MOST];
   const int t = blockIdx.x, tid = threadIdx.x, pairs = g.tokens * g.picks;
-  const int used = min(*g.used, pairs);
+  const int used = max(min(*g.used, pairs), 0);
   int place[MOST];
   float share[MOST], dot[MOST];
 #pragma unroll
@@ -422,17 +425,20 @@ int32_t launch_pick(const void *logits, int64_t ldl, int tokens, int experts, in
   return xorenc_internal_check_launch();
 }
 
+int rounds_of(int64_t pairs) { return pairs < kManyPairs ? kFewRounds : kManyRounds; }
+
 int64_t sort_workspace(int64_t pairs, int32_t experts) {
-  return pairs <= kFewPairs ? 0 : (pairs + kSegment - 1) / kSegment * (experts + 1) * 4;
+  const int segment = segment_of(rounds_of(pairs));
+  return pairs <= kFewPairs ? 0 : (pairs + segment - 1) / segment * (experts + 1) * 4;
 }
 
-template <class Id>
+template <class Id, int ROUNDS>
 int32_t launch_sort(const void *ids, int pairs, int picks, int experts, int32_t *places, int32_t *rows, int32_t *offsets, int *counts, hipStream_t st) {
-  const int segments = pairs ? (pairs + kSegment - 1) / kSegment : 1;
+  const int segments = pairs ? (pairs + segment_of(ROUNDS) - 1) / segment_of(ROUNDS) : 1;
   const Id *const id = static_cast<const Id *>(ids);
-  if (counts) hipLaunchKernelGGL((count_kernel<Id>), dim3((unsigned)segments), dim3(kSortWaves * 64), 0, st, id, pairs, experts, counts);
-  hipLaunchKernelGGL((sort_kernel<Id>), dim3((unsigned)segments), dim3(kSortWaves * 64), 0, st, id, pairs, picks, experts, counts, segments, places, rows,
-                     offsets);
+  if (counts) hipLaunchKernelGGL((count_kernel<Id, ROUNDS>), dim3((unsigned)segments), dim3(kSortWaves * 64), 0, st, id, pairs, experts, counts);
+  hipLaunchKernelGGL((sort_kernel<Id, ROUNDS>), dim3((unsigned)segments), dim3(kSortWaves * 64), 0, st, id, pairs, picks, experts, counts, segments, places,
+                     rows, offsets);
   return xorenc_internal_check_launch();
 }
 
@@ -485,8 +491,13 @@ extern "C" int32_t xorenc_sort_tokens(const void *ids, int32_t id_type, int32_t 
   int *const counts = need ? static_cast<int *>(workspace) : nullptr;
   hipStream_t st = static_cast<hipStream_t>(hip_stream);
   xorenc_internal_begin_call();
-  return id_type == XORENC_I64 ? launch_sort<int64_t>(ids, tokens * picks, picks, experts, places, rows, offsets, counts, st)
-                               : launch_sort<int32_t>(ids, tokens * picks, picks, experts, places, rows, offsets, counts, st);
+  auto launch = [&](auto id, auto rounds) {
+    return launch_sort<decltype(id), decltype(rounds)::value>(ids, tokens * picks, picks, experts, places, rows, offsets, counts, st);
+  };
+  typedef std::integral_constant<int, kFewRounds> Few;
+  typedef std::integral_constant<int, kManyRounds> Many;
+  if (rounds_of((int64_t)tokens * picks) == kFewRounds) return id_type == XORENC_I64 ? launch(int64_t(), Few()) : launch(int32_t(), Few());
+  return id_type == XORENC_I64 ? launch(int64_t(), Many()) : launch(int32_t(), Many());
 }
 
 extern "C" int32_t xorenc_gather_tokens(const void *X, int32_t x_dtype, int64_t ldx, const int32_t *places, const int32_t *used,

@@ -124,7 +124,18 @@ def test_sort(T, P, E):
     check_sort(draw_ids(gen(T + P + E), T, P, E, 0.1), E)
 
 
-@pytest.mark.parametrize("T,P,E", [(300, 2, 8), (12000, 2, 8)])
+@pytest.mark.parametrize("T,P,E", [(32768, 8, 128), (87381, 3, 256), (200000, 5, 9), (600000, 2, 200), (262145, 2, 64)])
+def test_sort_of_many_pairs(T, P, E):
+    # (as test_sort; Python's lists would take seconds)
+    ids = torch.randint(-1, E + 1, (T, P), generator=gen(T), dtype=torch.int32)
+    places, tokens, offsets = xe.sort_tokens(ids.to(DEV), E)
+    key = torch.where(ids < 0, E, ids).reshape(-1).long()
+    order = torch.sort(key, stable=True).indices
+    assert torch.equal(tokens.cpu().long(), order // P) and torch.equal(places.cpu().reshape(-1)[order].long(), torch.arange(T * P))
+    assert offsets.tolist() == [0] + torch.bincount(key, minlength=E + 1)[:E].cumsum(0).tolist()
+
+
+@pytest.mark.parametrize("T,P,E", [(300, 2, 8), (12000, 2, 8), (140000, 2, 8), (270000, 2, 8)])
 @pytest.mark.parametrize("what", ["all to one", "none", "one only", "descending", "the same twice"])
 def test_sort_of_uneven_shares(T, P, E, what):
     ids = torch.full((T, P), {"all to one": 5, "none": -1, "one only": -1, "descending": 0, "the same twice": 3}[what], dtype=torch.int32)
@@ -311,6 +322,9 @@ def test_places_out_of_range_are_pairs_without_an_expert():
     marked = torch.full_like(rows, 5.0)
     xe.gather_tokens(rows[:T], bad, offsets, R=marked)
     assert (marked[places[2, 1]] == 5).all() and (marked[places[4, 0]] == 5).all()
+    none = offsets.clone()
+    none[-1] = -3                               # as if no pair had an expert
+    assert (xe.combine_tokens(rows, places, none, shares) == 0).all()
     dR, ds = xe.combine_tokens_grad(rows[:T], rows, bad, offsets, shares, dR=marked)
     assert (marked[places[2, 1]] == 5).all() and ds[2, 1] == 0 and ds[4, 0] == 0
 
