@@ -6,7 +6,8 @@
                                     many: matmul_fp8 on the copy that decode and quant_fp8 have made of it
     d = (silu(gate) * up) W2^T      silu_mul_fp8, matmul_fp8
     s = t + d                       add_rmsnorm_fp8
-    y = s + experts(norm(s))        moe_fp8, 64 tokens a call
+    y = s + experts(norm(s))        few tokens: moe_fp8, 64 a call
+                                    many: pick_experts, sort_tokens, experts_fp8 (W13), silu_mul_fp8, experts_fp8 (W2), combine_tokens
 
     python examples/feed_forward.py [--config large_q1] [--tokens 1,8,64,1024] [--experts 8] [--picks 2]
 
@@ -28,6 +29,12 @@ from synth_inputs import CONFIGS, make_workload
 # Tokens up to which the encrypted matrix itself is multiplied: it has a seventh of the decoded copy's bytes, and takes as long for
 # 64 tokens and longer for more (16384 x 4096, one plane: 15.7 us and the copy 14.4 at 64 tokens, 39 and 31 at 256).
 MOST_ENCRYPTED = 64
+
+
+# Tokens up to which the experts run in calls of 64 tokens, which round no activation to 8 bits: each call reads the weights of nearly all experts, and
+# takes as long as the sorted tokens' two products do for many more (8 experts of 4096 x 2048, two a token, us: 64 tokens 79 and 77, of which the router 31 in
+# fp32; 128 158 and 78; 1024 1258 and 136).  What the calls of 64 are for is their precision.
+MOST_UNROUNDED = 128
 
 
 def encrypt(workload):
@@ -81,9 +88,16 @@ class ExpertLayer:
             xe.moe_fp8(n[part], self.router, *self.W13, *self.W2, self.picks, Y=out[part])
         return out
 
+    def sorted_experts(self, n, Q, S):
+        """The same for many tokens, whose norms in 8 bits (Q, S) the products take; the router takes them in n's 16 bits."""
+        ids, shares = xe.pick_experts(n.float() @ self.router.float().t(), self.picks)
+        places, tokens, offsets = xe.sort_tokens(ids, self.router.shape[0])
+        u = xe.experts_fp8(Q, S, *self.W13, offsets, tokens)
+        return xe.combine_tokens(xe.experts_fp8(*xe.silu_mul_fp8(u), *self.W2, offsets), places, offsets, shares)
+
     def __call__(self, x, r):
-        _, _, t, n = xe.add_rmsnorm_fp8(x, self.norm, r, normed=True)
-        return t, self.experts(n)
+        Q, S, t, n = xe.add_rmsnorm_fp8(x, self.norm, r, normed=True)
+        return t, self.experts(n) if n.shape[0] <= MOST_UNROUNDED else self.sorted_experts(n, Q, S)
 
 
 def build(workload, experts, picks, inner, seed=0):
