@@ -2,7 +2,16 @@
 
 An 8-bit matrix is a pair of tensors: the values (torch.float8_e4m3fn, rows on 16-byte boundaries) and the scales (float32,
 one for each 1 x 128 block of activations or 128 x 128 block of weights).  All tensors are on the current device, the
-work goes to its current stream, and nothing waits.  The marshalling is in csrc/xorenc_torch_fp8.cpp.
+work goes to its current stream, and nothing waits.  No call records anything for torch's gradients.  The marshalling is in
+csrc/xorenc_torch_fp8.cpp and csrc/xorenc_torch_experts.h.
+
+Experts for any number of tokens, as a layer runs them:
+
+    ids, shares = pick_experts(logits, picks)
+    places, tokens, offsets = sort_tokens(ids, experts)
+    u = experts_fp8(Q, S, *W13, offsets, tokens)
+    d = experts_fp8(*silu_mul_fp8(u), *W2, offsets)
+    y = combine_tokens(d, places, offsets, shares, residual)
 """
 import os
 import struct
