@@ -17,16 +17,19 @@ int64_t most_row_tiles(const Job &job, const MatmulArgs &g, int bm) {
   }
 }
 
-template <int TN, int TM, int WN, int WM, bool EXACT, class Job>
+// STREAMS: it may be that experts' weights are read past the caches.
+template <int TN, int TM, int WN, int WM, bool EXACT, bool STREAMS = false, bool STREAM = false, class Job>
 void launch_tile(const MatmulArgs &g, const Job &job, hipStream_t st) {
   typedef TileShape<TN, TM, WN, WM, EXACT> Shape;
+  if constexpr (STREAMS && !STREAM) {
+    if (streams_weights(job.y_rows, job.experts, g.ldw * g.N, Shape::BM)) return launch_tile<TN, TM, WN, WM, EXACT, STREAMS, true>(g, job, st);
+  }
   const int n_tiles = (g.N + Shape::BN - 1) / Shape::BN, m_tiles = (int)most_row_tiles(job, g, Shape::BM);
   const int per_xcd = (n_tiles * m_tiles + 7) / 8;
-  hipLaunchKernelGGL((matmul_tile_kernel<TN, TM, WN, WM, EXACT, Job>), dim3((unsigned)(per_xcd * 8)), dim3(Shape::WAVES * 64), Shape::LDS, st, g,
+  hipLaunchKernelGGL((matmul_tile_kernel<TN, TM, WN, WM, EXACT, Job, STREAM>), dim3((unsigned)(per_xcd * 8)), dim3(Shape::WAVES * 64), Shape::LDS, st, g,
                      n_tiles, m_tiles, per_xcd, job);
 }
 
-// STREAMS: it may be that experts' weights are read past the caches.
 template <int TN, int TM, int WN, int WM, int KG, int NS, bool EXACT, bool STREAMS = false, bool STREAM = false, class Job>
 void launch_ring(const MatmulArgs &g, const Job &job, hipStream_t st) {
   typedef RingShape<TN, TM, WN, WM, KG, NS> Shape;
@@ -46,7 +49,7 @@ int32_t dispatch_matmul(int kernel, const MatmulArgs &g, const Job &job, hipStre
       if constexpr (!EXACT) launch_tile<8, 4, 2, 4, EXACT>(g, job, st);
       break;
     case 1: launch_tile<4, 4, 2, 2, EXACT>(g, job, st); break;
-    case 2: launch_tile<4, 2, 2, 2, EXACT>(g, job, st); break;
+    case 2: launch_tile<4, 2, 2, 2, EXACT, Job::ROWS>(g, job, st); break;
     case 3: launch_ring<2, 2, 2, 2, 2, 2, EXACT, Job::ROWS>(g, job, st); break;
     case 4: launch_ring<2, 2, 2, 2, 1, 2, EXACT>(g, job, st); break;
     case 5: launch_ring<1, 1, 1, 1, 8, 2, EXACT>(g, job, st); break;

@@ -139,8 +139,8 @@ inline int64_t most_tiles_of_experts(int64_t rows, int64_t experts, int bm) {
 }
 
 // Experts' weights of 96 MB and more, which a last cache of 256 MB would not keep until the next call, are read past the caches where one tile of bm rows
-// takes an expert's (us: 64 tokens, two of eight experts of 4096 x 4096 36.5 and 33.4, 128 tokens 37.1 and 34.1, 30 tokens of 9216 x 4096 71 and 57; 512
-// tokens, two tiles, 74.8 and 77.3).
+// takes an expert's (us: 64 tokens, two of eight experts of 4096 x 4096 36.5 and 33.4, 128 tokens 37.1 and 34.1, 30 tokens of 9216 x 4096 71 and 57; 256
+// tokens, eight of 64 of 1024 x 2048, 34.2 and 32.6; 512 of the first, two tiles an expert, 74.8 and 77.3).
 inline bool streams_weights(int64_t rows, int64_t experts, int64_t bytes_of_one, int bm) {
   return bytes_of_one >= ((int64_t)96 << 20) / (rows < experts ? rows : experts) && rows <= experts * bm;
 }

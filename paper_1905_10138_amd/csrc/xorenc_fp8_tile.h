@@ -75,7 +75,7 @@ struct TileShape {
   static_assert(BM % 64 == 0 && TN >= 2 && TN % 2 == 0 && 128 % (16 * TN) == 0, "scales");
 };
 
-template <int TN, int TM, int WN, int WM, bool EXACT, class Job>
+template <int TN, int TM, int WN, int WM, bool EXACT, class Job, bool STREAM>
 __global__ __launch_bounds__(WN *WM * 64, 2) void matmul_tile_kernel(MatmulArgs g, int n_tiles, int m_tiles, int per_xcd, Job job) {
   typedef TileShape<TN, TM, WN, WM, EXACT> Shape;
   constexpr int BN = Shape::BN, BM = Shape::BM, STAGE = Shape::STAGE, N1 = Shape::GROUP1, N2 = Shape::GROUP2;
@@ -142,9 +142,13 @@ __global__ __launch_bounds__(WN *WM * 64, 2) void matmul_tile_kernel(MatmulArgs 
   const uint32_t s_step = (uint32_t)(g.sa_blk * 4);
   const int tail = g.K & (kBlock - 1);
   auto fetch1 = [&](int b, int i) {
-    fetch_16(lds0 + (b & 1) * STAGE + (of_a(i) ? BN * 128 : 0) + row1(i) * 128, at1[i], of_a(i) ? a_desc : w_desc, (uint32_t)b * kBlock);
+    const uint32_t to = lds0 + (b & 1) * STAGE + (of_a(i) ? BN * 128 : 0) + row1(i) * 128;
+    if (STREAM && !of_a(i))
+      fetch_16<true>(to, at1[i], w_desc, (uint32_t)b * kBlock);
+    else
+      fetch_16(to, at1[i], of_a(i) ? a_desc : w_desc, (uint32_t)b * kBlock);
   };
-  auto fetch2 = [&](int b, int i) { fetch_16(lds0 + (b & 1) * STAGE + row2(i) * 128, at2[i], w_desc, (uint32_t)b * kBlock); };
+  auto fetch2 = [&](int b, int i) { fetch_16<STREAM>(lds0 + (b & 1) * STAGE + row2(i) * 128, at2[i], w_desc, (uint32_t)b * kBlock); };
   auto fetch_scales = [&](int b) { fetch_4(lds0 + 2 * STAGE + (b & 1) * (BM * 4) + s_rows * 4, s_at, s_desc, (uint32_t)b * s_step); };
   // before the last block is fetched: chunks behind column K read as zero
   auto end1 = [&](int b) {

@@ -16,7 +16,7 @@ int main() {
   for (int exact = 0; exact < 2; ++exact) {
     // taken: up to 64 blocks, and beyond; each with weights through the caches, and past them (what some kernels never do)
     bool taken[kExpertsKernels][2][2] = {}, steady[kExpertsKernels][2] = {}, second_run[kExpertsKernels][2] = {};
-    auto past = [&](int k, int64_t R, int64_t E, int64_t bytes) { return (k == 3 || k >= 11) && streams_weights(R, E, bytes, kExpertsCosts[exact][k].bm); };
+    auto past = [&](int k, int64_t R, int64_t E, int64_t bytes) { return (k == 2 || k == 3 || k >= 11) && streams_weights(R, E, bytes, kExpertsCosts[exact][k].bm); };
     for (const Size &s : sizes) {
       const int64_t blocks = (s.K + 127) / 128;
       const int k = cheapest_for_experts(s.T * s.P, s.E, s.N, blocks, exact);
