@@ -184,11 +184,14 @@ struct EpilogueTile {
 
 // ---------------------------------------------------------------------------------------------- rows of experts
 
-// Which of all experts' tiles of BM rows (times n_tiles) is this workgroup's: the expert's rows and matrix in g, and its tile.  Tiles of one expert follow each
-// other, and each XCD (workgroup i runs on XCD i % 8) takes a run of them, so that they share W in its L2.  Every wave finds out
-// by itself: a lane has up to four neighbouring experts, and a scan over the lanes says how many tiles come before.
-template <int BM, class Elem>
-__device__ __forceinline__ bool take_tile(const Experts &job, MatmulArgs &g, Epilogue &epilogue, int n_tiles, int lane, int &local, int &m_tiles, int &first_row) {
+// Which of all experts' tiles of BM rows (times n_tiles) is this workgroup's: the expert's rows and matrix in g, and its tile.  Each XCD (workgroup i runs on XCD
+// i % 8) takes a run of tiles.  Where rows are few (COLUMNS 0) an expert's tiles follow each other, and those that share rows of W first.  Large tiles
+// come by groups of COLUMNS column tiles of all experts, so that every XCD has rows of all of them, heavy ones and light ones, and finishes with the
+// others (4096 tokens, two of eight experts of 8192 x 4096 346 -> 332 us, 8192, four of 32 of 2048 x 2048 198 -> 191; 512 columns, with 1024 329 and 191, and
+// 4096 tokens, two of eight of 4096 x 9216 411 and 430).  Every wave finds out by itself: a lane has up to four neighbouring experts, and a scan over the
+// lanes says how many tiles come before.
+template <int BM, int COLUMNS, class Elem>
+__device__ __forceinline__ bool take_tile(const Experts &job, MatmulArgs &g, Epilogue &epilogue, int n_tiles, int lane, int &tile_m, int &tile_n, int &first_row) {
   constexpr int PER = (XORENC_MOE_MAX_EXPERTS + 63) / 64;
   const int per = (job.experts + 63) / 64;
   int first[PER], rows[PER], sum = 0;
@@ -208,10 +211,11 @@ __device__ __forceinline__ bool take_tile(const Experts &job, MatmulArgs &g, Epi
     const int other = __shfl_up(upto, d);
     if (lane >= d) upto += other;
   }
-  const int total = __builtin_amdgcn_readlane(upto, 63) * n_tiles, per_xcd = (total + 7) / 8;
+  const int units = __builtin_amdgcn_readlane(upto, 63), total = units * n_tiles, per_xcd = (total + 7) / 8;
   const int in_run = blockIdx.x >> 3, tile = (blockIdx.x & 7) * per_xcd + in_run;
   if (in_run >= per_xcd || tile >= total) return false;
-  const int unit = tile / n_tiles;
+  const int columns = COLUMNS ? COLUMNS : n_tiles, group = tile / (columns * units), in_group = tile - group * (columns * units);
+  const int wide = min(columns, n_tiles - group * columns), unit = in_group / wide;
   const int owner = __ffsll((unsigned long long)__ballot(upto > unit)) - 1;
   int before = upto - sum, e = lane * per, r = rows[0], f = first[0];
 #pragma unroll
@@ -223,8 +227,14 @@ __device__ __forceinline__ bool take_tile(const Experts &job, MatmulArgs &g, Epi
   e = __builtin_amdgcn_readlane(e, owner);
   g.M = __builtin_amdgcn_readlane(r, owner);
   first_row = __builtin_amdgcn_readlane(f, owner);
-  local = tile - before * n_tiles;
-  m_tiles = (g.M + BM - 1) / BM;
+  const int local = in_group - before * wide, m_tiles = (g.M + BM - 1) / BM;
+  if constexpr (COLUMNS) {
+    tile_m = local / wide;
+    tile_n = group * columns + local - tile_m * wide;
+  } else {
+    tile_n = local / m_tiles;
+    tile_m = local - tile_n * m_tiles;
+  }
   g.W += e * job.w_stride;
   g.SW += e * job.sw_stride;
   g.Y = static_cast<Elem *>(g.Y) + first_row * g.ldy;

@@ -31,15 +31,16 @@ __global__ __launch_bounds__(WN *WM *KG * 64) void matmul_ring_kernel(MatmulArgs
   typedef RingShape<TN, TM, WN, WM, KG, NS> Shape;
   constexpr int BN = Shape::BN, BM = Shape::BM, PER = Shape::PER, BLOCK = Shape::BLOCK, STAGE = Shape::STAGE;
   extern __shared__ __attribute__((aligned(1024))) uint8_t ring_lds[];
-  int tile = (blockIdx.x & 7) * per_xcd + (blockIdx.x >> 3), first_row = 0;  // XCDs take runs of tiles that share rows of W
+  int first_row = 0, tile_m, tile_n;
   Epilogue epilogue = epilogue_of(job);
   if constexpr (Job::ROWS) {
-    if (!take_tile<BM, typename std::conditional<EXACT, float, uint16_t>::type>(job, g, epilogue, n_tiles, threadIdx.x & 63, tile, m_tiles, first_row))
-      return;
+    typedef typename std::conditional<EXACT, float, uint16_t>::type Elem;
+    if (!take_tile<BM, 0, Elem>(job, g, epilogue, n_tiles, threadIdx.x & 63, tile_m, tile_n, first_row)) return;
   } else {
+    const int tile = (blockIdx.x & 7) * per_xcd + (blockIdx.x >> 3);  // XCDs take runs of tiles that share rows of W
     if (tile >= n_tiles * m_tiles) return;
+    tile_n = tile / m_tiles, tile_m = tile - tile_n * m_tiles;
   }
-  const int tile_n = tile / m_tiles, tile_m = tile - tile_n * m_tiles;
   const int n0 = tile_n * BN, m0 = tile_m * BM;
   const int tid = threadIdx.x, lane = tid & 63, r = lane & 15;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);

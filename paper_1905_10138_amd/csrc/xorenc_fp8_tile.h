@@ -82,25 +82,24 @@ __global__ __launch_bounds__(WN *WM * 64, 2) void matmul_tile_kernel(MatmulArgs 
   extern __shared__ __attribute__((aligned(1024))) uint8_t tile_lds[];
 
   // workgroup i runs on XCD i % 8: each XCD takes a run of tiles, four row tiles of A wide, that share rows in its L2
-  int tile = (blockIdx.x & 7) * per_xcd + (blockIdx.x >> 3), first_row = 0;
+  int first_row = 0, tile_m, tile_n;
   Epilogue epilogue = epilogue_of(job);
   if constexpr (Job::ROWS) {
-    if (!take_tile<BM, typename std::conditional<EXACT, float, uint16_t>::type>(job, g, epilogue, n_tiles, threadIdx.x & 63, tile, m_tiles, first_row))
-      return;
+    typedef typename std::conditional<EXACT, float, uint16_t>::type Elem;
+    if (!take_tile<BM, 512 / BN, Elem>(job, g, epilogue, n_tiles, threadIdx.x & 63, tile_m, tile_n, first_row)) return;
   } else {
+    const int tile = (blockIdx.x & 7) * per_xcd + (blockIdx.x >> 3);
     if (tile >= n_tiles * m_tiles) return;
+    constexpr int GROUP = 4;
+    const int strip = tile / (GROUP * n_tiles), in_strip = tile - strip * (GROUP * n_tiles);
+    const int strip_m = min(GROUP, m_tiles - strip * GROUP);
+    // ... and each strip begins where an XCD's 32 CUs end that began with the strip before: rows of W that come from memory, not from
+    // the cache behind the L2s, are then waited for by one XCD, and in the first round (8192 x 16384 x 4096, three sets of operands in turn
+    // 553 -> 527 us, 4096 x 9216 x 8192 368 -> 344; one set, which that cache holds, 514 and 521)
+    const int at_n = in_strip / strip_m;
+    tile_m = strip * GROUP + in_strip - at_n * strip_m;
+    tile_n = (at_n + strip * (32 / GROUP)) % n_tiles;
   }
-  constexpr int GROUP = 4;
-  int group = GROUP;
-  // (an expert's strips are as high as each other, up to six row tiles: a last one alone would read W again for a few rows)
-  if constexpr (Job::ROWS) group = m_tiles <= 6 ? m_tiles : (m_tiles + (m_tiles + 3) / 4 - 1) / ((m_tiles + 3) / 4);
-  const int strip = tile / (group * n_tiles), in_strip = tile - strip * (group * n_tiles);
-  const int strip_m = min(group, m_tiles - strip * group);
-  // ... and each strip begins where an XCD's 32 CUs end that began with the strip before: rows of W that come from memory, not from
-  // the cache behind the L2s, are then waited for by one XCD, and in the first round (8192 x 16384 x 4096, three sets of operands in turn
-  // 553 -> 527 us, 4096 x 9216 x 8192 368 -> 344; one set, which that cache holds, 514 and 521)
-  const int at_n = in_strip / strip_m, tile_m = strip * group + in_strip - at_n * strip_m;
-  const int tile_n = (at_n + strip * (32 / GROUP)) % n_tiles;
   const int n0 = tile_n * BN, m0 = tile_m * BM;
 
   const int tid = threadIdx.x, lane = tid & 63;
