@@ -56,7 +56,8 @@ __device__ inline float times_logistic(float x, float u) {
 
 // x times the normal distribution function, erfc(-x / sqrt 2) / 2.  For z >= 0, erfc(z) exp(z^2) is t Q(t) with t = 1 / (1 + p z); Q and p were fitted to the
 // function's values for 0 <= z <= 10 so that the largest relative error is least: 5.2e-6 (results of 16 bits, 0.1 % of their half step) and 2e-8.
-// Beyond, exp(-z^2) is 0.  As precise in the lower tail as anywhere; a quarter of the time of the library's erfcf.
+// Beyond, exp(-z^2) is 0.  As precise in the lower tail as anywhere (8192 x 16384 x 4096: 51 us beside a bias alone,
+// with the library's erfcf 145).
 template <bool EXACT>
 __device__ inline float gelu(float x) {
   const float e = __builtin_amdgcn_exp2f(x * (x * -0.72134752f));

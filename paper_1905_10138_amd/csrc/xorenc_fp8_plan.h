@@ -90,10 +90,10 @@ inline int cheapest_for_linear(int64_t M, int64_t N, int64_t blocks, bool exact)
 // with rounds not rounded, and no tail up to one.  Fitted to 1057 shapes of 1 .. 8192 tokens, 1 .. 8 picks of 2 .. 128 experts of 128 .. 8192 x
 // 128 .. 8192, and for bf16 1660 more of 15 to 500 G products, with experts that differ in their shares by a factor of four; taking the one that this
 // says is the fastest costs 1.2 %, of the large shapes 2.9 %, over taking the one that was (fp32 1.0 %).  Some of the times it goes by (us, bf16, in the order of the list; tokens x picks x experts x outputs x inputs):
-//   4096x2x8x8192x4096     346  414  485  763  630 3150 1030  367 1950 1190
-//   2048x8x64x1024x2048     80   85   88  133  108  599  186   73  300  181
-//   512x2x8x4096x4096       73   59   58   75    -    -    -   67  135  110
-//   256x8x64x1024x2048      41   34   34   46   44  109   58   38   57   47
+//   4096x2x8x8192x4096     332  390  458  763  630 3150 1030  359 1950 1190
+//   2048x8x64x1024x2048     80   84   86  133  108  599  186   72  300  181
+//   512x2x8x4096x4096       73   57   56   75    -    -    -   66  135  110
+//   256x8x64x1024x2048      41   33   32   46   44  109   58   37   57   47
 //   64x2x8x4096x4096        70   48   44   33   42   50   42   63   37   39
 //   64x6x64x2048x1024        -    -   35   43    -   76   65    -   36   31
 //   4x2x8x4096x4096          -    -   38   25    -   25   35    -   20   36

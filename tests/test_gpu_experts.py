@@ -255,6 +255,40 @@ def test_experts_beyond_32_bits():
         xe.experts_fp8(rows, torch.ones(1025, 2, device=DEV), W, SW, offsets, tokens, b)
 
 
+@pytest.mark.parametrize("out", TYPES)
+def test_experts_of_many_rows(out):
+    check_experts(150000, 2, 3, 65, 70, out, None, "relu", True, without=0.05)
+    check_experts(70000, 1, 256, 64, 130, out, torch.bfloat16, None, False)
+
+
+def test_one_matrix_and_one_bias_for_all_experts():
+    g = gen(11)
+    T, P, E, N, K = 90, 2, 5, 140, 260
+    A, SA, W, SW, offsets, tokens, b, Y = check_experts(T, P, E, N, K, torch.bfloat16, torch.float32, "silu", True)
+    one = xe.experts_fp8(A, SA, W[:1].expand(E, -1, -1), SW[:1].expand(E, -1, -1), offsets, tokens, b[:1].expand(E, -1), "silu")
+    rows = tokens.long()
+    ld = A.stride(0)
+    copy = torch.zeros(len(rows), ld, dtype=torch.uint8, device=DEV)
+    copy[:, :K] = A.view(torch.uint8)[rows]
+    check(one, dense_on_gpu(copy.view(A.dtype)[:, :K], SA[rows], 1), dense_on_gpu(W[0], SW[0], 128), b[0], "silu", None)
+
+
+def test_calls_on_two_streams_at_once():
+    args = [check_experts(T, 2, 8, 1000, 520, torch.bfloat16, torch.float32, "gelu", True, seed=T) for T in (300, 700)]
+    streams = [torch.cuda.Stream() for _ in args]
+    torch.cuda.synchronize()
+    got = [[], []]
+    for _ in range(10):
+        for i, (A, SA, W, SW, offsets, tokens, b, Y) in enumerate(args):
+            with torch.cuda.stream(streams[i]):
+                y = xe.experts_fp8(A, SA, W, SW, offsets, tokens, b, "gelu")
+                got[i].append((y, xe.linear_fp8(A, SA, W[1], SW[1], b[1], "gelu", y[:A.shape[0]])))
+    torch.cuda.synchronize()
+    for i, (A, SA, W, SW, offsets, tokens, b, Y) in enumerate(args):
+        want = xe.linear_fp8(A, SA, W[1], SW[1], b[1], "gelu", Y[:A.shape[0]])
+        assert all(torch.equal(y, Y) and torch.equal(z, want) for y, z in got[i])
+
+
 def test_offsets_and_tokens_out_of_range_stay_within_the_operands():
     A, SA, W, SW, offsets, tokens, b, Y = check_experts(50, 2, 4, 130, 200, torch.bfloat16, None, None, True)
     bad = tokens.clone()

@@ -349,6 +349,22 @@ def test_rows_beyond_32_bits(dtype):
     assert torch.equal(far[:T], xe.combine_tokens(rows, places, offsets, shares))
 
 
+def test_many_pairs_there_and_back():
+    g = gen(12)
+    T, P, E, H = 1 << 20, 8, 64, 9
+    ids = torch.randint(-1, E, (T, P), generator=g, dtype=torch.int32).to(DEV)
+    places, tokens, offsets = xe.sort_tokens(ids, E)
+    x = torch.randint(-8, 9, (T, H), generator=g).float().to(DEV)
+    R = xe.gather_tokens(x, places, offsets)
+    used = int(offsets[-1])
+    assert torch.equal(R[:used], x[tokens[:used].long()]) and (R[used:] == 0).all()
+    have = (places < used).sum(1, keepdim=True)
+    assert torch.equal(xe.combine_tokens(R, places, offsets), x * have)  # (sums of small whole numbers are exact)
+    shares = torch.ones(T, P, device=DEV)
+    dR, ds = xe.combine_tokens_grad(x, R, places, offsets, shares)
+    assert torch.equal(dR, R) and torch.equal(ds, torch.where(places < used, x.square().sum(1, keepdim=True), 0.0))
+
+
 def test_no_tokens():
     ids, shares = xe.pick_experts(torch.empty(0, 8, device=DEV), 2)
     assert ids.shape == shares.shape == (0, 2)
