@@ -87,9 +87,9 @@ inline int cheapest_for_linear(int64_t M, int64_t N, int64_t blocks, bool exact)
 
 // The products of rows sorted by expert.  Their tiles come in all degrees of emptiness, and their weights from memory: the kernels take
 //   start + (rounds + `tail`) * (`tile` + steps * (`step` + `load` * share of the chip in use)) + `byte` * (MB of the weights of experts that have rows),
-// with rounds not rounded, and no tail up to one.  Fitted to 1057 shapes of 1 .. 8192 tokens, 1 .. 8 picks of 2 .. 128 experts of 128 .. 8192 x
-// 128 .. 8192, and for bf16 1660 more of 15 to 500 G products, with experts that differ in their shares by a factor of four; taking the one that this
-// says is the fastest costs 1.2 %, of the large shapes 2.9 %, over taking the one that was (fp32 1.0 %).  Some of the times it goes by (us, bf16, in the order of the list; tokens x picks x experts x outputs x inputs):
+// with rounds not rounded, and no tail up to one.  Fitted to 2815 shapes of 1 .. 8192 tokens, 1 .. 8 picks of 2 .. 128 experts of 128 .. 9216 x
+// 128 .. 9216, 1200 of them of 15 to 500 G products, with experts that differ in their shares by a factor of four; taking the one that this says is the
+// fastest costs 2.1 % (fp32 0.9 %) over taking the one that was, on the quarter of them that was not fitted to.  Some of the times it goes by (us, bf16, in the order of the list; tokens x picks x experts x outputs x inputs):
 //   4096x2x8x8192x4096     332  390  458  763  630 3150 1030  359 1950 1190
 //   2048x8x64x1024x2048     80   84   86  133  108  599  186   72  300  181
 //   512x2x8x4096x4096       73   57   56   75    -    -    -   66  135  110
@@ -104,32 +104,32 @@ struct ExpertsCost {
 };
 constexpr int kExpertsKernels = 13;  // 0 .. 10 as above, of which 6, 7 and 10 would be the fastest for hardly any size
 constexpr ExpertsCost kExpertsCosts[2][kExpertsKernels] = {
-    {{256, 256, 256, 1, 9.24f, 4.48f, 1.32f, 0.45f, 0.001f, 0.68f},
-     {128, 128, 512, 1, 0.39f, 6.14f, 1.05f, 0.28f, 0.028f, 0.32f},
-     {128, 64, 768, 1, 2.72f, 1.84f, 0.78f, 0.54f, 0.043f, 0.65f},
-     {64, 64, 512, 2, 1.33f, 6.49f, 0.57f, 0.52f, 0.067f, 1.35f},
-     {64, 64, 1024, 1, 0.34f, 1.94f, 0.84f, 0.77f, 0.203f, 0.89f},
-     {16, 16, 512, 8, 1.05f, 3.26f, 0.06f, 1.12f, 0.013f, 0.86f},
+    {{256, 256, 256, 1, 18.66f, 2.12f, 1.37f, 0.18f, 0.002f, 0.90f},
+     {128, 128, 512, 1, 0.24f, 7.85f, 1.09f, 0.15f, 0.012f, 0.44f},
+     {128, 64, 768, 1, 3.57f, 0.99f, 0.84f, 0.30f, 0.070f, 1.37f},
+     {64, 64, 512, 2, 2.18f, 6.09f, 0.71f, 0.28f, 0.082f, 1.00f},
+     {64, 64, 1024, 1, 0.67f, 2.00f, 0.73f, 1.11f, 0.205f, 0.74f},
+     {16, 16, 512, 8, 0.99f, 3.48f, 0.03f, 1.45f, 0.006f, 0.35f},
      {},
      {},
-     {64, 64, 256, 2, 1.56f, 3.90f, 0.55f, 0.07f, 0.079f, 1.21f},
-     {256, 192, 256, 1, 0.63f, 6.54f, 1.48f, 0.12f, 0.010f, 1.15f},
+     {64, 64, 256, 2, 1.76f, 3.63f, 0.65f, 0.03f, 0.072f, 1.17f},
+     {256, 192, 256, 1, 1.18f, 7.77f, 1.47f, 0.05f, 0.008f, 0.74f},
      {},
-     {32, 16, 768, 4, 0.56f, 2.04f, 0.67f, 0.50f, 0.058f, 0.80f},    // 11: rings of two stages: of 32 x 16, four waves that split the reduction
-     {64, 32, 1024, 1, 0.94f, 2.26f, 0.74f, 0.29f, 0.039f, 1.72f}},  // 12: of three: of 64 x 32, one group of two waves
+     {32, 16, 768, 4, 0.23f, 2.47f, 0.73f, 0.59f, 0.037f, 0.68f},    // 11: rings of two stages: of 32 x 16, four waves that split the reduction
+     {64, 32, 1024, 1, 1.38f, 2.07f, 0.76f, 0.40f, 0.021f, 2.97f}},  // 12: of three: of 64 x 32, one group of two waves
     {{},
-     {128, 128, 512, 1, 4.84f, 5.73f, 1.52f, 0.55f, 0.000f, 0.47f},
-     {128, 64, 768, 1, 2.45f, 2.74f, 1.26f, 0.67f, 0.027f, 0.20f},
-     {64, 64, 512, 2, 1.52f, 3.66f, 0.44f, 1.58f, 0.053f, 0.43f},
-     {64, 64, 768, 1, 0.88f, 2.59f, 0.80f, 0.86f, 0.096f, 0.47f},
-     {16, 16, 512, 8, 1.15f, 3.33f, 0.19f, 0.99f, 0.030f, 0.55f},
+     {128, 128, 512, 1, 12.12f, 5.45f, 1.49f, 0.22f, 0.020f, 0.46f},
+     {128, 64, 768, 1, 3.71f, 3.09f, 1.09f, 0.79f, 0.012f, 0.25f},
+     {64, 64, 512, 2, 0.61f, 5.36f, 0.56f, 0.99f, 0.086f, 0.24f},
+     {64, 64, 768, 1, 0.35f, 2.63f, 1.06f, 0.39f, 0.186f, 1.02f},
+     {16, 16, 512, 8, 1.63f, 3.42f, 0.08f, 1.38f, 0.013f, 0.25f},
      {},
      {},
      {},
      {},
      {},
-     {32, 16, 768, 4, 1.31f, 1.95f, 0.57f, 0.70f, 0.054f, 0.63f},
-     {64, 32, 1024, 1, 1.02f, 2.79f, 0.88f, 0.47f, 0.046f, 0.60f}}};
+     {32, 16, 768, 4, 0.53f, 2.74f, 0.82f, 0.37f, 0.023f, 0.68f},
+     {64, 32, 1024, 1, 0.41f, 3.35f, 1.12f, 0.19f, 0.019f, 1.07f}}};
 
 // `rows` rows sorted by expert: at most this many tiles of bm rows, whatever the experts' shares (one row each for as many as there
 // are, the rest in whole tiles).
