@@ -84,7 +84,8 @@ __device__ inline float activated(float x) {
 // A wave's 16 TN x 16 TM results with the epilogue, from row n_first of W and m_first of A on.  Sixteen rows at a time change places in LDS in fp32 (the wave's
 // own; 16-byte chunks of row m at chunk ^ m), so that a lane has as many neighbours of a row as 16 bytes of Y hold, and always the same columns:
 // their bias is read once, the residual and Y in whole runs.
-template <int TN, int TM, bool EXACT>
+// RESIDUAL: there may be one (rows of experts have none; 17576 of them by 2746 x 71 with SiLU 57.5 -> 53.4 us, 15396 by 335 x 256 in fp32 15.6 -> 13.6).
+template <int TN, int TM, bool EXACT, bool RESIDUAL>
 struct EpilogueTile {
   typedef typename std::conditional<EXACT, F32, BF16>::type T;
   typedef typename T::Elem Out;
@@ -126,7 +127,7 @@ struct EpilogueTile {
 #pragma unroll
       for (int k = 0; k < STEPS; ++k) {
         old[j][k] = u32x4{0u, 0u, 0u, 0u};
-        if (residual && whole)  // (rows past the last: the last one again)
+        if (RESIDUAL && residual && whole)  // (rows past the last: the last one again)
           old[j][k] = *reinterpret_cast<const u32x4_anywhere *>(residual + (int64_t)min(m_first + row_of(j, k), M - 1) * epilogue.ld_residual + n);
       }
   }
@@ -154,19 +155,21 @@ struct EpilogueTile {
         if (whole) {
           if constexpr (EXACT) {
             const u32x4 r = old[j][k];
-            __builtin_nontemporal_store(f32x4{y[0] + __uint_as_float(r[0]), y[1] + __uint_as_float(r[1]), y[2] + __uint_as_float(r[2]), y[3] + __uint_as_float(r[3])},
-                                        reinterpret_cast<f32x4_anywhere *>(to));
+            f32x4 v = {y[0], y[1], y[2], y[3]};
+            if constexpr (RESIDUAL) v += f32x4{__uint_as_float(r[0]), __uint_as_float(r[1]), __uint_as_float(r[2]), __uint_as_float(r[3])};
+            __builtin_nontemporal_store(v, reinterpret_cast<f32x4_anywhere *>(to));
           } else {
             u32x4 v;
 #pragma unroll
-            for (int q = 0; q < 4; ++q) v[q] = to_bf16x2(y[2 * q] + bf16_lo(old[j][k][q]), y[2 * q + 1] + bf16_hi(old[j][k][q]));
+            for (int q = 0; q < 4; ++q)
+              v[q] = RESIDUAL ? to_bf16x2(y[2 * q] + bf16_lo(old[j][k][q]), y[2 * q + 1] + bf16_hi(old[j][k][q])) : to_bf16x2(y[2 * q], y[2 * q + 1]);
             __builtin_nontemporal_store(v, reinterpret_cast<u32x4_anywhere *>(to));
           }
         } else {
-          const Out *const from = residual ? residual + (int64_t)row * epilogue.ld_residual + n : nullptr;
+          const Out *const from = RESIDUAL && residual ? residual + (int64_t)row * epilogue.ld_residual + n : nullptr;
 #pragma unroll
           for (int e = 0; e < PER; ++e)
-            if (n + e < N) T::store(to + e, y[e] + (from ? widen(from[e]) : 0.f));
+            if (n + e < N) T::store(to + e, RESIDUAL && from ? y[e] + widen(from[e]) : y[e]);
         }
       }
     }

@@ -87,7 +87,7 @@ __global__ __launch_bounds__(WN *WM *KG * 64) void matmul_ring_kernel(MatmulArgs
   const float *const sw_row = g.SW + (int64_t)(w_row * kBlock < g.N ? w_row : 0) * g.ldsw;
   float sw_run = sw_row[min(lane, g.blocks - 1)];
 
-  EpilogueTile<TN, TM, EXACT> results(g, m0 + wm * (16 * TM), n0 + wn * (16 * TN), lane);
+  EpilogueTile<TN, TM, EXACT, !Job::ROWS> results(g, m0 + wm * (16 * TM), n0 + wn * (16 * TN), lane);
   // Before the loop, so that nothing waits for it at the end (1 x 9216 x 4096 with a bias 11.0 -> 10.3 us, onto a residual 11.7 -> 10.3), but not where the
   // registers that this takes cost a workgroup of the CU (128 rows, eight experts of 4096 x 4096 36 -> 47).
   constexpr bool EARLY = Shape::LDS > 80 * 1024 || TN * TM <= 2;

@@ -277,7 +277,7 @@ __global__ __launch_bounds__(WN *WM * 64, 2) void matmul_tile_kernel(MatmulArgs 
   __syncthreads();
   if constexpr (Job::EPILOGUE) {
     if (!Job::ROWS || !epilogue.none()) {
-      typedef EpilogueTile<TN, TM, EXACT> Results;
+      typedef EpilogueTile<TN, TM, EXACT, !Job::ROWS> Results;
       static_assert(Shape::WAVES * Results::LDS <= Shape::LDS, "sixteen rows of each wave's results fit");
       Results results(g, m0 + wm * (16 * TM), n0 + wn * (16 * TN), lane);
       results.load(epilogue);
