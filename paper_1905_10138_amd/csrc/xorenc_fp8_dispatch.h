@@ -103,7 +103,7 @@ inline MatmulArgs arguments_of(const uint8_t *A, int64_t lda, const float *SA, i
   return MatmulArgs{A, W, SA, SW, Y, lda, ldw, a_rows > 1 ? sa_row : 0, sa_blk, ldsw, ldy, M, N, K, (K + kBlock - 1) / kBlock};
 }
 
-// The epilogue of a call, whose Y has y_rows rows of N values; `stride` from one bias to the next where there are several.
+// The epilogue of a call whose Y has rows of N values of y_dtype; `residual`: whether it may have one.
 inline int32_t read_epilogue(const xorenc_epilogue *given, int32_t N, int32_t y_dtype, bool residual, Epilogue *out) {
   *out = Epilogue{nullptr, nullptr, 0, 0, XORENC_NO_ACTIVATION};
   if (!given) return XORENC_OK;

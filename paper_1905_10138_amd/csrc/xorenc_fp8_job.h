@@ -64,7 +64,8 @@ __device__ inline float gelu(float x) {
   const float t = __builtin_amdgcn_rcpf(fmaf(fabsf(x), EXACT ? 0.212132037f : 0.311126977f, 1.f));
   float q;
   if constexpr (EXACT) {
-    q = fmaf(fmaf(fmaf(fmaf(fmaf(fmaf(fmaf(fmaf(-0.0647613779f, t, 0.242781237f), t, -0.256138295f), t, 0.273859143f), t, -0.0473247766f), t, 0.107462786f), t, 0.0741696507f), t, 0.0853576064f), t, 0.0845940039f);
+    q = fmaf(fmaf(fmaf(fmaf(-0.0647613779f, t, 0.242781237f), t, -0.256138295f), t, 0.273859143f), t, -0.0473247766f);
+    q = fmaf(fmaf(fmaf(fmaf(q, t, 0.107462786f), t, 0.0741696507f), t, 0.0853576064f), t, 0.0845940039f);
   } else {
     q = fmaf(fmaf(fmaf(fmaf(fmaf(-0.0730531067f, t, 0.175327033f), t, 0.0203646906f), t, 0.131793633f), t, 0.121284649f), t, 0.12428052f);
   }

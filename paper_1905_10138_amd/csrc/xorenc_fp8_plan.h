@@ -74,8 +74,8 @@ inline int cheapest(int64_t M, int64_t N, int64_t blocks, bool exact) {
 
 // The products with an epilogue have one kernel more: rings of two stages, of 32 x 16, four waves that split the reduction (11).  Of 1363 shapes of 1 .. 64 x
 // 128 .. 16384 x 128 .. 9216 it is the fastest of 560 (fp32 530); the choice costs 1.9 % (0.6 %) over the fastest kernel's times, without it 3.4 %
-// (3.1 %).  (us, with a bias, this and the fastest of the others: 1 x 9216 x 4096 9.3 and 10.2, 1 x 16384 x 4096 12.0 and 13.4, 32 x 9216 x 4096 10.1 and 10.7, 16 x 4096 x
-// 4096 8.2 and 5.8.)
+// (3.1 %).  (us, with a bias, this and the fastest of the others: 1 x 9216 x 4096 9.1 and 10.3, 1 x 16384 x 4096 12.0 and 13.4, 32 x 9216 x 4096 10.1
+// and 10.7, 16 x 4096 x 4096 8.2 and 5.8.)
 constexpr Cost kFewRows[2] = {{32, 16, 768, 4, 3.52f, 0.33f, 0.35f, 0.75f}, {32, 16, 768, 4, 3.41f, 0.39f, 0.40f, 0.78f}};
 constexpr int kFewRowsKernel = 11;
 inline int cheapest_for_linear(int64_t M, int64_t N, int64_t blocks, bool exact) {
@@ -89,7 +89,8 @@ inline int cheapest_for_linear(int64_t M, int64_t N, int64_t blocks, bool exact)
 //   start + (rounds + `tail`) * (`tile` + steps * (`step` + `load` * share of the chip in use)) + `byte` * (MB of the weights of experts that have rows),
 // with rounds not rounded, and no tail up to one.  Fitted to 2815 shapes of 1 .. 8192 tokens, 1 .. 8 picks of 2 .. 128 experts of 128 .. 9216 x
 // 128 .. 9216, 1200 of them of 15 to 500 G products, with experts that differ in their shares by a factor of four; taking the one that this says is the
-// fastest costs 2.1 % (fp32 0.9 %) over taking the one that was, on the quarter of them that was not fitted to.  Some of the times it goes by (us, bf16, in the order of the list; tokens x picks x experts x outputs x inputs):
+// fastest costs 2.1 % (fp32 0.9 %) over taking the one that was, on the quarter of them that was not fitted to.
+// Some of the times it goes by (us, bf16, in the order of the list; tokens x picks x experts x outputs x inputs):
 //   4096x2x8x8192x4096     332  390  458  763  630 3150 1030  359 1950 1190
 //   2048x8x64x1024x2048     80   84   86  133  108  599  186   72  300  181
 //   512x2x8x4096x4096       73   57   56   75    -    -    -   66  135  110
