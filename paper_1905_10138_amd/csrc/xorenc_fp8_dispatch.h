@@ -17,12 +17,16 @@ int64_t most_row_tiles(const Job &job, const MatmulArgs &g, int bm) {
   }
 }
 
+inline bool streams_weights(const Experts &job, const MatmulArgs &g, int bm) {
+  return streams_weights(job.y_rows, job.experts, bytes_of_one_expert(job.experts, g.N, g.K, g.ldw, job.w_stride), bm);
+}
+
 // STREAMS: it may be that experts' weights are read past the caches.
 template <int TN, int TM, int WN, int WM, bool EXACT, bool STREAMS = false, bool STREAM = false, class Job>
 void launch_tile(const MatmulArgs &g, const Job &job, hipStream_t st) {
   typedef TileShape<TN, TM, WN, WM, EXACT> Shape;
   if constexpr (STREAMS && !STREAM) {
-    if (streams_weights(job.y_rows, job.experts, g.ldw * g.N, Shape::BM)) return launch_tile<TN, TM, WN, WM, EXACT, STREAMS, true>(g, job, st);
+    if (streams_weights(job, g, Shape::BM)) return launch_tile<TN, TM, WN, WM, EXACT, STREAMS, true>(g, job, st);
   }
   const int n_tiles = (g.N + Shape::BN - 1) / Shape::BN, m_tiles = (int)most_row_tiles(job, g, Shape::BM);
   const int per_xcd = (n_tiles * m_tiles + 7) / 8;
@@ -34,7 +38,7 @@ template <int TN, int TM, int WN, int WM, int KG, int NS, bool EXACT, bool STREA
 void launch_ring(const MatmulArgs &g, const Job &job, hipStream_t st) {
   typedef RingShape<TN, TM, WN, WM, KG, NS> Shape;
   if constexpr (STREAMS && !STREAM) {
-    if (streams_weights(job.y_rows, job.experts, g.ldw * g.N, Shape::BM)) return launch_ring<TN, TM, WN, WM, KG, NS, EXACT, STREAMS, true>(g, job, st);
+    if (streams_weights(job, g, Shape::BM)) return launch_ring<TN, TM, WN, WM, KG, NS, EXACT, STREAMS, true>(g, job, st);
   }
   const int n_tiles = (g.N + Shape::BN - 1) / Shape::BN, m_tiles = (int)most_row_tiles(job, g, Shape::BM);
   const int per_xcd = (n_tiles * m_tiles + 7) / 8;

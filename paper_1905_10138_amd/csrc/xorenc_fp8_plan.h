@@ -146,6 +146,15 @@ inline bool streams_weights(int64_t rows, int64_t experts, int64_t bytes_of_one,
   return bytes_of_one >= ((int64_t)96 << 20) / (rows < experts ? rows : experts) && rows <= experts * bm;
 }
 
+// What streams_weights counts of each expert: the bytes of its matrix, whatever lies between its rows, and none where experts share some of them (one matrix
+// for all, w_stride 0, or strides that let them overlap), as what one expert has read is there for the next.  Matrices are apart one after the other, or in
+// turn, a row of each.  (us, past the caches and through them: 128 tokens, two of eight experts that are one matrix of 4096 x 4096 32.0 and 25.1; that are
+// 4096 x 1024 in rows of 8192 15.3 and 11.3.)
+inline int64_t bytes_of_one_expert(int64_t experts, int64_t N, int64_t K, int64_t ldw, int64_t w_stride) {
+  const bool apart = experts == 1 || w_stride >= (N - 1) * ldw + K || (w_stride >= K && (experts - 1) * w_stride + K <= ldw);
+  return apart ? N * ((K + 15) / 16 * 16) : 0;
+}
+
 inline int cheapest_for_experts(int64_t rows, int64_t experts, int64_t N, int64_t blocks, bool exact) {
   const float all = (float)rows, used = (float)experts * (1.f - expf(-all / (float)experts));  // (experts that have rows)
   const float weights = used * (float)N * (float)blocks * 128e-6f;
