@@ -480,7 +480,8 @@ XORENC_API int32_t xorenc_gather_tokens(const void *X, int32_t x_dtype, int64_t 
 
 /*
  * Y[t] = sum over p of shares[t][p] R[places[t][p]] (shares NULL: of the rows alone), plus residual[t] unless that is NULL: in fp32, in the order of
- * p, the residual last.  Y and residual have R's type; Y may be residual.
+ * p, the residual last.  Y and residual have R's type; Y may be residual, with
+ * ldy = ld_residual (XORENC_EINVAL with another one).
  */
 XORENC_API int32_t xorenc_combine_tokens(const void *R, int32_t x_dtype, int64_t ldr, const int32_t *places, const int32_t *used,
                                          const float *shares, const void *residual, int64_t ld_residual, int32_t tokens, int32_t picks, int32_t cols,
@@ -500,7 +501,7 @@ XORENC_API int32_t xorenc_combine_tokens_grad(const void *dY, int32_t x_dtype, i
  * What a product does to its results before they are rounded, in fp32:  y = residual + f(z + bias).
  *   bias      DEV, fp32 or bf16 (bias_dtype), a value for each column of Y, contiguous, or NULL
  *   f         one of the below; erf in XORENC_GELU is the error function, XORENC_GELU_TANH has tanh(sqrt(2 / pi) (z + 0.044715 z^3)) in its place
- *   residual  DEV, the type of Y, or NULL; it may be Y
+ *   residual  DEV, the type of Y, or NULL; it may be Y, with ld_residual = ldy (XORENC_EINVAL with another one)
  */
 enum { XORENC_NO_ACTIVATION = 0, XORENC_RELU = 1, XORENC_SILU = 2, XORENC_GELU = 3, XORENC_GELU_TANH = 4 };
 typedef struct xorenc_epilogue {

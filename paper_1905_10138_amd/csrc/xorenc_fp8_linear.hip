@@ -12,6 +12,7 @@ extern "C" int32_t xorenc_linear_fp8(const uint8_t *A, int64_t lda, const float 
   Linear job;
   rc = read_epilogue(epilogue, N, y_dtype, true, &job.epilogue);
   if (rc != XORENC_OK || M == 0) return rc;
+  if (job.epilogue.residual && job.epilogue.residual == Y && job.epilogue.ld_residual != ldy && M > 1) return XORENC_EINVAL;
   if (job.epilogue.none()) return xorenc_matmul_fp8(A, lda, SA, sa_row, sa_blk, W, ldw, SW, ldsw, M, N, K, Y, y_dtype, ldy, hip_stream);
   const MatmulArgs g = arguments_of(A, lda, SA, sa_row, sa_blk, W, ldw, SW, ldsw, M, M, N, K, Y, ldy);
   hipStream_t st = static_cast<hipStream_t>(hip_stream);

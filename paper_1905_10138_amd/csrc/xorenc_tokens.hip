@@ -530,7 +530,7 @@ extern "C" int32_t xorenc_combine_tokens(const void *R, int32_t x_dtype, int64_t
                                          void *Y, int64_t ldy, void *hip_stream) {
   const int32_t rc = check_rows(x_dtype, tokens, picks, cols);
   if (rc != XORENC_OK) return rc;
-  if (ldr < cols || ldy < cols || (residual && ld_residual < cols)) return XORENC_EINVAL;
+  if (ldr < cols || ldy < cols || (residual && ld_residual < cols) || (residual && residual == Y && ld_residual != ldy && tokens > 1)) return XORENC_EINVAL;
   if (tokens == 0) return XORENC_OK;
   if (!R || !places || !used || !Y) return XORENC_EINVAL;
   const int esz = dtype_bytes(x_dtype);
