@@ -89,11 +89,12 @@ class ExpertLayer:
         return out
 
     def sorted_experts(self, n, Q, S):
-        """The same for many tokens, whose norms in 8 bits (Q, S) the products take; the router takes them in n's 16 bits."""
+        """The same for many tokens, whose norms in 8 bits (Q, S) the products take; the router takes n itself, and results have its type."""
         ids, shares = xe.pick_experts(n.float() @ self.router.float().t(), self.picks)
         places, tokens, offsets = xe.sort_tokens(ids, self.router.shape[0])
-        u = xe.experts_fp8(Q, S, *self.W13, offsets, tokens)
-        return xe.combine_tokens(xe.experts_fp8(*xe.silu_mul_fp8(u), *self.W2, offsets), places, offsets, shares)
+        u = xe.experts_fp8(Q, S, *self.W13, offsets, tokens, out_dtype=n.dtype)
+        d = xe.experts_fp8(*xe.silu_mul_fp8(u), *self.W2, offsets, out_dtype=n.dtype)
+        return xe.combine_tokens(d, places, offsets, shares)
 
     def __call__(self, x, r):
         Q, S, t, n = xe.add_rmsnorm_fp8(x, self.norm, r, normed=True)
