@@ -6,10 +6,11 @@
                                     many: matmul_fp8 on the copy that decode and quant_fp8 have made of it
     d = (silu(gate) * up) W2^T      silu_mul_fp8, matmul_fp8
     s = t + d                       add_rmsnorm_fp8
-    y = s + experts(norm(s))        few tokens: moe_fp8, 64 a call
-                                    many: pick_experts, sort_tokens, experts_fp8 (W13), silu_mul_fp8, experts_fp8 (W2), combine_tokens
+    y = s + experts(norm(s))        moe_fp8, 64 tokens a call, with activations in 16 bits
+                                    more than --most-unrounded tokens: pick_experts, sort_tokens, experts_fp8 (W13), silu_mul_fp8, experts_fp8 (W2),
+                                    combine_tokens, with activations in 8 bits
 
-    python examples/feed_forward.py [--config large_q1] [--tokens 1,8,64,1024] [--experts 8] [--picks 2]
+    python examples/feed_forward.py [--config large_q1] [--tokens 1,8,64,1024] [--experts 8] [--picks 2] [--most-unrounded 128]
 
 prints the time of a pass and how far its parts are from 64-bit arithmetic.  Inputs and weights are synthetic.
 """
@@ -31,9 +32,10 @@ from synth_inputs import CONFIGS, make_workload
 MOST_ENCRYPTED = 64
 
 
-# Tokens up to which the experts run in calls of 64 tokens, which round no activation to 8 bits: each call reads the weights of nearly all experts, and
-# takes as long as the sorted tokens' two products do for many more (8 experts of 4096 x 2048, two a token, us: 64 tokens 79 and 77, of which the router 31 in
-# fp32; 128 158 and 78; 1024 1258 and 136).  What the calls of 64 are for is their precision.
+# Tokens from which on the experts are faster sorted, with activations rounded to 8 bits twice (off by up to 0.05 in the 2-norm), than in calls of 64 tokens, which
+# round none: each call reads the weights of nearly all experts, and takes as long as the sorted tokens' two products do for many more (8 experts of 4096 x
+# 2048, two a token, us: 64 tokens 79 and 77, of which the router 31 in fp32; 128 158 and 78; 1024 1258 and 136).  Whoever makes the layer
+# chooses between time and precision.
 MOST_UNROUNDED = 128
 
 
@@ -74,10 +76,12 @@ class GatedLayer:
 
 
 class ExpertLayer:
-    """norm, router and experts: W13 (experts, 2 inner, hidden), W2 (experts, hidden, inner), given in 16 or 32 bits."""
+    """norm, router and experts: W13 (experts, 2 inner, hidden), W2 (experts, hidden, inner), given in 16 or 32 bits.
 
-    def __init__(self, router, W13, W2, norm, picks):
-        self.router, self.norm, self.picks = router, norm, picks
+    most_unrounded: the most tokens whose activations keep 16 bits; those of more are rounded to 8.  None: any number."""
+
+    def __init__(self, router, W13, W2, norm, picks, most_unrounded=None):
+        self.router, self.norm, self.picks, self.most_unrounded = router, norm, picks, most_unrounded
         self.W13 = xe.quant_fp8(W13, block_rows=xe.FP8_BLOCK)
         self.W2 = xe.quant_fp8(W2, block_rows=xe.FP8_BLOCK)
 
@@ -98,11 +102,12 @@ class ExpertLayer:
 
     def __call__(self, x, r):
         Q, S, t, n = xe.add_rmsnorm_fp8(x, self.norm, r, normed=True)
-        return t, self.experts(n) if n.shape[0] <= MOST_UNROUNDED else self.sorted_experts(n, Q, S)
+        unrounded = self.most_unrounded is None or n.shape[0] <= self.most_unrounded
+        return t, self.experts(n) if unrounded else self.sorted_experts(n, Q, S)
 
 
-def build(workload, experts, picks, inner, seed=0):
-    """Both layers: W13 of the first is the workload's matrix, the experts have `inner` inner features."""
+def build(workload, experts, picks, inner, seed=0, most_unrounded=MOST_UNROUNDED):
+    """Both layers: W13 of the first is the workload's matrix, the experts have `inner` inner features and most_unrounded."""
     g = torch.Generator(device="cuda").manual_seed(seed)
 
     def draw(*shape, scale=1.0, dtype=torch.bfloat16):
@@ -111,7 +116,7 @@ def build(workload, experts, picks, inner, seed=0):
     H, I = workload.n, workload.m // 2
     gated = GatedLayer(encrypt(workload), draw(H, I, scale=I ** -0.5), 1 + draw(H, scale=0.1, dtype=torch.float32))
     moe = ExpertLayer(draw(experts, H, scale=H ** -0.5), draw(experts, 2 * inner, H, scale=H ** -0.5),
-                      draw(experts, H, inner, scale=inner ** -0.5), 1 + draw(H, scale=0.1, dtype=torch.float32), picks)
+                      draw(experts, H, inner, scale=inner ** -0.5), 1 + draw(H, scale=0.1, dtype=torch.float32), picks, most_unrounded)
     return gated, moe, draw
 
 
@@ -147,8 +152,10 @@ def main():
     p.add_argument("--experts", type=int, default=8)
     p.add_argument("--picks", type=int, default=2)
     p.add_argument("--inner", type=int, default=2048)
+    p.add_argument("--most-unrounded", type=int, help="tokens up to which the experts' activations keep 16 bits (default: any number); "
+                   f"more than {MOST_UNROUNDED} are faster in 8")
     args = p.parse_args()
-    gated, moe, draw = build(make_workload(CONFIGS[args.config]), args.experts, args.picks, args.inner)
+    gated, moe, draw = build(make_workload(CONFIGS[args.config]), args.experts, args.picks, args.inner, most_unrounded=args.most_unrounded)
     for tokens in map(int, args.tokens.split(",")):
         x, r = draw(tokens, gated.encrypted.n), draw(tokens, gated.encrypted.n)
         for _ in range(3):
