@@ -524,7 +524,7 @@ XORENC_API int32_t xorenc_linear_fp8(const uint8_t *A, int64_t lda, const float 
  * rows: A holds each token once, a_rows of them), or i where rows is NULL (A is sorted, a_rows = the rows of Y).  W_e starts at W + e * w_stride bytes (a
  * multiple of 16), its scales at SW + e * sw_stride.  Y has y_rows rows, of which those from offsets[experts] on are left as they are.
  * No residual.  XORENC_ELIMIT as xorenc_matmul_fp8 with M = y_rows, beyond XORENC_MOE_MAX_EXPERTS, and with `rows` where a_rows * lda exceeds 2^31 - 256
- * or a_rows * sa_row + sa_blk * ceil(K / 128) 2^29.
+ * or a_rows * sa_row + sa_blk * ceil(K / 128) is 2^29 - 64 or more.
  */
 XORENC_API int32_t xorenc_experts_fp8(const uint8_t *A, int64_t lda, const float *SA, int64_t sa_row, int64_t sa_blk, int32_t a_rows,
                                       const int32_t *rows, const int32_t *offsets, int32_t experts, const uint8_t *W, int64_t ldw, int64_t w_stride,

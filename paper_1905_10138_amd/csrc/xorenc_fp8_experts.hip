@@ -22,8 +22,8 @@ extern "C" int32_t xorenc_experts_fp8(const uint8_t *A, int64_t lda, const float
   if (!offsets || a_rows == 0 || (!rows && a_rows != y_rows)) return XORENC_EINVAL;
   if (!aligned_to(offsets, 4) || !aligned_to(rows, 4) || (experts > 1 && w_stride % 16)) return XORENC_EALIGN;
   const MatmulArgs g = arguments_of(A, lda, SA, sa_row, sa_blk, W, ldw, SW, ldsw, y_rows, a_rows, N, K, Y, ldy);
-  // with `rows` every row of A and its scales are addressed with 32-bit offsets from the first
-  if (rows && (a_rows * lda > kMostTileBytes || a_rows * g.sa_row + sa_blk * g.blocks >= (1 << 29))) return XORENC_ELIMIT;
+  // with `rows` every row of A and its scales are addressed with 32-bit offsets from the first, and what is past the descriptors' extent reads as zero
+  if (rows && (a_rows * lda > kMostTileBytes || a_rows * g.sa_row + sa_blk * g.blocks >= kMostTileBytes / 4)) return XORENC_ELIMIT;
   job.offsets = offsets, job.rows = rows, job.w_stride = w_stride, job.sw_stride = sw_stride;
   job.experts = experts, job.a_rows = a_rows, job.y_rows = y_rows;
   hipStream_t st = static_cast<hipStream_t>(hip_stream);
