@@ -107,7 +107,8 @@ class ExpertLayer:
 
 
 def build(workload, experts, picks, inner, seed=0, most_unrounded=MOST_UNROUNDED):
-    """Both layers: W13 of the first is the workload's matrix, the experts have `inner` inner features and most_unrounded."""
+    """Both layers: W13 of the first is the workload's matrix, the experts have `inner` inner features, and the most_unrounded of
+    ExpertLayer."""
     g = torch.Generator(device="cuda").manual_seed(seed)
 
     def draw(*shape, scale=1.0, dtype=torch.bfloat16):

@@ -55,9 +55,10 @@ __device__ inline float times_logistic(float x, float u) {
 }
 
 // x times the normal distribution function, erfc(-x / sqrt 2) / 2.  For z >= 0, erfc(z) exp(z^2) is t Q(t) with t = 1 / (1 + p z); Q and p were fitted to the
-// function's values for 0 <= z <= 10 so that the largest relative error is least: 5.2e-6 (results of 16 bits, 0.1 % of their half step) and 2e-8.
-// Beyond, exp(-z^2) is 0.  As precise in the lower tail as anywhere (8192 x 16384 x 4096: 51 us beside a bias alone,
-// with the library's erfcf 145).
+// function's values for 0 <= z <= 10 so that the largest relative error of the fit is least: 5.2e-6 (results of 16 bits, 0.1 % of their half step) and 2e-8.
+// In fp32 arithmetic results of 32 bits are off by 5.5e-7 for x >= -2, and below by what rounding the exponential's argument makes, which grows with x^2: 1e-6
+// down to -4, 2.1e-6 to -6, 3.4e-6 to -9, 8e-6 to -13 (measured; results of 1e-37 there).  1 + erf, a difference, would leave no digit from -6 on.
+// Beyond, exp(-z^2) is 0.  (8192 x 16384 x 4096: 51 us beside a bias alone, with the library's erfcf 145.)
 template <bool EXACT>
 __device__ inline float gelu(float x) {
   const float e = __builtin_amdgcn_exp2f(x * (x * -0.72134752f));
